@@ -74,7 +74,7 @@ def draw(rng):
     kind = rng.choice(["loss", "loss_step", "loss_step", "distill", "distill_step", "embed", "embed_grad"])
     V = _round(rng, _log(rng, 1000, 160000), 80)
     if kind.startswith("loss"):
-        T, D = _round(rng, _log(rng, 1, 4096), 64), _round(rng, _log(rng, 64, 4096), 80)
+        T, D = _round(rng, _log(rng, 1, 4096), 80), _round(rng, _log(rng, 64, 4096), 80)
         T = min(T, 4096 if rng.random() < 0.5 else 4095)
         most = 4096 * 128256 * 4096 // 4
         return {"kind": kind, "T": max(1, min(T, most // (V * D))), "V": V, "D": min(D, 4096),
