@@ -380,6 +380,94 @@ int domino_mask_logits_noalloc(const void* logits_dev, int32_t dtype, int32_t ba
                                int64_t row_stride_elems, const uint32_t* mask_dev, int32_t* argmax_dev,
                                float* lse_dev, float* logprobs_dev, void* stream);
 
+/* ---- Losses over the vocabulary and the embedding ------------------------------
+ *
+ * Not steps of the paper: what training or distilling a model that answers
+ * under a grammar needs next to the masks (the proposer of speculation, Sec.
+ * 3.6, is such a model).  These calls need a handle with a device but no loaded
+ * vocabulary or automaton: n_tokens (V) is an argument, 1 <= V <= 2^24, and masks
+ * are [rows][ceil(V/32)] words as written by domino_step_mask; NULL allows
+ * every token.  Bits at or beyond V are ignored.  rows = 0 is allowed (a weight's
+ * gradient is then zero).  Scratch is the handle's and grows on demand: the
+ * first call at larger sizes must not run under a stream capture
+ * (DOMINO_E_INVALID_ARG; the calls that need no scratch are marked).  All sums
+ * are held in fp32 and every result is the same on every run.  A target, teacher
+ * id or token at or beyond V sets DOMINO_DEVERR_BAD_TOKEN and counts as below
+ * 0.  Inputs and outputs do not overlap unless said otherwise. */
+
+/* Cross entropy of target tokens under the masked softmax of hidden . weight^T,
+ * without keeping the logits:
+ *   x[t][v] = sum_d hidden[t][d] weight[v][d],
+ *   lse[t]  = log sum exp x[t][v] over the tokens that row t's mask allows
+ *             (-inf when it allows none),
+ *   loss[t] = lse[t] - x[t][targets[t]]; 0 for targets below 0 (no target, padding);
+ *             +inf where the mask excludes the target.
+ * hidden_dev [rows][hidden_stride] and weight_dev [n_tokens][weight_stride],
+ * bf16, strides in elements, at least dim; 1 <= dim <= 2^20.  Rows on 16-byte
+ * boundaries are read in place, others are first copied to scratch.  fp32:
+ * DOMINO_E_UNSUPPORTED.  Values are finite (a NaN in a hidden row makes that
+ * row's results NaN).  lse_dev may be NULL. */
+int domino_token_loss(domino_t h, const void* hidden_dev, int64_t hidden_stride, const void* weight_dev,
+                      int64_t weight_stride, int32_t dtype, int32_t rows, int32_t dim, int32_t n_tokens,
+                      const uint32_t* mask_dev, const int32_t* targets_dev, float* loss_dev, float* lse_dev,
+                      void* stream);
+
+/* Gradient of sum_t grad_loss[t] loss[t]; the other arguments as given to (and
+ * lse_dev as written by) domino_token_loss:
+ *   G[t][v] = grad_loss[t] (exp(x[t][v] - lse[t]) - [v = targets[t]]) for allowed v,
+ *   dhidden = G weight, dweight = G^T hidden, in bf16, both written whole.
+ * Rows without a target, or whose mask excludes it, have no gradient, whatever
+ * their hidden values or grad_loss.  The logits are computed again, in pieces of the
+ * vocabulary; G is rounded to bf16 before the two products, relative to the
+ * largest |grad_loss|. */
+int domino_token_loss_grad(domino_t h, const void* hidden_dev, int64_t hidden_stride, const void* weight_dev,
+                           int64_t weight_stride, int32_t dtype, int32_t rows, int32_t dim, int32_t n_tokens,
+                           const uint32_t* mask_dev, const int32_t* targets_dev, const float* lse_dev,
+                           const float* grad_loss_dev, void* dhidden_dev, int64_t dhidden_stride, void* dweight_dev,
+                           int64_t dweight_stride, void* stream);
+
+/* Distillation from a teacher's top logits.  Row t's list holds k entries
+ * (teacher_dev [rows][k] logits or log-probabilities of teacher_dtype, ids_dev
+ * [rows][k]); entries with an id below 0 are none, and so are those whose token
+ * the mask excludes or whose student logit is -inf; of equal ids the first
+ * counts.  With p = softmax(teacher / temperature) over the entries and q =
+ * softmax(logits / temperature) over the allowed tokens:
+ *   lse[t]  = log sum exp(logits / temperature),
+ *   loss[t] = temperature^2 sum_i p_i (ln p_i - ln q[id_i]); 0 without entries.
+ * logits_dev [rows][row_stride_elems] of dtype (fp32 or bf16), any alignment.
+ * 1 <= k <= 1024, temperature > 0 and finite, its inverse too.  lse_dev may be
+ * NULL.  Logits of masked tokens are not used.  Needs no scratch. */
+int domino_distill_loss(domino_t h, const void* logits_dev, int32_t dtype, int32_t rows, int64_t row_stride_elems,
+                        int32_t n_tokens, const uint32_t* mask_dev, const void* teacher_dev, int32_t teacher_dtype,
+                        const int32_t* ids_dev, int32_t k, float temperature, float* loss_dev, float* lse_dev,
+                        void* stream);
+
+/* Gradient of sum_t grad_loss[t] loss[t] for the logits:
+ *   dlogits[t][v] = grad_loss[t] temperature (q[v] - p of v's entry) for allowed v, else 0,
+ * in the logits' type; rows without entries are 0.  lse_dev as written by
+ * domino_distill_loss.  dlogits_dev may be logits_dev, with the same stride.
+ * Needs no scratch. */
+int domino_distill_grad(domino_t h, const void* logits_dev, int32_t dtype, int32_t rows, int64_t row_stride_elems,
+                        int32_t n_tokens, const uint32_t* mask_dev, const void* teacher_dev, int32_t teacher_dtype,
+                        const int32_t* ids_dev, int32_t k, float temperature, const float* lse_dev,
+                        const float* grad_loss_dev, void* dlogits_dev, int64_t dlogits_stride, void* stream);
+
+/* Embedding lookup: out[i] = scale * weight[tokens[i]], zeros for tokens below 0
+ * (domino_step_decode's -1).  weight_dev [n_tokens][weight_stride] and out_dev
+ * [n][out_stride] of dtype (fp32 or bf16).  Needs no scratch. */
+int domino_embed(domino_t h, const int32_t* tokens_dev, int32_t n, const void* weight_dev, int64_t weight_stride,
+                 int32_t dtype, int32_t n_tokens, int32_t dim, float scale, void* out_dev, int64_t out_stride,
+                 void* stream);
+
+/* Gradient of the table: dweight[v] = scale * the sum of grad[i] over the i with
+ * tokens[i] = v, in the order of the list, rounded once.  accumulate = 0: every
+ * row is written (zeros for tokens that do not occur); 1: added to what
+ * dweight_dev holds, and the other rows are not touched (a table that is the
+ * loss's weight too: domino_token_loss_grad first, then this). */
+int domino_embed_grad(domino_t h, const int32_t* tokens_dev, int32_t n, const void* grad_dev, int64_t grad_stride,
+                      int32_t dtype, int32_t n_tokens, int32_t dim, float scale, int32_t accumulate,
+                      void* dweight_dev, int64_t dweight_stride, void* stream);
+
 /* Synchronises `stream`, returns the sticky device error word (DOMINO_DEVERR_*
  * bits, 0 = none) in *code and clears it. */
 int domino_get_device_error(domino_t h, int32_t* code, void* stream);

@@ -15,6 +15,69 @@ from . import _binding as B
 from ._binding import DominoError, DTYPE_BF16, DTYPE_F32  # noqa: F401
 
 
+def _torch():
+    import torch
+    return torch
+
+
+def _dtype(x) -> int:
+    torch = _torch()
+    if x.dtype == torch.bfloat16:
+        return DTYPE_BF16
+    if x.dtype == torch.float32:
+        return DTYPE_F32
+    raise TypeError("float32 or bfloat16 expected")
+
+
+def _rows(x, what, dtype=None, cols=None, rows=None):
+    """x, a matrix of contiguous rows (of `dtype`, with `cols` columns and `rows` rows where given)."""
+    if x.dim() != 2 or (cols is not None and x.shape[1] != cols) or (rows is not None and x.shape[0] != rows):
+        raise ValueError(f"{what}: shape {tuple(x.shape)}")
+    if dtype is not None and x.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}")
+    if x.shape[1] > 1 and x.stride(1) != 1:
+        raise ValueError(f"{what} rows must be contiguous")
+    return x
+
+
+def _step(x) -> int:
+    """Elements from a row to the next; of at most one row, its length."""
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def _ints(x, shape, what):
+    if x.dtype != _torch().int32:
+        raise TypeError(f"{what} must be int32")
+    if tuple(x.shape) != tuple(shape) or not x.is_contiguous():
+        raise ValueError(f"{what}: {tuple(shape)} contiguous expected")
+
+
+def _floats(x, n, what):
+    if x.dtype != _torch().float32:
+        raise TypeError(f"{what} must be float32")
+    if x.numel() != n or not x.is_contiguous():
+        raise ValueError(f"{what}: {n} contiguous values expected")
+    return x
+
+
+def _mask(mask, rows, n_tokens):
+    if mask is not None and (tuple(mask.shape) != (rows, (n_tokens + 31) // 32) or mask.element_size() != 4
+                             or not mask.is_contiguous()):
+        raise ValueError("mask: one contiguous row of ceil(n_tokens / 32) 32-bit words per row expected")
+
+
+def _distill_args(logits, teacher, ids, mask):
+    _rows(logits, "logits")
+    rows, V = logits.shape
+    _rows(teacher, "teacher", rows=rows)
+    k = teacher.shape[1]
+    if not teacher.is_contiguous():
+        raise ValueError("teacher must be contiguous")
+    _ints(ids, (rows, k), "ids")
+    _mask(mask, rows, V)
+    return rows, V, k
+
+
 class Domino:
     """One library handle: a vocabulary plus a scanner (+ bracket rules).
 
@@ -192,6 +255,95 @@ class Domino:
         so = states if states_out is None else states_out
         B.domino_advance_table(self.h, table_next, states, tokens, states.shape[0], so, stream)
         return so
+
+    # -- losses over the vocabulary, the embedding (no loaded vocabulary needed) -----
+    def token_loss(self, hidden, weight, targets, mask=None, out=None, stream=None) -> Tuple:
+        """Cross entropy of `targets` under the masked softmax of hidden @ weight.T, the logits never kept: (loss,
+        lse), fp32 [rows].  hidden [rows, dim], weight [n_tokens, dim] bf16; targets int32 (below 0: none); mask as
+        step_mask's or None.  out: (loss, lse) to write to."""
+        hidden, weight = _rows(hidden, "hidden"), _rows(weight, "weight", hidden.dtype, hidden.shape[1])
+        rows = hidden.shape[0]
+        _ints(targets, (rows,), "targets")
+        _mask(mask, rows, weight.shape[0])
+        loss, lse = out if out is not None else (None, None)
+        if loss is None:
+            loss = self._empty(rows, _torch().float32, hidden.device)
+        if lse is None:
+            lse = self._empty(rows, _torch().float32, hidden.device)
+        B.domino_token_loss(self.h, hidden.data_ptr(), _step(hidden), weight.data_ptr(), _step(weight), _dtype(hidden),
+                            rows, hidden.shape[1], weight.shape[0], mask, targets, _floats(loss, rows, "loss"),
+                            _floats(lse, rows, "lse"), stream)
+        return loss, lse
+
+    def token_loss_grad(self, hidden, weight, targets, lse, grad_loss, mask=None, out=None, stream=None) -> Tuple:
+        """(dhidden, dweight) of sum(grad_loss * loss), lse as token_loss returned it; in the inputs' type."""
+        hidden, weight = _rows(hidden, "hidden"), _rows(weight, "weight", hidden.dtype, hidden.shape[1])
+        rows = hidden.shape[0]
+        _ints(targets, (rows,), "targets")
+        _mask(mask, rows, weight.shape[0])
+        dh, dw = out if out is not None else (None, None)
+        if dh is None:
+            dh = self._empty(tuple(hidden.shape), hidden.dtype, hidden.device)
+        if dw is None:
+            dw = self._empty(tuple(weight.shape), weight.dtype, weight.device)
+        _rows(dh, "dhidden", hidden.dtype, hidden.shape[1], rows)
+        _rows(dw, "dweight", weight.dtype, weight.shape[1], weight.shape[0])
+        B.domino_token_loss_grad(self.h, hidden.data_ptr(), _step(hidden), weight.data_ptr(), _step(weight),
+                                 _dtype(hidden), rows, hidden.shape[1], weight.shape[0], mask, targets,
+                                 _floats(lse, rows, "lse"), _floats(grad_loss, rows, "grad_loss"), dh.data_ptr(),
+                                 _step(dh), dw.data_ptr(), _step(dw), stream)
+        return dh, dw
+
+    def distill_loss(self, logits, teacher, ids, temperature: float = 1.0, mask=None, out=None, stream=None) -> Tuple:
+        """Divergence of the teacher's top logits (teacher, ids [rows, k]; ids below 0: no entry) from the masked
+        softmax of logits / temperature, times temperature^2: (loss, lse), fp32 [rows]."""
+        rows, V, k = _distill_args(logits, teacher, ids, mask)
+        loss, lse = out if out is not None else (None, None)
+        if loss is None:
+            loss = self._empty(rows, _torch().float32, logits.device)
+        if lse is None:
+            lse = self._empty(rows, _torch().float32, logits.device)
+        B.domino_distill_loss(self.h, logits.data_ptr(), _dtype(logits), rows, _step(logits), V, mask, teacher,
+                              _dtype(teacher), ids, k, temperature, _floats(loss, rows, "loss"),
+                              _floats(lse, rows, "lse"), stream)
+        return loss, lse
+
+    def distill_grad(self, logits, teacher, ids, temperature: float, lse, grad_loss, mask=None, out=None, stream=None):
+        """d sum(grad_loss * loss) / d logits, in the logits' type; out may be `logits` itself."""
+        rows, V, k = _distill_args(logits, teacher, ids, mask)
+        if out is None:
+            out = self._empty((rows, V), logits.dtype, logits.device)
+        _rows(out, "out", logits.dtype, V, rows)
+        B.domino_distill_grad(self.h, logits.data_ptr(), _dtype(logits), rows, _step(logits), V, mask, teacher,
+                              _dtype(teacher), ids, k, temperature, _floats(lse, rows, "lse"),
+                              _floats(grad_loss, rows, "grad_loss"), out.data_ptr(), _step(out), stream)
+        return out
+
+    def embed(self, tokens, weight, scale: float = 1.0, out=None, stream=None):
+        """scale * weight[tokens], zeros for tokens below 0: [n, dim] of the weight's type."""
+        weight = _rows(weight, "weight")
+        n, dim = tokens.shape[0], weight.shape[1]
+        _ints(tokens, (n,), "tokens")
+        if out is None:
+            out = self._empty((n, dim), weight.dtype, weight.device)
+        _rows(out, "out", weight.dtype, dim, n)
+        B.domino_embed(self.h, tokens, n, weight.data_ptr(), _step(weight), _dtype(weight), weight.shape[0], dim, scale,
+                       out.data_ptr(), _step(out), stream)
+        return out
+
+    def embed_grad(self, tokens, grad, n_tokens: int, scale: float = 1.0, into=None, stream=None):
+        """Gradient of the table [n_tokens, dim]: scale * the sums of grad's rows by token.  into: a gradient that the
+        sums are added to (the loss's, for a table that is its weight too)."""
+        grad = _rows(grad, "grad")
+        n, dim = grad.shape
+        _ints(tokens, (n,), "tokens")
+        dw = into
+        if dw is None:
+            dw = self._empty((n_tokens, dim), grad.dtype, grad.device)
+        _rows(dw, "into", grad.dtype, dim, n_tokens)
+        B.domino_embed_grad(self.h, tokens, n, grad.data_ptr(), _step(grad), _dtype(grad), n_tokens, dim, scale,
+                            0 if into is None else 1, dw.data_ptr(), _step(dw), stream)
+        return dw
 
     def device_error(self, stream=None) -> int:
         return B.domino_get_device_error(self.h, stream)

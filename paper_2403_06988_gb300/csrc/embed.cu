@@ -1,0 +1,430 @@
+// embed.cu -- rows of an embedding table for a list of tokens, and the table's
+// gradient (sm_103a).
+//
+//   out[i]  = scale W[tokens[i]]              zeros for tokens below 0
+//   dW[v]   = scale sum_{i: tokens[i] = v} g[i]
+//
+// Both are bound by HBM.  The gradient sorts the tokens (stable, so that a
+// row's sum always runs in the order of the list) and sums runs of equal
+// tokens in fp32: a CTA per chunk of the sorted list and stretch of columns; a
+// run that crosses chunks is kept in parts, which a second pass joins in order.
+#include <cooperative_groups.h>
+#include <cuda_bf16.h>
+
+#include <algorithm>
+
+#include "loss.h"
+#include "walk_common.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace domino {
+namespace {
+
+constexpr int kEmbedThreads = 256;
+constexpr int kEmbedUnroll = 4;
+
+template <bool BF16>
+__device__ __forceinline__ uint4 scaled(const uint4& u, float scale) {
+    uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (BF16) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float(w[i] << 16) * scale,
+                                                           __uint_as_float(w[i] & 0xFFFF0000u) * scale);
+            w[i] = *reinterpret_cast<const uint32_t*>(&b);
+        } else {
+            w[i] = __float_as_uint(__uint_as_float(w[i]) * scale);
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <bool BF16>
+__device__ __forceinline__ float value_at(const void* p, int64_t i) {
+    if constexpr (BF16) return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[i]);
+    else return reinterpret_cast<const float*>(p)[i];
+}
+template <bool BF16>
+__device__ __forceinline__ void put_at(void* p, int64_t i, float x) {
+    if constexpr (BF16) reinterpret_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(x);
+    else reinterpret_cast<float*>(p)[i] = x;
+}
+
+// A thread takes kEmbedUnroll pieces (16-byte vectors, or with !VEC single
+// values) of the output's `per_row` a row, a grid's width apart.
+template <bool BF16, bool VEC>
+__global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const EmbedArgs a, const uint32_t per_row, const int64_t pieces) {
+    pdl_wait();
+    pdl_trigger();
+    constexpr int kSize = BF16 ? 2 : 4;
+    const int64_t width = (int64_t)gridDim.x * kEmbedThreads;
+    int64_t at[kEmbedUnroll];
+    uint4 u[kEmbedUnroll];
+#pragma unroll
+    for (int j = 0; j < kEmbedUnroll; ++j) {
+        const int64_t i = (int64_t)blockIdx.x * kEmbedThreads + threadIdx.x + j * width;
+        at[j] = -1;
+        u[j] = make_uint4(0, 0, 0, 0);
+        if (i >= pieces) continue;
+        const uint32_t r = pieces <= UINT_MAX ? (uint32_t)i / per_row : (uint32_t)(i / per_row);
+        const uint32_t c = (uint32_t)(i - (int64_t)r * per_row);
+        const int32_t t = __ldg(a.tokens + r);
+        at[j] = (int64_t)r * a.out_stride + (int64_t)c * (VEC ? 16 / kSize : 1);
+        if (t >= 0 && t < a.n_tokens) {
+            const int64_t from = (int64_t)t * a.weight_stride + (int64_t)c * (VEC ? 16 / kSize : 1);
+            if constexpr (VEC) u[j] = __ldg(reinterpret_cast<const uint4*>((const char*)a.weight + from * kSize));
+            else u[j].x = __float_as_uint(value_at<BF16>(a.weight, from));
+        } else if (t >= a.n_tokens && c == 0) {
+            atomicOr(a.err, DOMINO_DEVERR_BAD_TOKEN);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < kEmbedUnroll; ++j) {
+        if (at[j] < 0) continue;
+        if constexpr (VEC) *reinterpret_cast<uint4*>((char*)a.out + at[j] * kSize) = scaled<BF16>(u[j], a.scale);
+        else put_at<BF16>(a.out, at[j], __uint_as_float(u[j].x) * a.scale);
+    }
+}
+
+// ---- the list sorted by token ---------------------------------------------------
+constexpr int kSortThreads = 1024;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kSortCtas = 8;               // one cluster
+constexpr int kSortBits = 8;               // at most, of a token id per pass
+constexpr int kSortBins = 1 << kSortBits;
+
+struct SortArgs {
+    const int32_t* tokens;
+    int32_t n, n_tokens;
+    int32_t passes, bits;      // bits per pass
+    int32_t ctas;
+    uint2* a;                  // [n] {token (n_tokens: none), place in the list}
+    uint2* b;                  // [n]
+    uint32_t* err;
+};
+
+// Stable least-significant-digit radix sort by one cluster.  The list is cut
+// into one strip per warp.  A pass counts the strips' digits, turns the counts
+// into places (all smaller digits first, then the same digit of earlier CTAs
+// and warps), and moves every strip in order.  The last pass ends in `a`.
+__global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortArgs s) {
+    __shared__ uint32_t count[kSortWarps][kSortBins];
+    __shared__ uint32_t total[kSortBins], base[kSortBins], warp_sum[kSortBins / 32];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
+    pdl_wait();
+    pdl_trigger();
+    const int64_t strips = (int64_t)s.ctas * kSortWarps, strip = (int64_t)cta * kSortWarps + warp;
+    const int32_t lo = (int32_t)(s.n * strip / strips), hi = (int32_t)(s.n * (strip + 1) / strips);
+    const uint32_t bins = 1u << s.bits, digit_mask = bins - 1u;
+    for (int pass = 0; pass < s.passes; ++pass) {
+        const int shift = pass * s.bits;
+        // passes alternate between the buffers, the last into `a`
+        uint2* to = (s.passes - pass) & 1 ? s.a : s.b;
+        const uint2* from = (s.passes - pass) & 1 ? s.b : s.a;
+        const auto entry = [&](int32_t i) {
+            if (pass) return from[i];
+            int32_t t = __ldg(s.tokens + i);
+            if (t >= s.n_tokens) atomicOr(s.err, DOMINO_DEVERR_BAD_TOKEN);
+            if (t < 0 || t >= s.n_tokens) t = s.n_tokens;
+            return make_uint2((uint32_t)t, (uint32_t)i);
+        };
+        for (uint32_t i = lane; i < bins; i += 32) count[warp][i] = 0u;
+        __syncwarp();
+        for (int32_t i = lo + lane; i < hi; i += 32) atomicAdd(&count[warp][(entry(i).x >> shift) & digit_mask], 1u);
+        __syncthreads();
+        if (tid < (int)bins) {   // before each warp's: the CTA's earlier warps'
+            uint32_t sum = 0;
+            for (int w = 0; w < kSortWarps; ++w) {
+                const uint32_t n = count[w][tid];
+                count[w][tid] = sum;
+                sum += n;
+            }
+            total[tid] = sum;
+        }
+        cluster.sync();
+        uint32_t all = 0, before = 0;
+        if (tid < (int)bins) {
+            for (int c = 0; c < s.ctas; ++c) {
+                const uint32_t n = *cluster.map_shared_rank(&total[tid], c);
+                all += n;
+                if (c < cta) before += n;
+            }
+        }
+        uint32_t scan = all;   // of the bins: smaller digits
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const uint32_t x = __shfl_up_sync(0xffffffffu, scan, off);
+            if (lane >= off) scan += x;
+        }
+        if (lane == 31 && warp < kSortBins / 32) warp_sum[warp] = scan;
+        __syncthreads();
+        if (tid < (int)bins) {
+            uint32_t smaller = scan - all;
+            for (int w = 0; w < warp; ++w) smaller += warp_sum[w];
+            base[tid] = smaller + before;
+        }
+        __syncthreads();
+        for (int32_t i0 = lo; i0 < hi; i0 += 32) {
+            const int32_t i = i0 + lane;
+            const bool on = i < hi;
+            uint2 e = make_uint2(0u, 0u);
+            if (on) e = entry(i);
+            const uint32_t d = on ? (e.x >> shift) & digit_mask : bins;
+            const uint32_t peers = __match_any_sync(0xffffffffu, d);
+            const uint32_t rank = __popc(peers & ((1u << lane) - 1u));
+            uint32_t place = 0;
+            if (on) place = base[d] + count[warp][d] + rank;
+            __syncwarp();
+            if (on && rank == 0) count[warp][d] += __popc(peers);
+            __syncwarp();
+            if (on) to[place] = e;
+        }
+        __threadfence();
+        cluster.sync();   // also: the others have read this CTA's totals
+    }
+}
+
+// ---- sums of runs -----------------------------------------------------------------
+constexpr int kSumThreads = 256;
+constexpr int kSumUnroll = 8;
+
+struct SumArgs {
+    EmbedArgs a;
+    const uint2* order;
+    int32_t chunk, chunks;
+    int32_t stretches;         // of the columns, kSumThreads pieces each
+    float* part;               // [chunks][2][dim]: the run that began before the chunk; the one that goes on after it
+};
+
+template <bool BF16, bool VEC>
+struct Piece {
+    static constexpr int kN = !VEC ? 1 : BF16 ? 8 : 4;
+    float v[kN];
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) v[i] = 0.0f;
+    }
+    __device__ __forceinline__ void add(const Piece& o) {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) v[i] += o.v[i];
+    }
+    __device__ __forceinline__ void load(const void* p, int64_t i) {
+        if constexpr (!VEC) {
+            v[0] = value_at<BF16>(p, i);
+        } else {
+            const uint4 u = __ldcs(reinterpret_cast<const uint4*>((const char*)p + i * (BF16 ? 2 : 4)));
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if constexpr (BF16) {
+                    v[2 * k] = __uint_as_float(w[k] << 16);
+                    v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+                } else {
+                    v[k] = __uint_as_float(w[k]);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void store(void* p, int64_t i) const {
+        if constexpr (!VEC) {
+            put_at<BF16>(p, i, v[0]);
+        } else {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if constexpr (BF16) {
+                    const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+                    w[k] = *reinterpret_cast<const uint32_t*>(&b);
+                } else {
+                    w[k] = __float_as_uint(v[k]);
+                }
+            }
+            *reinterpret_cast<uint4*>((char*)p + i * (BF16 ? 2 : 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+};
+
+// One row's sum is complete: scaled, with what dW holds where asked for, rounded once.
+template <bool BF16, bool VEC>
+__device__ __forceinline__ void finish_row(const EmbedArgs& a, uint32_t token, int32_t c, Piece<BF16, VEC> sum) {
+    const int64_t at = (int64_t)token * a.dweight_stride + c;
+#pragma unroll
+    for (int i = 0; i < sum.kN; ++i) sum.v[i] *= a.scale;
+    if (a.add) {
+        Piece<BF16, VEC> old;
+        old.load(a.dweight, at);
+        sum.add(old);
+    }
+    sum.store(a.dweight, at);
+}
+
+template <bool BF16, bool VEC>
+__global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs s) {
+    using P = Piece<BF16, VEC>;
+    const EmbedArgs& a = s.a;
+    pdl_wait();
+    pdl_trigger();
+    const int32_t chunk = blockIdx.x / s.stretches, stretch = blockIdx.x - chunk * s.stretches;
+    const int32_t c = (stretch * kSumThreads + threadIdx.x) * P::kN;
+    if (c >= a.dim) return;
+    const int32_t lo = chunk * s.chunk, hi = min(a.n, lo + s.chunk);
+    const uint32_t none = (uint32_t)a.n_tokens;
+    const uint32_t before = lo > 0 ? s.order[lo - 1].x : none, after = hi < a.n ? s.order[hi].x : none;
+    float* part = s.part + (int64_t)chunk * 2 * a.dim + c;
+    P sum;
+    sum.zero();
+    uint32_t token = s.order[lo].x;
+    bool first = true;   // the chunk's first run
+    const auto flush = [&](bool last) {
+        if (token == none) return;
+        if (first && token == before) {
+#pragma unroll
+            for (int i = 0; i < P::kN; ++i) part[i] = sum.v[i];
+        } else if (last && token == after) {
+#pragma unroll
+            for (int i = 0; i < P::kN; ++i) part[a.dim + i] = sum.v[i];
+        } else {
+            finish_row<BF16, VEC>(a, token, c, sum);
+        }
+    };
+    for (int32_t i0 = lo; i0 < hi; i0 += kSumUnroll) {
+        uint2 o[kSumUnroll];
+        P g[kSumUnroll];
+#pragma unroll
+        for (int j = 0; j < kSumUnroll; ++j) {
+            o[j] = i0 + j < hi ? s.order[i0 + j] : make_uint2(none, 0u);
+            g[j].zero();
+            if (o[j].x != none) g[j].load(a.grad, (int64_t)o[j].y * a.grad_stride + c);
+        }
+#pragma unroll
+        for (int j = 0; j < kSumUnroll; ++j) {
+            if (i0 + j >= hi) break;
+            if (o[j].x != token) {
+                flush(false);
+                first = false;
+                token = o[j].x;
+                sum.zero();
+            }
+            sum.add(g[j]);
+        }
+    }
+    flush(true);
+}
+
+// The runs that cross chunks: each by the CTAs of the chunk that it begins in.
+template <bool BF16, bool VEC>
+__global__ void __launch_bounds__(kSumThreads) join_kernel(const SumArgs s) {
+    using P = Piece<BF16, VEC>;
+    const EmbedArgs& a = s.a;
+    pdl_wait();
+    pdl_trigger();
+    const int32_t chunk = blockIdx.x / s.stretches, stretch = blockIdx.x - chunk * s.stretches;
+    const int32_t c = (stretch * kSumThreads + threadIdx.x) * P::kN;
+    const int32_t lo = chunk * s.chunk, hi = lo + s.chunk;
+    if (c >= a.dim || hi >= a.n) return;
+    const uint32_t token = s.order[hi - 1].x;
+    if (token == (uint32_t)a.n_tokens || s.order[hi].x != token) return;         // no run goes on after the chunk
+    if (s.order[lo].x == token && lo > 0 && s.order[lo - 1].x == token) return;   // it began before the chunk
+    P sum;
+    const float* part = s.part + (int64_t)chunk * 2 * a.dim + c;
+#pragma unroll
+    for (int i = 0; i < P::kN; ++i) sum.v[i] = part[a.dim + i];
+    for (int32_t k = chunk + 1; k < s.chunks; ++k) {
+        part += 2 * a.dim;
+        if (s.order[(int64_t)k * s.chunk].x != token) break;
+#pragma unroll
+        for (int i = 0; i < P::kN; ++i) sum.v[i] += part[i];
+    }
+    finish_row<BF16, VEC>(a, token, c, sum);
+}
+
+// ---- host --------------------------------------------------------------------------
+bool vectors_fit(const void* p, int64_t stride, int32_t dim, int size) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * size % 16 == 0 && (int64_t)dim * size % 16 == 0;
+}
+
+template <bool BF16, bool VEC>
+cudaError_t launch_rows(const EmbedArgs& a, cudaStream_t st) {
+    const uint32_t per_row = (uint32_t)(VEC ? a.dim * (BF16 ? 2 : 4) / 16 : a.dim);
+    const int64_t pieces = (int64_t)a.n * per_row;
+    const int64_t ctas = (pieces + kEmbedThreads * kEmbedUnroll - 1) / (kEmbedThreads * kEmbedUnroll);
+    if (ctas > INT_MAX) return cudaErrorInvalidValue;
+    return launch_pdl(embed_kernel<BF16, VEC>, dim3((unsigned)ctas), dim3(kEmbedThreads), 0, st, a, per_row, pieces);
+}
+
+struct EmbedSpace {
+    size_t a, b, part, end;
+    int32_t chunk, chunks;
+};
+EmbedSpace embed_space(const EmbedArgs& a) {
+    EmbedSpace s{};
+    s.chunk = 32;
+    while ((int64_t)s.chunk * 4096 < a.n) s.chunk *= 2;
+    s.chunks = (a.n + s.chunk - 1) / s.chunk;
+    const auto align = [](size_t n) { return (n + 255) & ~(size_t)255; };
+    s.b = align((size_t)a.n * sizeof(uint2));
+    s.part = 2 * s.b;
+    s.end = s.part + align((size_t)s.chunks * 2 * a.dim * 4);
+    return s;
+}
+
+template <bool BF16, bool VEC>
+cudaError_t launch_sums(const EmbedArgs& a, const SumArgs& in, cudaStream_t st) {
+    SumArgs s = in;
+    constexpr int kN = Piece<BF16, VEC>::kN;
+    s.stretches = (a.dim + kSumThreads * kN - 1) / (kSumThreads * kN);
+    const dim3 grid((unsigned)s.chunks * (unsigned)s.stretches);
+    cudaError_t e = launch_pdl(sum_kernel<BF16, VEC>, grid, dim3(kSumThreads), 0, st, s);
+    if (e != cudaSuccess || s.chunks == 1) return e;
+    return launch_pdl(join_kernel<BF16, VEC>, grid, dim3(kSumThreads), 0, st, s);
+}
+
+}  // namespace
+
+cudaError_t launch_embed(const EmbedArgs& a, const LaunchEnv&, cudaStream_t st) {
+    const bool bf16 = a.dtype == DOMINO_DTYPE_BF16;
+    const int size = bf16 ? 2 : 4;
+    const bool vec = vectors_fit(a.weight, a.weight_stride, a.dim, size) && vectors_fit(a.out, a.out_stride, a.dim, size);
+    if (bf16) return vec ? launch_rows<true, true>(a, st) : launch_rows<true, false>(a, st);
+    return vec ? launch_rows<false, true>(a, st) : launch_rows<false, false>(a, st);
+}
+
+size_t embed_workspace(const EmbedArgs& a, const LaunchEnv&) { return embed_space(a).end; }
+
+cudaError_t launch_embed_grad(const EmbedArgs& a, const LaunchEnv&, void* space, cudaStream_t st) {
+    const bool bf16 = a.dtype == DOMINO_DTYPE_BF16;
+    const int size = bf16 ? 2 : 4;
+    cudaError_t e = cudaSuccess;
+    if (!a.add)
+        e = cudaMemset2DAsync(a.dweight, (size_t)a.dweight_stride * size, 0, (size_t)a.dim * size, (size_t)a.n_tokens, st);
+    if (e != cudaSuccess || a.n == 0) return e;
+    const EmbedSpace sp = embed_space(a);
+    char* ws = (char*)space;
+    SortArgs so{};
+    so.tokens = a.tokens;
+    so.n = a.n;
+    so.n_tokens = a.n_tokens;
+    int bits = 1;   // of the ids 0..n_tokens
+    while ((a.n_tokens >> bits) > 0) ++bits;
+    so.passes = (bits + kSortBits - 1) / kSortBits;
+    so.bits = (bits + so.passes - 1) / so.passes;
+    so.ctas = kSortCtas;
+    while (so.ctas > 1 && a.n <= so.ctas / 2 * kSortThreads) so.ctas /= 2;
+    so.a = (uint2*)(ws + sp.a);
+    so.b = (uint2*)(ws + sp.b);
+    so.err = a.err;
+    if ((e = launch_cluster(sort_kernel, dim3((unsigned)so.ctas), dim3(kSortThreads), so.ctas, 0, st, so)) != cudaSuccess) return e;
+    SumArgs s{};
+    s.a = a;
+    s.order = so.a;
+    s.chunk = sp.chunk;
+    s.chunks = sp.chunks;
+    s.part = (float*)(ws + sp.part);
+    const bool vec = vectors_fit(a.grad, a.grad_stride, a.dim, size) && vectors_fit(a.dweight, a.dweight_stride, a.dim, size);
+    if (bf16) return vec ? launch_sums<true, true>(a, s, st) : launch_sums<true, false>(a, s, st);
+    return vec ? launch_sums<false, true>(a, s, st) : launch_sums<false, false>(a, s, st);
+}
+
+}  // namespace domino

@@ -18,6 +18,7 @@
 
 #include "domino.h"
 #include "domino_internal.h"
+#include "loss.h"
 
 using namespace domino;
 
@@ -58,7 +59,8 @@ struct domino_ctx {
     DevBuf d_head, d_info, d_tail_off, d_tail, d_pos_of, d_cls_start, d_eos_slot;
     DevBuf d_dense, d_sparse, d_accept, d_self, d_tok_cls;
     DevBuf d_err, d_fpart;
-    std::vector<DevBuf> fpart_old;   // outgrown ones: recorded graphs may still name them
+    DevBuf d_space;                  // scratch of the losses and the embedding's gradient
+    std::vector<DevBuf> fpart_old;   // outgrown ones (of d_fpart and d_space): recorded graphs may still name them
     bool arena_ready = false;
     // prefix tree of the class strings (domino_get_prefix_tree)
     std::vector<uint4> t_node;
@@ -138,7 +140,7 @@ void dev_free(DevBuf& b) {
 
 int64_t dev_bytes(const domino_ctx* h) {
     const DevBuf* all[] = {&h->d_head, &h->d_info, &h->d_tail_off, &h->d_tail, &h->d_pos_of, &h->d_cls_start,
-                           &h->d_eos_slot, &h->d_dense, &h->d_sparse, &h->d_accept, &h->d_self, &h->d_tok_cls, &h->d_err, &h->d_fpart, &h->s_logits, &h->s_mask, &h->s_io,
+                           &h->d_eos_slot, &h->d_dense, &h->d_sparse, &h->d_accept, &h->d_self, &h->d_tok_cls, &h->d_err, &h->d_fpart, &h->d_space, &h->s_logits, &h->s_mask, &h->s_io,
                            &h->o_prop, &h->o_rows, &h->o_count, &h->d_rnode, &h->d_rncls, &h->d_rdtok, &h->d_srec,
                            &h->d_srec_next, &h->d_rret, &h->d_rstart, &h->d_loop_of, &h->d_loopbits, &h->d_keeps,
                            &h->d_xrange, &h->d_exits, &h->d_trec};
@@ -169,18 +171,21 @@ int dev_upload(DevBuf& b, const void* src, size_t n) {
 
 int dev_reserve(DevBuf& b, size_t n) { return dev_upload(b, nullptr, n); }
 
-// The fused decode's partials, n bytes or more.  An outgrown buffer is kept
-// until the handle is destroyed: a graph that a caller recorded at a smaller
-// batch goes on using it.  Sizes at least double, so the outgrown ones take
-// no more than the buffer itself.
-int grow_fpart(domino_ctx* h, size_t n) {
-    if (h->d_fpart.n >= n) return DOMINO_OK;
+// A scratch buffer of n bytes or more.  An outgrown buffer is kept until the
+// handle is destroyed: a graph that a caller recorded at a smaller batch goes on
+// using it.  Sizes at least double, so the outgrown ones take no more than the
+// buffer itself.
+int grow_scratch(domino_ctx* h, DevBuf& of, size_t n) {
+    if (of.n >= n) return DOMINO_OK;
     DevBuf b;
-    if (int rc = dev_reserve(b, std::max(n, 2 * h->d_fpart.n))) return rc;
-    if (h->d_fpart.p) h->fpart_old.push_back(h->d_fpart);
-    h->d_fpart = b;
+    if (int rc = dev_reserve(b, std::max(n, 2 * of.n))) return rc;
+    if (of.p) h->fpart_old.push_back(of);
+    of = b;
     return DOMINO_OK;
 }
+
+// The fused decode's partials.
+int grow_fpart(domino_ctx* h, size_t n) { return grow_scratch(h, h->d_fpart, n); }
 
 bool is_host_only(const domino_ctx* h) { return h->device < 0; }
 
@@ -1077,7 +1082,7 @@ int domino_destroy(domino_t h) {
         DeviceGuard g(h->device);
         cudaDeviceSynchronize();
         DevBuf* all[] = {&h->d_head, &h->d_info, &h->d_tail_off, &h->d_tail, &h->d_pos_of, &h->d_cls_start,
-                         &h->d_eos_slot, &h->d_dense, &h->d_sparse, &h->d_accept, &h->d_self, &h->d_tok_cls, &h->d_err, &h->d_fpart, &h->s_logits, &h->s_mask, &h->s_io,
+                         &h->d_eos_slot, &h->d_dense, &h->d_sparse, &h->d_accept, &h->d_self, &h->d_tok_cls, &h->d_err, &h->d_fpart, &h->d_space, &h->s_logits, &h->s_mask, &h->s_io,
                          &h->o_prop, &h->o_rows, &h->o_count, &h->d_rnode, &h->d_rncls, &h->d_rdtok, &h->d_srec, &h->d_srec_next, &h->d_rret,
                          &h->d_rstart, &h->d_loop_of, &h->d_loopbits, &h->d_keeps, &h->d_xrange, &h->d_exits,
                          &h->d_trec};
@@ -1936,6 +1941,220 @@ int domino_decode_step_host(domino_t h, const void* logits_host, int32_t dtype, 
     return DOMINO_E_OOM;
 }
 
+
+// ---- losses over the vocabulary, the embedding --------------------------------------
+namespace {
+
+constexpr int32_t kMaxTokens = 1 << 24, kMaxDim = 1 << 20;
+
+bool is_dtype(int32_t t) { return t == DOMINO_DTYPE_F32 || t == DOMINO_DTYPE_BF16; }
+
+int device_handle(domino_ctx* h) {
+    if (!h) return DOMINO_E_INVALID_ARG;
+    return is_host_only(h) ? DOMINO_E_NO_DEVICE : DOMINO_OK;
+}
+
+// The handle's scratch, n bytes or more: allocating is not allowed while the
+// stream is captured.
+int loss_scratch(domino_ctx* h, size_t n, cudaStream_t st) {
+    if (h->d_space.n >= n) return DOMINO_OK;
+    cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(st, &cs) != cudaSuccess) return cuda_status(cudaGetLastError());
+    if (cs != cudaStreamCaptureStatusNone) return DOMINO_E_INVALID_ARG;
+    return grow_scratch(h, h->d_space, n);
+}
+
+int token_loss_args(LossArgs& a, domino_ctx* h, const void* hidden, int64_t hidden_stride, const void* weight,
+                    int64_t weight_stride, int32_t dtype, int32_t rows, int32_t dim, int32_t n_tokens,
+                    const uint32_t* mask, const int32_t* targets) {
+    if (int rc = device_handle(h)) return rc;
+    if (!is_dtype(dtype) || rows < 0 || dim < 1 || dim > kMaxDim || n_tokens < 1 || n_tokens > kMaxTokens ||
+        hidden_stride < dim || weight_stride < dim || !weight || (rows > 0 && (!hidden || !targets)))
+        return DOMINO_E_INVALID_ARG;
+    if (dtype != DOMINO_DTYPE_BF16) return DOMINO_E_UNSUPPORTED;
+    a = LossArgs{};
+    a.hidden = hidden;
+    a.hidden_stride = rows == 1 ? (dim + 7) / 8 * 8 : hidden_stride;   // one row has no next one
+    a.weight = weight;
+    a.weight_stride = n_tokens == 1 ? (dim + 7) / 8 * 8 : weight_stride;
+    a.rows = rows;
+    a.dim = dim;
+    a.n_tokens = n_tokens;
+    a.mask = mask;
+    a.targets = targets;
+    a.err = (uint32_t*)h->d_err.p;
+    return rows == 0 || loss_fits(a) ? DOMINO_OK : DOMINO_E_UNSUPPORTED;
+}
+
+int distill_args(DistillArgs& a, domino_ctx* h, const void* logits, int32_t dtype, int32_t rows, int64_t stride,
+                 int32_t n_tokens, const uint32_t* mask, const void* teacher, int32_t teacher_dtype,
+                 const int32_t* ids, int32_t k, float temperature) {
+    if (int rc = device_handle(h)) return rc;
+    if (!is_dtype(dtype) || !is_dtype(teacher_dtype) || rows < 0 || rows > INT32_MAX / 8 || n_tokens < 1 ||
+        n_tokens > kMaxTokens || stride < n_tokens || k < 1 || k > kDistillMaxK || !(temperature > 0.0f) ||
+        !std::isfinite(temperature) || !std::isfinite(1.0f / temperature) ||
+        (rows > 0 && (!logits || !teacher || !ids)))
+        return DOMINO_E_INVALID_ARG;
+    a = DistillArgs{};
+    a.logits = logits;
+    a.dtype = dtype;
+    a.stride = stride;
+    a.rows = rows;
+    a.n_tokens = n_tokens;
+    a.mask = mask;
+    a.teacher = teacher;
+    a.teacher_dtype = teacher_dtype;
+    a.ids = ids;
+    a.k = k;
+    a.temperature = temperature;
+    a.err = (uint32_t*)h->d_err.p;
+    return DOMINO_OK;
+}
+
+}  // namespace
+
+int domino_token_loss(domino_t h, const void* hidden_dev, int64_t hidden_stride, const void* weight_dev,
+                      int64_t weight_stride, int32_t dtype, int32_t rows, int32_t dim, int32_t n_tokens,
+                      const uint32_t* mask_dev, const int32_t* targets_dev, float* loss_dev, float* lse_dev,
+                      void* stream) try {
+    DOMINO_API_RANGE();
+    LossArgs a;
+    if (int rc = token_loss_args(a, h, hidden_dev, hidden_stride, weight_dev, weight_stride, dtype, rows, dim, n_tokens,
+                                 mask_dev, targets_dev))
+        return rc;
+    if (rows == 0) return DOMINO_OK;
+    if (!loss_dev) return DOMINO_E_INVALID_ARG;
+    a.loss = loss_dev;
+    a.lse = lse_dev;
+    DeviceGuard g(h->device);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (int rc = loss_scratch(h, loss_workspace(a, h->env, false), st)) return rc;
+    return cuda_status(launch_token_loss(a, h->env, h->d_space.p, st));
+} catch (...) {   // std::bad_alloc
+    return DOMINO_E_OOM;
+}
+
+int domino_token_loss_grad(domino_t h, const void* hidden_dev, int64_t hidden_stride, const void* weight_dev,
+                           int64_t weight_stride, int32_t dtype, int32_t rows, int32_t dim, int32_t n_tokens,
+                           const uint32_t* mask_dev, const int32_t* targets_dev, const float* lse_dev,
+                           const float* grad_loss_dev, void* dhidden_dev, int64_t dhidden_stride, void* dweight_dev,
+                           int64_t dweight_stride, void* stream) try {
+    DOMINO_API_RANGE();
+    LossArgs a;
+    if (int rc = token_loss_args(a, h, hidden_dev, hidden_stride, weight_dev, weight_stride, dtype, rows, dim, n_tokens,
+                                 mask_dev, targets_dev))
+        return rc;
+    if (dhidden_stride < dim || dweight_stride < dim || !dweight_dev ||
+        (rows > 0 && (!lse_dev || !grad_loss_dev || !dhidden_dev)))
+        return DOMINO_E_INVALID_ARG;
+    DeviceGuard g(h->device);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (rows == 0)
+        return cuda_status(cudaMemset2DAsync(dweight_dev, (size_t)dweight_stride * 2, 0, (size_t)dim * 2, (size_t)n_tokens, st));
+    a.lse = const_cast<float*>(lse_dev);
+    a.grad_loss = grad_loss_dev;
+    a.dhidden = dhidden_dev;
+    a.dhidden_stride = dhidden_stride;
+    a.dweight = dweight_dev;
+    a.dweight_stride = dweight_stride;
+    if (int rc = loss_scratch(h, loss_workspace(a, h->env, true), st)) return rc;
+    return cuda_status(launch_token_loss_grad(a, h->env, h->d_space.p, st));
+} catch (...) {   // std::bad_alloc
+    return DOMINO_E_OOM;
+}
+
+int domino_distill_loss(domino_t h, const void* logits_dev, int32_t dtype, int32_t rows, int64_t row_stride_elems,
+                        int32_t n_tokens, const uint32_t* mask_dev, const void* teacher_dev, int32_t teacher_dtype,
+                        const int32_t* ids_dev, int32_t k, float temperature, float* loss_dev, float* lse_dev,
+                        void* stream) {
+    DOMINO_API_RANGE();
+    DistillArgs a;
+    if (int rc = distill_args(a, h, logits_dev, dtype, rows, row_stride_elems, n_tokens, mask_dev, teacher_dev,
+                              teacher_dtype, ids_dev, k, temperature))
+        return rc;
+    if (rows == 0) return DOMINO_OK;
+    if (!loss_dev) return DOMINO_E_INVALID_ARG;
+    a.loss = loss_dev;
+    a.lse = lse_dev;
+    DeviceGuard g(h->device);
+    return cuda_status(launch_distill(a, h->env, false, (cudaStream_t)stream));
+}
+
+int domino_distill_grad(domino_t h, const void* logits_dev, int32_t dtype, int32_t rows, int64_t row_stride_elems,
+                        int32_t n_tokens, const uint32_t* mask_dev, const void* teacher_dev, int32_t teacher_dtype,
+                        const int32_t* ids_dev, int32_t k, float temperature, const float* lse_dev,
+                        const float* grad_loss_dev, void* dlogits_dev, int64_t dlogits_stride, void* stream) {
+    DOMINO_API_RANGE();
+    DistillArgs a;
+    if (int rc = distill_args(a, h, logits_dev, dtype, rows, row_stride_elems, n_tokens, mask_dev, teacher_dev,
+                              teacher_dtype, ids_dev, k, temperature))
+        return rc;
+    if (dlogits_stride < n_tokens || (logits_dev && dlogits_dev == logits_dev && dlogits_stride != row_stride_elems))
+        return DOMINO_E_INVALID_ARG;
+    if (rows == 0) return DOMINO_OK;
+    if (!lse_dev || !grad_loss_dev || !dlogits_dev) return DOMINO_E_INVALID_ARG;
+    a.lse = const_cast<float*>(lse_dev);
+    a.grad_loss = grad_loss_dev;
+    a.dlogits = dlogits_dev;
+    a.dstride = dlogits_stride;
+    DeviceGuard g(h->device);
+    return cuda_status(launch_distill(a, h->env, true, (cudaStream_t)stream));
+}
+
+int domino_embed(domino_t h, const int32_t* tokens_dev, int32_t n, const void* weight_dev, int64_t weight_stride,
+                 int32_t dtype, int32_t n_tokens, int32_t dim, float scale, void* out_dev, int64_t out_stride,
+                 void* stream) {
+    DOMINO_API_RANGE();
+    if (int rc = device_handle(h)) return rc;
+    if (!is_dtype(dtype) || n < 0 || n_tokens < 1 || n_tokens > kMaxTokens || dim < 1 || dim > kMaxDim ||
+        weight_stride < dim || out_stride < dim || (n > 0 && (!tokens_dev || !weight_dev || !out_dev)))
+        return DOMINO_E_INVALID_ARG;
+    if (n == 0) return DOMINO_OK;
+    EmbedArgs a{};
+    a.tokens = tokens_dev;
+    a.n = n;
+    a.n_tokens = n_tokens;
+    a.dim = dim;
+    a.dtype = dtype;
+    a.scale = scale;
+    a.weight = weight_dev;
+    a.weight_stride = weight_stride;
+    a.out = out_dev;
+    a.out_stride = out_stride;
+    a.err = (uint32_t*)h->d_err.p;
+    DeviceGuard g(h->device);
+    return cuda_status(launch_embed(a, h->env, (cudaStream_t)stream));
+}
+
+int domino_embed_grad(domino_t h, const int32_t* tokens_dev, int32_t n, const void* grad_dev, int64_t grad_stride,
+                      int32_t dtype, int32_t n_tokens, int32_t dim, float scale, int32_t accumulate,
+                      void* dweight_dev, int64_t dweight_stride, void* stream) try {
+    DOMINO_API_RANGE();
+    if (int rc = device_handle(h)) return rc;
+    if (!is_dtype(dtype) || n < 0 || n_tokens < 1 || n_tokens > kMaxTokens || dim < 1 || dim > kMaxDim ||
+        (accumulate != 0 && accumulate != 1) || grad_stride < dim || dweight_stride < dim || !dweight_dev ||
+        (n > 0 && (!tokens_dev || !grad_dev)))
+        return DOMINO_E_INVALID_ARG;
+    EmbedArgs a{};
+    a.tokens = tokens_dev;
+    a.n = n;
+    a.n_tokens = n_tokens;
+    a.dim = dim;
+    a.dtype = dtype;
+    a.scale = scale;
+    a.grad = grad_dev;
+    a.grad_stride = grad_stride;
+    a.dweight = dweight_dev;
+    a.dweight_stride = dweight_stride;
+    a.add = accumulate != 0;
+    a.err = (uint32_t*)h->d_err.p;
+    DeviceGuard g(h->device);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (int rc = n ? loss_scratch(h, embed_workspace(a, h->env), st) : DOMINO_OK) return rc;
+    return cuda_status(launch_embed_grad(a, h->env, h->d_space.p, st));
+} catch (...) {   // std::bad_alloc
+    return DOMINO_E_OOM;
+}
 
 int domino_get_device_error(domino_t h, int32_t* code, void* stream) {
     if (!h || !code) return DOMINO_E_INVALID_ARG;

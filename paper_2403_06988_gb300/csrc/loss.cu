@@ -1,0 +1,655 @@
+// loss.cu -- the cross entropy of target tokens under the masked softmax of
+// hidden . weight^T, and its gradient (sm_103a).  The logits [rows][V] are
+// never kept: their products are computed on the tensor cores tile by tile and
+// folded at once, and the gradient recomputes them in pieces of the
+// vocabulary.
+//
+//   x[t][v] = sum_d h[t][d] w[v][d]            A_t: the tokens the mask allows
+//   lse[t]  = log sum_{v in A_t} exp x[t][v]
+//   loss[t] = lse[t] - x[t][y_t]               0 without a target, +inf where
+//                                              the mask excludes the target
+//   G[t][v] = c_t (exp(x[t][v] - lse[t]) - [v = y_t]) for v in A_t, else 0
+//             c_t = grad_loss[t], 0 for rows without a finite loss
+//   dh      = G w          dw = G^T h
+//
+// product_kernel  one warp-specialised persistent kernel for all four products
+//                 (a tile of A B^T per step): TMA loads into a ring of
+//                 swizzled tiles, tcgen05.mma into two accumulators in tensor
+//                 memory, eight warps that fold one accumulator while the next
+//                 is filled.  What it does with a tile is its Fold.
+// loss_kernel     merges a row's partials into lse and loss.
+// coef_kernel, pack_kernel, dhidden_kernel: the rows' coefficients, operands
+//                 laid out for TMA, the sum of the hidden gradient's parts.
+#include <cuda_bf16.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "loss.h"
+#include "tcgen05.cuh"
+#include "walk_common.cuh"
+
+namespace domino {
+namespace {
+
+constexpr int kTileM = 128, kTileN = 256, kTileK = 64;
+constexpr int kStages = 4;
+constexpr int kAccs = 2;                       // accumulators of kTileN columns: all of tensor memory
+constexpr int kTmemColumns = kAccs * kTileN;
+constexpr int kBytesA = kTileM * kTileK * 2, kBytesB = kTileN * kTileK * 2;
+constexpr int kStageBytes = kBytesA + kBytesB;
+constexpr int kProductSmem = kStages * kStageBytes + 1024;   // tiles lie on 1024-byte boundaries
+constexpr int kFoldWarps = 8;
+constexpr int kProductThreads = 128 + 32 * kFoldWarps;
+constexpr int kFoldColumns = kTileN / (kFoldWarps / 4);      // a warp's: 32 rows, half of the columns
+constexpr int kGroupM = 16;                    // row tiles that share a pass over the columns' tiles
+
+// What becomes of a tile of products.
+enum ProductFold : int {
+    kFoldLogSum = 0,   // rows of tokens, columns of the vocabulary: (max, sum of exp) and the target's logit
+    kFoldGrad = 1,     // the same tile: G, in bf16
+    kFoldHidden = 2,   // G w: added to fp32 planes
+    kFoldWeight = 3,   // G^T h: the weight's gradient, in bf16
+};
+
+struct Product {
+    CUtensorMap a, b;
+    int32_t m, n;                  // valid rows and columns of the product
+    int32_t m_tiles, n_tiles, splits, k_blocks;   // k_blocks: of the whole sum, shared out over the splits
+    int32_t a_mn, b_mn;            // operands whose rows of memory run along k (MN-major)
+    int32_t items;                 // m_tiles * n_tiles * splits
+    // kFoldLogSum, kFoldGrad
+    const uint32_t* mask;          // at the first column's word; nullptr: everything allowed
+    int64_t mask_words;            // of a row
+    const int32_t* targets;
+    int32_t column0;               // token id of column 0
+    float2* part;                  // [m][part_pitch]
+    int32_t part_pitch;
+    float* target_logit;           // [m]
+    const float* lse;
+    const float* coef;             // c_t / scale
+    // outputs
+    __nv_bfloat16* out;            // kFoldGrad: G [m][ld]; kFoldWeight: [m][ld]
+    float* planes;                 // kFoldHidden: [splits][m][n]
+    int64_t ld;
+    const float* scale;
+    int32_t add;                   // kFoldHidden: to what the planes hold
+    int32_t vec;                   // rows of `out` lie on 16-byte boundaries
+    uint32_t* err;
+};
+
+struct Item {
+    int32_t m, n, k0, k1, split;
+};
+
+// Row tiles in groups of kGroupM; in a group the columns' tiles one after the
+// other, each with all of the group's row tiles: what CTAs read at a time is
+// one column tile and a group of row tiles.
+__device__ __forceinline__ Item item_at(const Product& p, int32_t i) {
+    Item t;
+    const int32_t tiles = p.m_tiles * p.n_tiles;
+    t.split = i / tiles;
+    i -= t.split * tiles;
+    const int32_t group = i / (kGroupM * p.n_tiles);
+    const int32_t m0 = group * kGroupM, rows = min(kGroupM, p.m_tiles - m0);
+    i -= group * kGroupM * p.n_tiles;
+    t.n = i / rows;
+    t.m = m0 + i - t.n * rows;
+    t.k0 = (int32_t)((int64_t)p.k_blocks * t.split / p.splits);
+    t.k1 = (int32_t)((int64_t)p.k_blocks * (t.split + 1) / p.splits);
+    return t;
+}
+
+// An operand's tile of `rows` m or n and kTileK k, from (r0, k0) on.
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, bool mn, int rows, int32_t r0,
+                                          int32_t k0, uint32_t bar) {
+    if (!mn) {
+        tma_load(dst, map, k0, r0, bar);
+    } else {
+        for (int c = 0; c < rows; c += 64) tma_load(dst + c * kTileK * 2, map, r0 + c, k0, bar);
+    }
+}
+
+// Bits of the columns [c, c + 32) of a row that are allowed and below n.
+__device__ __forceinline__ uint32_t allowed_word(const uint32_t* mrow, int32_t c, int32_t n) {
+    if (c >= n) return 0u;
+    const uint32_t word = mrow ? __ldg(mrow + (c >> 5)) : 0xFFFFFFFFu;
+    return n - c < 32 ? word & ((1u << (n - c)) - 1u) : word;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// 32 values from column c on of a row of bf16, those below n.
+__device__ __forceinline__ void store_bf16(__nv_bfloat16* row, int32_t c, int32_t n, bool vec, const float (&v)[32]) {
+    if (vec && c + 32 <= n) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 8)
+            *reinterpret_cast<uint4*>(row + c + i) = make_uint4(pack_bf16(v[i], v[i + 1]), pack_bf16(v[i + 2], v[i + 3]),
+                                                                pack_bf16(v[i + 4], v[i + 5]), pack_bf16(v[i + 6], v[i + 7]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (c + i < n) row[c + i] = __float2bfloat16_rn(v[i]);
+    }
+}
+
+template <int FOLD>
+__global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ Product p) {
+    extern __shared__ unsigned char smem[];
+    __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_acc_full[kAccs], s_acc_empty[kAccs], s_done;
+    __shared__ uint32_t s_tmem, s_failed;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t tiles = (smem_addr(smem) + 1023u) & ~1023u;
+    volatile uint32_t* failed = &s_failed;
+    if (threadIdx.x == 0) {
+        s_failed = 0u;
+        for (int s = 0; s < kStages; ++s) {
+            bar_init(smem_addr(&s_full[s]), 1);
+            bar_init(smem_addr(&s_empty[s]), 1);
+        }
+        for (int s = 0; s < kAccs; ++s) {
+            bar_init(smem_addr(&s_acc_full[s]), 1);
+            bar_init(smem_addr(&s_acc_empty[s]), kFoldWarps);
+        }
+        bar_init(smem_addr(&s_done), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+        tma_prefetch_map(&p.a);
+        tma_prefetch_map(&p.b);
+    }
+    if (warp == 2) tmem_alloc(smem_addr(&s_tmem), kTmemColumns);
+    tcgen_before();
+    __syncthreads();
+    tcgen_after();
+    const uint32_t tmem = s_tmem;
+    pdl_wait();
+    pdl_trigger();
+
+    if (warp == 0) {   // ---- loads
+        if (lane == 0) {
+            uint32_t loads = 0;
+            bool ok = true;
+            for (int32_t i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
+                const Item t = item_at(p, i);
+                for (int32_t k = t.k0; k < t.k1; ++k, ++loads) {
+                    const uint32_t s = loads % kStages, turn = loads / kStages;
+                    if (!(ok = bar_wait(smem_addr(&s_empty[s]), (turn & 1u) ^ 1u, failed))) break;
+                    const uint32_t full = smem_addr(&s_full[s]), a = tiles + s * kStageBytes;
+                    bar_expect(full, kStageBytes);
+                    load_tile(a, &p.a, p.a_mn, kTileM, t.m * kTileM, k * kTileK, full);
+                    load_tile(a + kBytesA, &p.b, p.b_mn, kTileN, t.n * kTileN, k * kTileK, full);
+                }
+            }
+            // given up: the loads on their way write into this CTA's memory
+            if (!ok)
+                for (uint32_t s = 0; s < kStages && s < loads; ++s) {
+                    const uint32_t last = loads - 1 - s;   // the stages' last loads
+                    const uint64_t end = timer_ns() + kWaitNs;
+                    while (!bar_try(smem_addr(&s_full[last % kStages]), (last / kStages) & 1u) && timer_ns() < end) {}
+                }
+        }
+    } else if (warp == 1) {   // ---- products
+        if (lane == 0) {
+            const uint32_t desc = mma_desc(kTileM, kTileN, p.a_mn, p.b_mn);
+            // 16 k further: 32 bytes along a row of a K-major tile, 16 rows of an MN-major one (16-byte units)
+            const uint32_t step_a = p.a_mn ? 2048 / 16 : 32 / 16, step_b = p.b_mn ? 2048 / 16 : 32 / 16;
+            uint32_t loads = 0, accs = 0;
+            bool ok = true;
+            for (int32_t i = blockIdx.x; i < p.items && ok; i += gridDim.x, ++accs) {
+                const Item t = item_at(p, i);
+                const uint32_t s_acc = accs % kAccs, acc = tmem + s_acc * kTileN;
+                if (!(ok = bar_wait(smem_addr(&s_acc_empty[s_acc]), ((accs / kAccs) & 1u) ^ 1u, failed))) break;
+                tcgen_after();
+                for (int32_t k = t.k0; k < t.k1; ++k, ++loads) {
+                    const uint32_t s = loads % kStages;
+                    if (!(ok = bar_wait(smem_addr(&s_full[s]), (loads / kStages) & 1u, failed))) break;
+                    tcgen_after();
+                    const uint64_t a = operand_desc(tiles + s * kStageBytes, kTileK * 128);
+                    const uint64_t b = operand_desc(tiles + s * kStageBytes + kBytesA, kTileK * 128);
+#pragma unroll
+                    for (int j = 0; j < kTileK / 16; ++j)
+                        mma_bf16(acc, a + (uint64_t)(j * step_a), b + (uint64_t)(j * step_b), desc, k > t.k0 || j > 0);
+                    mma_commit(smem_addr(&s_empty[s]));
+                }
+                if (ok) mma_commit(smem_addr(&s_acc_full[s_acc]));
+            }
+            // no product may be on its way when tensor memory is given back
+            mma_commit(smem_addr(&s_done));
+            const uint64_t end = timer_ns() + kWaitNs;
+            while (!bar_try(smem_addr(&s_done), 0u) && timer_ns() < end) {}
+        }
+    } else if (warp >= 4) {   // ---- folds
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        uint32_t accs = 0;
+        for (int32_t i = blockIdx.x; i < p.items; i += gridDim.x, ++accs) {
+            const Item t = item_at(p, i);
+            const uint32_t s_acc = accs % kAccs;
+            const int32_t row = t.m * kTileM + quarter * 32 + lane, c0 = t.n * kTileN + half * kFoldColumns;
+            const bool on = row < p.m;
+            // what the fold needs beside the products
+            constexpr int kWords = kFoldColumns / 32;
+            uint32_t word[kWords];
+            int32_t target = -1;
+            float lse = 0.0f, coef = 0.0f, scale = 0.0f;
+            if constexpr (FOLD == kFoldLogSum || FOLD == kFoldGrad) {
+                const uint32_t* mrow = p.mask && on ? p.mask + (int64_t)row * p.mask_words : nullptr;
+#pragma unroll
+                for (int j = 0; j < kWords; ++j) word[j] = on ? allowed_word(mrow, c0 + 32 * j, p.n) : 0u;
+                if (on) target = __ldg(p.targets + row) - p.column0;
+                if (FOLD == kFoldGrad && on) {
+                    lse = p.lse[row];
+                    coef = p.coef[row];
+                }
+            }
+            if constexpr (FOLD == kFoldWeight) scale = *p.scale;
+            // the whole warp goes on or leaves: loads from tensor memory are a warp's
+            if (!__all_sync(0xffffffffu, bar_wait(smem_addr(&s_acc_full[s_acc]), (accs / kAccs) & 1u, failed))) break;
+            tcgen_after();
+            const uint32_t acc = tmem + s_acc * kTileN + half * kFoldColumns + ((uint32_t)(quarter * 32) << 16);
+            float m = -INFINITY, sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) {
+                float v[32];
+                tmem_load32(v, acc + 32 * j);
+                const int32_t c = c0 + 32 * j;
+                if constexpr (FOLD == kFoldLogSum) {
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        if (!((word[j] >> e) & 1u)) v[e] = -INFINITY;
+                        else if (c + e == target) p.target_logit[row] = v[e];
+                        top = fmaxf(top, v[e]);
+                    }
+                    const float m2 = fmaxf(m, top), ref = sum_ref(m2);
+                    sum *= exp_diff(m, ref);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) sum += exp_diff(v[e], ref);
+                    m = m2;
+                } else if constexpr (FOLD == kFoldGrad) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const float q = exp_diff(v[e], lse) - (c + e == target ? 1.0f : 0.0f);
+                        v[e] = coef != 0.0f && ((word[j] >> e) & 1u) ? q * coef : 0.0f;
+                    }
+                    // columns beyond the vocabulary, up to the tile's end, are written as zeros: they are read again
+                    if (on) store_bf16(p.out + (int64_t)row * p.ld, c, (int32_t)p.ld, true, v);
+                } else if constexpr (FOLD == kFoldHidden) {
+                    // a split of a short piece may have no products: its accumulator holds an earlier tile's
+                    float* out = p.planes + ((int64_t)t.split * p.m + row) * p.n + c;
+                    if (on) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (c + e < p.n) {
+                                const float x = t.k0 < t.k1 ? v[e] : 0.0f;
+                                out[e] = p.add ? out[e] + x : x;
+                            }
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] *= scale;
+                    if (on) store_bf16(p.out + (int64_t)row * p.ld, c, p.n, p.vec, v);
+                }
+            }
+            if constexpr (FOLD == kFoldLogSum) {
+                if (on) p.part[(int64_t)row * p.part_pitch + t.n * (kTileN / kFoldColumns) + half] = make_float2(m, sum);
+            }
+            tcgen_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_addr(&s_acc_empty[s_acc]));
+        }
+    }
+    __syncwarp();
+    tcgen_before();
+    __syncthreads();
+    tcgen_after();
+    if (warp == 2) tmem_free(tmem, kTmemColumns);
+    if (threadIdx.x == 0 && *failed) atomicOr(p.err, DOMINO_DEVERR_INTERNAL);
+}
+
+// Whether row t's loss is finite by its target and mask.  report: a target
+// beyond the vocabulary sets the error word.
+__device__ __forceinline__ bool has_target(const int32_t* targets, const uint32_t* mask, int64_t W, int32_t V, int32_t t,
+                                           uint32_t* report, bool* excluded) {
+    const int32_t y = __ldg(targets + t);
+    *excluded = false;
+    if (y < 0) return false;
+    if (y >= V) {
+        if (report) atomicOr(report, DOMINO_DEVERR_BAD_TOKEN);
+        return false;
+    }
+    if (mask && !((__ldg(mask + t * W + (y >> 5)) >> (y & 31)) & 1u)) {
+        *excluded = true;
+        return false;
+    }
+    return true;
+}
+
+constexpr int kMergeThreads = 256;
+
+// A warp per row: its partials, each a (max, sum of exp against it), into lse.
+__global__ void __launch_bounds__(kMergeThreads)
+    loss_kernel(const float2* part, int32_t parts, int32_t pitch, const float* target_logit, const int32_t* targets,
+                const uint32_t* mask, int32_t rows, int32_t V, float* loss, float* lse, uint32_t* err) {
+    pdl_wait();
+    pdl_trigger();
+    const int32_t row = blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (row >= rows) return;
+    float m = -INFINITY, s = 0.0f;
+    for (int32_t i = lane; i < parts; i += 32) {
+        const float2 a = part[(int64_t)row * pitch + i];
+        const float m2 = fmaxf(m, a.x), ref = sum_ref(m2);
+        s = s * exp_diff(m, ref) + a.y * exp_diff(a.x, ref);
+        m = m2;
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+        const float mo = __shfl_xor_sync(0xffffffffu, m, off), so = __shfl_xor_sync(0xffffffffu, s, off);
+        const float m2 = fmaxf(m, mo), ref = sum_ref(m2);
+        s = s * exp_diff(m, ref) + so * exp_diff(mo, ref);
+        m = m2;
+    }
+    if (lane == 0) {
+        // no number among the row's logits: none comes out
+        const float z = isnan(s) ? s : log_sum_exp(m, s);
+        bool excluded;
+        const bool target = has_target(targets, mask, (V + 31) / 32, V, row, err, &excluded);
+        if (lse) lse[row] = z;
+        loss[row] = target ? z - target_logit[row] : excluded ? INFINITY : 0.0f;
+    }
+}
+
+constexpr int kCoefThreads = 1024;
+
+// The rows' coefficients over the largest finite one's magnitude: what G is
+// rounded from.  G is kept in bf16, so a coefficient that all rows share (a
+// mean's 1 / rows) would otherwise be off by one rounding, the same in every
+// entry; the scale is given back in fp32.
+__global__ void __launch_bounds__(kCoefThreads)
+    coef_kernel(const int32_t* targets, const uint32_t* mask, const float* grad_loss, int32_t rows, int32_t V, float* coef,
+                float* scale, uint32_t* err) {
+    __shared__ float s_top[kCoefThreads / 32];
+    pdl_wait();
+    pdl_trigger();
+    float top = 0.0f;
+    for (int32_t t = threadIdx.x; t < rows; t += kCoefThreads) {
+        bool excluded;
+        const float c = has_target(targets, mask, (V + 31) / 32, V, t, err, &excluded) ? __ldg(grad_loss + t) : 0.0f;
+        coef[t] = c;
+        if (fabsf(c) <= FLT_MAX) top = fmaxf(top, fabsf(c));
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    if ((threadIdx.x & 31) == 0) s_top[threadIdx.x >> 5] = top;
+    __syncthreads();
+    top = 0.0f;
+    for (int w = 0; w < kCoefThreads / 32; ++w) top = fmaxf(top, s_top[w]);
+    if (top == 0.0f) top = 1.0f;
+    if (threadIdx.x == 0) *scale = top;
+    for (int32_t t = threadIdx.x; t < rows; t += kCoefThreads) coef[t] = coef[t] / top;
+}
+
+constexpr int kPackThreads = 256;
+
+// Rows of bf16 into rows of `pitch` (a multiple of 8: what TMA can read).
+// coef: rows whose coefficient is 0 become zeros, so that what stands in rows
+// without a gradient (a padding's NaN) meets no other row.
+__global__ void __launch_bounds__(kPackThreads)
+    pack_kernel(const __nv_bfloat16* src, int64_t stride, int32_t rows, int32_t cols, __nv_bfloat16* dst, int64_t pitch,
+                const float* coef, bool vec) {
+    pdl_wait();
+    pdl_trigger();
+    for (int32_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        const bool zero = coef && coef[r] == 0.0f;
+        const __nv_bfloat16* from = src + (int64_t)r * stride;
+        __nv_bfloat16* to = dst + (int64_t)r * pitch;
+        if (vec) {
+            for (int32_t c = threadIdx.x * 8; c < cols; c += kPackThreads * 8)
+                *reinterpret_cast<uint4*>(to + c) = zero ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(from + c));
+        } else {
+            for (int32_t c = threadIdx.x; c < cols; c += kPackThreads) to[c] = zero ? __float2bfloat16_rn(0.0f) : from[c];
+        }
+    }
+}
+
+// dhidden = scale * the sum of the planes, in their order.
+__global__ void __launch_bounds__(kPackThreads)
+    dhidden_kernel(const float* planes, int32_t splits, int32_t rows, int32_t cols, const float* scale, __nv_bfloat16* out,
+                   int64_t ld) {
+    pdl_wait();
+    pdl_trigger();
+    const int64_t n = (int64_t)rows * cols;
+    const float s = *scale;
+    for (int64_t i = (int64_t)blockIdx.x * kPackThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kPackThreads) {
+        float v = 0.0f;
+        for (int k = 0; k < splits; ++k) v += planes[k * n + i];
+        const int64_t r = i / cols;
+        out[r * ld + (i - r * cols)] = __float2bfloat16_rn(s * v);
+    }
+}
+
+// ---- host --------------------------------------------------------------------
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+    static const EncodeTiled f = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            p = nullptr;
+        }
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return f;
+}
+
+// A [rows][cols] bf16 matrix, rows `pitch` elements apart, read in boxes of 64
+// columns (128 bytes, swizzled) and `box_rows` rows; zeros outside.
+cudaError_t make_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t pitch, int box_rows) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return cudaErrorNotSupported;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, steps,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+void cut_product(Product& p, int32_t m, int32_t n, int64_t k, int splits) {
+    p.m = m;
+    p.n = n;
+    p.m_tiles = ceil_div(m, kTileM);
+    p.n_tiles = ceil_div(n, kTileN);
+    p.k_blocks = ceil_div(k, kTileK);
+    p.splits = splits;
+    p.items = p.m_tiles * p.n_tiles * splits;
+}
+
+template <int FOLD>
+cudaError_t product_smem_ready() {
+    constexpr int kDevices = 64;
+    static std::atomic<bool> ready[kDevices];   // one array per fold
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || (dev < kDevices && ready[dev].load())) return e;
+    e = cudaFuncSetAttribute(product_kernel<FOLD>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
+    if (e == cudaSuccess && dev < kDevices) ready[dev].store(true);
+    return e;
+}
+
+template <int FOLD>
+cudaError_t launch_product(const LaunchEnv& env, const Product& p, cudaStream_t st) {
+    if (cudaError_t e = product_smem_ready<FOLD>(); e != cudaSuccess) return e;
+    return launch_pdl(product_kernel<FOLD>, dim3((unsigned)std::min(p.items, env.num_sms)), dim3(kProductThreads),
+                      kProductSmem, st, p);
+}
+
+cudaError_t launch_pack(const LaunchEnv& env, const void* src, int64_t stride, int32_t rows, int32_t cols, void* dst,
+                        int64_t pitch, const float* coef, cudaStream_t st) {
+    const bool vec = reinterpret_cast<uintptr_t>(src) % 16 == 0 && stride % 8 == 0 && cols % 8 == 0;
+    return launch_pdl(pack_kernel, dim3((unsigned)std::min(rows, env.num_sms * 8)), dim3(kPackThreads), 0, st,
+                      (const __nv_bfloat16*)src, stride, rows, cols, (__nv_bfloat16*)dst, pitch, coef, vec);
+}
+
+bool tma_ready(const void* p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0; }
+
+// Where a call's parts lie in its workspace.
+struct LossSpace {
+    size_t hidden, weight, part, target_logit, coef, scale, grad, planes, end;
+    int64_t pitch;        // of packed rows
+    int32_t part_pitch;
+    int32_t piece;        // tokens of the vocabulary at a time (gradient)
+    int32_t splits;       // of the hidden gradient's sum
+};
+
+// G takes at most this many bytes at a time.
+constexpr int64_t kGradBytes = (int64_t)256 << 20;
+
+LossSpace loss_space(const LossArgs& a, const LaunchEnv& env, bool grad) {
+    LossSpace s{};
+    s.pitch = (a.dim + 7) / 8 * 8;
+    size_t at = 0;
+    const auto take = [&](size_t n) {
+        const size_t p = at;
+        at += align256(n);
+        return p;
+    };
+    if (grad || !tma_ready(a.hidden, a.hidden_stride)) s.hidden = take((size_t)a.rows * s.pitch * 2);
+    if (!tma_ready(a.weight, a.weight_stride)) s.weight = take((size_t)a.n_tokens * s.pitch * 2);
+    if (!grad) {
+        s.part_pitch = ceil_div(a.n_tokens, kTileN) * (kTileN / kFoldColumns);
+        s.part = take((size_t)a.rows * s.part_pitch * sizeof(float2));
+        s.target_logit = take((size_t)a.rows * 4);
+    } else {
+        s.coef = take((size_t)a.rows * 4);
+        s.scale = take(4);
+        const int64_t most = std::max<int64_t>(kTileN, kGradBytes / 2 / a.rows / kTileN * kTileN);
+        const int pieces = ceil_div(a.n_tokens, most);
+        s.piece = ceil_div(ceil_div(a.n_tokens, pieces), kTileN) * kTileN;
+        s.grad = take((size_t)a.rows * s.piece * 2);
+        // few tiles: their sums are split, each part into a plane of its own
+        const int64_t tiles = (int64_t)ceil_div(a.rows, kTileM) * ceil_div(a.dim, kTileN);
+        s.splits = (int)std::max<int64_t>(1, std::min<int64_t>(env.num_sms / tiles, s.piece / kTileK / 4));
+        s.planes = take((size_t)s.splits * a.rows * a.dim * 4);
+    }
+    s.end = at;
+    return s;
+}
+
+}  // namespace
+
+size_t loss_workspace(const LossArgs& a, const LaunchEnv& env, bool grad) { return loss_space(a, env, grad).end; }
+
+bool loss_fits(const LossArgs& a) {
+    // tiles are counted in 32 bits
+    return (int64_t)ceil_div(a.rows, kTileM) * ceil_div(std::max(a.n_tokens, a.dim), kTileN) < ((int64_t)1 << 28);
+}
+
+cudaError_t launch_token_loss(const LossArgs& a, const LaunchEnv& env, void* space, cudaStream_t st) {
+    const LossSpace s = loss_space(a, env, false);
+    char* ws = (char*)space;
+    cudaError_t e = cudaSuccess;
+    const void *h = a.hidden, *w = a.weight;
+    int64_t hs = a.hidden_stride, wst = a.weight_stride;
+    if (!tma_ready(h, hs)) {
+        e = launch_pack(env, h, hs, a.rows, a.dim, ws + s.hidden, s.pitch, nullptr, st);
+        h = ws + s.hidden;
+        hs = s.pitch;
+    }
+    if (e == cudaSuccess && !tma_ready(w, wst)) {
+        e = launch_pack(env, w, wst, a.n_tokens, a.dim, ws + s.weight, s.pitch, nullptr, st);
+        w = ws + s.weight;
+        wst = s.pitch;
+    }
+    if (e != cudaSuccess) return e;
+    Product p{};
+    if ((e = make_map(&p.a, h, a.rows, a.dim, hs, kTileM)) != cudaSuccess) return e;
+    if ((e = make_map(&p.b, w, a.n_tokens, a.dim, wst, kTileN)) != cudaSuccess) return e;
+    cut_product(p, a.rows, a.n_tokens, a.dim, 1);
+    p.mask = a.mask;
+    p.mask_words = (a.n_tokens + 31) / 32;
+    p.targets = a.targets;
+    p.part = (float2*)(ws + s.part);
+    p.part_pitch = s.part_pitch;
+    p.target_logit = (float*)(ws + s.target_logit);
+    p.err = a.err;
+    if ((e = launch_product<kFoldLogSum>(env, p, st)) != cudaSuccess) return e;
+    return launch_pdl(loss_kernel, dim3((unsigned)ceil_div(a.rows, kMergeThreads / 32)), dim3(kMergeThreads), 0, st,
+                      (const float2*)p.part, s.part_pitch, s.part_pitch, (const float*)p.target_logit, a.targets, a.mask,
+                      a.rows, a.n_tokens, a.loss, a.lse, a.err);
+}
+
+cudaError_t launch_token_loss_grad(const LossArgs& a, const LaunchEnv& env, void* space, cudaStream_t st) {
+    const LossSpace s = loss_space(a, env, true);
+    char* ws = (char*)space;
+    float* coef = (float*)(ws + s.coef);
+    float* scale = (float*)(ws + s.scale);
+    cudaError_t e = launch_pdl(coef_kernel, dim3(1), dim3(kCoefThreads), 0, st, a.targets, a.mask, a.grad_loss, a.rows,
+                               a.n_tokens, coef, scale, a.err);
+    if (e != cudaSuccess) return e;
+    if ((e = launch_pack(env, a.hidden, a.hidden_stride, a.rows, a.dim, ws + s.hidden, s.pitch, coef, st)) != cudaSuccess)
+        return e;
+    const void* h = ws + s.hidden;
+    const char* w = (const char*)a.weight;
+    int64_t wst = a.weight_stride;
+    if (!tma_ready(w, wst)) {
+        e = launch_pack(env, w, wst, a.n_tokens, a.dim, ws + s.weight, s.pitch, nullptr, st);
+        if (e != cudaSuccess) return e;
+        w = ws + s.weight;
+        wst = s.pitch;
+    }
+    const int64_t words = (a.n_tokens + 31) / 32;
+    for (int32_t v0 = 0; v0 < a.n_tokens; v0 += s.piece) {
+        const int32_t n = std::min(s.piece, a.n_tokens - v0), width = ceil_div(n, kTileN) * kTileN;
+        const char* wp = w + (int64_t)v0 * wst * 2;
+        Product g{};   // G of the piece, [rows][width]
+        if ((e = make_map(&g.a, h, a.rows, a.dim, s.pitch, kTileM)) != cudaSuccess) return e;
+        if ((e = make_map(&g.b, wp, n, a.dim, wst, kTileN)) != cudaSuccess) return e;
+        cut_product(g, a.rows, n, a.dim, 1);
+        g.mask = a.mask ? a.mask + v0 / 32 : nullptr;
+        g.mask_words = words;
+        g.targets = a.targets;
+        g.column0 = v0;
+        g.lse = a.lse;
+        g.coef = coef;
+        g.out = (__nv_bfloat16*)(ws + s.grad);
+        g.ld = width;
+        g.err = a.err;
+        if ((e = launch_product<kFoldGrad>(env, g, st)) != cudaSuccess) return e;
+        Product d{};   // its part of the hidden gradient
+        if ((e = make_map(&d.a, ws + s.grad, a.rows, width, width, kTileM)) != cudaSuccess) return e;
+        if ((e = make_map(&d.b, wp, n, a.dim, wst, 64)) != cudaSuccess) return e;
+        cut_product(d, a.rows, a.dim, n, s.splits);
+        d.b_mn = 1;
+        d.planes = (float*)(ws + s.planes);
+        d.add = v0 > 0;
+        d.err = a.err;
+        if ((e = launch_product<kFoldHidden>(env, d, st)) != cudaSuccess) return e;
+        Product g2{};   // the piece's rows of the weight's gradient
+        if ((e = make_map(&g2.a, ws + s.grad, a.rows, width, width, 64)) != cudaSuccess) return e;
+        if ((e = make_map(&g2.b, h, a.rows, a.dim, s.pitch, 64)) != cudaSuccess) return e;
+        cut_product(g2, n, a.dim, a.rows, 1);
+        g2.a_mn = g2.b_mn = 1;
+        g2.out = (__nv_bfloat16*)a.dweight + (int64_t)v0 * a.dweight_stride;
+        g2.ld = a.dweight_stride;
+        g2.scale = scale;
+        g2.vec = tma_ready(a.dweight, a.dweight_stride);
+        g2.err = a.err;
+        if ((e = launch_product<kFoldWeight>(env, g2, st)) != cudaSuccess) return e;
+    }
+    const int64_t cells = (int64_t)a.rows * a.dim;
+    return launch_pdl(dhidden_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(cells, kPackThreads), env.num_sms * 8)),
+                      dim3(kPackThreads), 0, st, (const float*)(ws + s.planes), s.splits, a.rows, a.dim, (const float*)scale,
+                      (__nv_bfloat16*)a.dhidden, a.dhidden_stride);
+}
+
+}  // namespace domino
