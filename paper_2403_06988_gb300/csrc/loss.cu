@@ -25,9 +25,9 @@
 #include <algorithm>
 #include <atomic>
 
+#include "decode.cuh"
 #include "loss.h"
 #include "tcgen05.cuh"
-#include "walk_common.cuh"
 
 namespace domino {
 namespace {
@@ -38,8 +38,10 @@ constexpr int kAccs = 2;                       // accumulators of kTileN columns
 constexpr int kTmemColumns = kAccs * kTileN;
 constexpr int kBytesA = kTileM * kTileK * 2, kBytesB = kTileN * kTileK * 2;
 constexpr int kStageBytes = kBytesA + kBytesB;
-constexpr int kProductSmem = kStages * kStageBytes + 1024;   // tiles lie on 1024-byte boundaries
 constexpr int kFoldWarps = 8;
+// Results leave through shared memory: 32 rows of 64 bytes, two a warp, in the 64-byte swizzle.
+constexpr int kOutBytes = 32 * 64;
+constexpr int kProductSmem = kStages * kStageBytes + kFoldWarps * 2 * kOutBytes + 1024;   // tiles lie on 1024-byte boundaries
 constexpr int kProductThreads = 128 + 32 * kFoldWarps;
 constexpr int kFoldColumns = kTileN / (kFoldWarps / 4);      // a warp's: 32 rows, half of the columns
 constexpr int kGroupM = 16;                    // row tiles that share a pass over the columns' tiles
@@ -54,6 +56,7 @@ enum ProductFold : int {
 
 struct Product {
     CUtensorMap a, b;
+    CUtensorMap to;                // where the results go, in boxes of 32 rows and 64 bytes (kFoldGrad, kFoldHidden, kFoldWeight)
     int32_t m, n;                  // valid rows and columns of the product
     int32_t m_tiles, n_tiles, splits, k_blocks;   // k_blocks: of the whole sum, shared out over the splits
     int32_t a_mn, b_mn;            // operands whose rows of memory run along k (MN-major)
@@ -68,13 +71,11 @@ struct Product {
     float* target_logit;           // [m]
     const float* lse;
     const float* coef;             // c_t / scale
-    // outputs
-    __nv_bfloat16* out;            // kFoldGrad: G [m][ld]; kFoldWeight: [m][ld]
-    float* planes;                 // kFoldHidden: [splits][m][n]
+    const float* scale;            // kFoldWeight
+    __nv_bfloat16* out;            // kFoldWeight: where `to` cannot be, rows off 16-byte boundaries
     int64_t ld;
-    const float* scale;
+    int32_t plane_rows;            // kFoldHidden: `to` is [splits][plane_rows][n]
     int32_t add;                   // kFoldHidden: to what the planes hold
-    int32_t vec;                   // rows of `out` lie on 16-byte boundaries
     uint32_t* err;
 };
 
@@ -122,17 +123,56 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// 32 values from column c on of a row of bf16, those below n.
-__device__ __forceinline__ void store_bf16(__nv_bfloat16* row, int32_t c, int32_t n, bool vec, const float (&v)[32]) {
-    if (vec && c + 32 <= n) {
+__device__ __forceinline__ float2 mul2(float2 a, float b) {
+    unsigned long long x, y, r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a.x), "f"(a.y));
+    asm("mov.b64 %0, {%1, %1};" : "=l"(y) : "f"(b));
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    float2 o;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(o.x), "=f"(o.y) : "l"(r));
+    return o;
+}
+
+// What a warp's lane needs beside the products of its row in a tile.
+struct Side {
+    uint32_t word[kFoldColumns / 32];   // allowed tokens
+    int32_t target;                     // its column
+    float lse, coef;
+};
+
+template <int FOLD>
+__device__ __forceinline__ Side load_side(const Product& p, int32_t item, int row_in_tile, int half) {
+    Side s;
+    const Item t = item_at(p, item);
+    const int32_t row = t.m * kTileM + row_in_tile, c0 = t.n * kTileN + half * kFoldColumns;
+    const bool on = row < p.m;
+    s.target = on ? (int32_t)((uint32_t)__ldg(p.targets + row) - (uint32_t)p.column0) : -1;
+    s.lse = FOLD == kFoldGrad && on ? p.lse[row] : 0.0f;
+    s.coef = FOLD == kFoldGrad && on ? p.coef[row] : 0.0f;
+    const uint32_t* mrow = p.mask && on ? p.mask + (int64_t)row * p.mask_words : nullptr;
 #pragma unroll
-        for (int i = 0; i < 32; i += 8)
-            *reinterpret_cast<uint4*>(row + c + i) = make_uint4(pack_bf16(v[i], v[i + 1]), pack_bf16(v[i + 2], v[i + 3]),
-                                                                pack_bf16(v[i + 4], v[i + 5]), pack_bf16(v[i + 6], v[i + 7]));
-    } else {
+    for (int j = 0; j < kFoldColumns / 32; ++j) s.word[j] = on ? allowed_word(mrow, c0 + 32 * j, p.n) : 0u;
+    return s;
+}
+
+// 16 words (64 bytes) of each lane's row to one of the warp's buffers, and from there to (x, y).
+// A buffer was read by its copy before it is written again: at most one copy is behind.
+__device__ __forceinline__ void put_rows(const CUtensorMap* map, int32_t x, int32_t y, bool add, uint32_t buffer, int lane,
+                                         const uint32_t* w) {
+    if (lane == 0) tma_wait_read<1>();
+    __syncwarp();
+    const uint32_t row = buffer + lane * 64;
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (c + i < n) row[c + i] = __float2bfloat16_rn(v[i]);
+    for (int i = 0; i < 4; ++i)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(row + ((i ^ ((lane >> 1) & 3)) << 4)), "r"(w[4 * i]),
+                     "r"(w[4 * i + 1]), "r"(w[4 * i + 2]), "r"(w[4 * i + 3])
+                     : "memory");
+    tma_fence();
+    __syncwarp();
+    if (lane == 0) {
+        if (add) tma_add(map, x, y, buffer);
+        else tma_store(map, x, y, buffer);
+        tma_commit();
     }
 }
 
@@ -222,74 +262,112 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         }
     } else if (warp >= 4) {   // ---- folds
         const int quarter = warp & 3, half = (warp - 4) >> 2;
-        uint32_t accs = 0;
+        const uint32_t buffers = tiles + kStages * kStageBytes + (warp - 4) * 2 * kOutBytes;
+        constexpr bool kTokens = FOLD == kFoldLogSum || FOLD == kFoldGrad;
+        uint32_t accs = 0, puts = 0;
+        Side next{};
+        if (kTokens && blockIdx.x < p.items) next = load_side<FOLD>(p, blockIdx.x, quarter * 32 + lane, half);
+        float scale = 1.0f;
+        if constexpr (FOLD == kFoldWeight) scale = *p.scale;
         for (int32_t i = blockIdx.x; i < p.items; i += gridDim.x, ++accs) {
             const Item t = item_at(p, i);
             const uint32_t s_acc = accs % kAccs;
-            const int32_t row = t.m * kTileM + quarter * 32 + lane, c0 = t.n * kTileN + half * kFoldColumns;
+            const int32_t row0 = t.m * kTileM + quarter * 32, row = row0 + lane, c0 = t.n * kTileN + half * kFoldColumns;
             const bool on = row < p.m;
-            // what the fold needs beside the products
-            constexpr int kWords = kFoldColumns / 32;
-            uint32_t word[kWords];
-            int32_t target = -1;
-            float lse = 0.0f, coef = 0.0f, scale = 0.0f;
-            if constexpr (FOLD == kFoldLogSum || FOLD == kFoldGrad) {
-                const uint32_t* mrow = p.mask && on ? p.mask + (int64_t)row * p.mask_words : nullptr;
-#pragma unroll
-                for (int j = 0; j < kWords; ++j) word[j] = on ? allowed_word(mrow, c0 + 32 * j, p.n) : 0u;
-                if (on) target = __ldg(p.targets + row) - p.column0;
-                if (FOLD == kFoldGrad && on) {
-                    lse = p.lse[row];
-                    coef = p.coef[row];
-                }
-            }
-            if constexpr (FOLD == kFoldWeight) scale = *p.scale;
+            // the next tile's are on their way while this one is folded
+            const Side side = next;
+            if (kTokens && i + (int32_t)gridDim.x < p.items)
+                next = load_side<FOLD>(p, i + gridDim.x, quarter * 32 + lane, half);
             // the whole warp goes on or leaves: loads from tensor memory are a warp's
             if (!__all_sync(0xffffffffu, bar_wait(smem_addr(&s_acc_full[s_acc]), (accs / kAccs) & 1u, failed))) break;
             tcgen_after();
             const uint32_t acc = tmem + s_acc * kTileN + half * kFoldColumns + ((uint32_t)(quarter * 32) << 16);
             float m = -INFINITY, sum = 0.0f;
-#pragma unroll
-            for (int j = 0; j < kWords; ++j) {
+#pragma unroll 1
+            for (int j = 0; j < kFoldColumns / 32; ++j) {
+                const int32_t c = c0 + 32 * j;
+                if (c >= p.n && FOLD != kFoldGrad) break;   // the tile's columns beyond the last
                 float v[32];
                 tmem_load32(v, acc + 32 * j);
-                const int32_t c = c0 + 32 * j;
+                const uint32_t word = j == 0 ? side.word[0] : j == 1 ? side.word[1] : j == 2 ? side.word[2] : side.word[3];
+                const uint32_t at = (uint32_t)side.target - (uint32_t)c;   // below 32: the target's place
                 if constexpr (FOLD == kFoldLogSum) {
-                    float top = -INFINITY;
+                    if (__any_sync(0xffffffffu, at < 32u)) {
+                        float x = 0.0f;
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        if (!((word[j] >> e) & 1u)) v[e] = -INFINITY;
-                        else if (c + e == target) p.target_logit[row] = v[e];
-                        top = fmaxf(top, v[e]);
+                        for (int e = 0; e < 32; ++e) x = at == (uint32_t)e ? v[e] : x;
+                        if (at < 32u && on) p.target_logit[row] = x;
                     }
-                    const float m2 = fmaxf(m, top), ref = sum_ref(m2);
-                    sum *= exp_diff(m, ref);
+                    if (!__all_sync(0xffffffffu, word == 0xFFFFFFFFu)) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) sum += exp_diff(v[e], ref);
-                    m = m2;
+                        for (int e = 0; e < 32; ++e) v[e] = (word & (1u << e)) ? v[e] : -INFINITY;
+                    }
+                    float top = m;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) top = fmaxf(fmaxf(top, v[e]), v[e + 1]);
+                    const float ref = sum_ref(top);
+                    float2 s0 = make_float2(sum * exp_diff(m, ref), 0.0f), s1 = make_float2(0.0f, 0.0f);
+                    const float2 nref = make_float2(-ref, -ref);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        const float2 d0 = mul2(add2(make_float2(v[e], v[e + 1]), nref), kLog2e);
+                        const float2 d1 = mul2(add2(make_float2(v[e + 2], v[e + 3]), nref), kLog2e);
+                        s0 = add2(s0, make_float2(ex2(d0.x), ex2(d0.y)));
+                        s1 = add2(s1, make_float2(ex2(d1.x), ex2(d1.y)));
+                    }
+                    s0 = add2(s0, s1);
+                    sum = s0.x + s0.y;
+                    m = top;
                 } else if constexpr (FOLD == kFoldGrad) {
+                    const float2 nlse = make_float2(-side.lse, -side.lse);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const float q = exp_diff(v[e], lse) - (c + e == target ? 1.0f : 0.0f);
-                        v[e] = coef != 0.0f && ((word[j] >> e) & 1u) ? q * coef : 0.0f;
+                    for (int e = 0; e < 32; e += 2) {
+                        const float2 d = mul2(add2(make_float2(v[e], v[e + 1]), nlse), kLog2e);
+                        const float2 q = mul2(make_float2(ex2(d.x), ex2(d.y)), side.coef);
+                        v[e] = q.x;
+                        v[e + 1] = q.y;
                     }
-                    // columns beyond the vocabulary, up to the tile's end, are written as zeros: they are read again
-                    if (on) store_bf16(p.out + (int64_t)row * p.ld, c, (int32_t)p.ld, true, v);
+                    if (__any_sync(0xffffffffu, at < 32u)) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = at == (uint32_t)e ? v[e] - side.coef : v[e];
+                    }
+                    // rows without a gradient, and columns beyond the vocabulary (they are read again): zeros
+                    const uint32_t keep = side.coef != 0.0f ? word : 0u;
+                    if (!__all_sync(0xffffffffu, keep == 0xFFFFFFFFu)) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = (keep & (1u << e)) ? v[e] : 0.0f;
+                    }
+                    uint32_t w[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+                    if (row0 < p.m) put_rows(&p.to, c, row0, false, buffers + (puts++ & 1u) * kOutBytes, lane, w);
                 } else if constexpr (FOLD == kFoldHidden) {
                     // a split of a short piece may have no products: its accumulator holds an earlier tile's
-                    float* out = p.planes + ((int64_t)t.split * p.m + row) * p.n + c;
-                    if (on) {
+                    if (t.k0 < t.k1 || !p.add) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (c + e < p.n) {
-                                const float x = t.k0 < t.k1 ? v[e] : 0.0f;
-                                out[e] = p.add ? out[e] + x : x;
-                            }
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t w[16];
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) w[e] = t.k0 < t.k1 ? __float_as_uint(v[16 * h + e]) : 0u;
+                            if (c + 16 * h < p.n)
+                                put_rows(&p.to, c + 16 * h, t.split * p.plane_rows + row0, p.add != 0,
+                                         buffers + (puts++ & 1u) * kOutBytes, lane, w);
+                        }
                     }
                 } else {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] *= scale;
-                    if (on) store_bf16(p.out + (int64_t)row * p.ld, c, p.n, p.vec, v);
+                    if (!p.out) {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+                        if (row0 < p.m) put_rows(&p.to, c, row0, false, buffers + (puts++ & 1u) * kOutBytes, lane, w);
+                    } else if (on) {
+                        __nv_bfloat16* out = p.out + (int64_t)row * p.ld + c;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (c + e < p.n) out[e] = __float2bfloat16_rn(v[e]);
+                    }
                 }
             }
             if constexpr (FOLD == kFoldLogSum) {
@@ -299,6 +377,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             __syncwarp();
             if (lane == 0) bar_arrive(smem_addr(&s_acc_empty[s_acc]));
         }
+        if (lane == 0) tma_wait_all();
     }
     __syncwarp();
     tcgen_before();
@@ -415,17 +494,30 @@ __global__ void __launch_bounds__(kPackThreads)
 
 // dhidden = scale * the sum of the planes, in their order.
 __global__ void __launch_bounds__(kPackThreads)
-    dhidden_kernel(const float* planes, int32_t splits, int32_t rows, int32_t cols, const float* scale, __nv_bfloat16* out,
-                   int64_t ld) {
+    dhidden_kernel(const float* planes, int32_t splits, int64_t plane, int32_t rows, int32_t cols, int32_t pitch,
+                   const float* scale, __nv_bfloat16* out, int64_t ld) {
     pdl_wait();
     pdl_trigger();
-    const int64_t n = (int64_t)rows * cols;
+    const int32_t vectors = pitch / 4;   // of a row of a plane
+    const int64_t n = (int64_t)rows * vectors;
     const float s = *scale;
     for (int64_t i = (int64_t)blockIdx.x * kPackThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kPackThreads) {
-        float v = 0.0f;
-        for (int k = 0; k < splits; ++k) v += planes[k * n + i];
-        const int64_t r = i / cols;
-        out[r * ld + (i - r * cols)] = __float2bfloat16_rn(s * v);
+        const int32_t r = (int32_t)(i / vectors), c = (int32_t)(i - (int64_t)r * vectors) * 4;
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int k = 0; k < splits; ++k) {
+            const float4 x = *reinterpret_cast<const float4*>(planes + k * plane + (int64_t)r * pitch + c);
+            v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+        }
+        __nv_bfloat16* to = out + (int64_t)r * ld + c;
+        const uint32_t lo = pack_bf16(s * v.x, s * v.y), hi = pack_bf16(s * v.z, s * v.w);
+        if (c + 4 <= cols && (reinterpret_cast<uintptr_t>(to) & 7) == 0) {
+            *reinterpret_cast<uint2*>(to) = make_uint2(lo, hi);
+        } else {
+            const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e < cols) to[e] = __float2bfloat16_rn(s * x[e]);
+        }
     }
 }
 
@@ -448,17 +540,28 @@ EncodeTiled encode_tiled() {
     return f;
 }
 
-// A [rows][cols] bf16 matrix, rows `pitch` elements apart, read in boxes of 64
-// columns (128 bytes, swizzled) and `box_rows` rows; zeros outside.
-cudaError_t make_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t pitch, int box_rows) {
+// A [rows][cols] matrix, rows `pitch` elements apart: bf16, read in boxes of 64
+// columns (128 bytes, swizzled) and `box_rows` rows, zeros outside; or written
+// in boxes of 32 rows of 64 bytes.
+cudaError_t encode_map(CUtensorMap* map, CUtensorMapDataType type, int size, const void* base, int64_t rows, int64_t cols,
+                       int64_t pitch, int box_cols, int box_rows, CUtensorMapSwizzle swizzle) {
     const EncodeTiled encode = encode_tiled();
     if (!encode) return cudaErrorNotSupported;
-    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch * 2};
-    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, steps[2] = {1, 1};
-    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, steps,
-                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch * size};
+    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+    const CUresult r = encode(map, type, 2, const_cast<void*>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+cudaError_t make_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t pitch, int box_rows) {
+    return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, rows, cols, pitch, 64, box_rows,
+                      CU_TENSOR_MAP_SWIZZLE_128B);
+}
+cudaError_t make_out_map(CUtensorMap* map, void* base, int64_t rows, int64_t cols, int64_t pitch) {
+    return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, rows, cols, pitch, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+}
+cudaError_t make_plane_map(CUtensorMap* map, void* base, int64_t rows, int64_t cols, int64_t pitch) {
+    return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, base, rows, cols, pitch, 16, 32, CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
@@ -509,6 +612,7 @@ struct LossSpace {
     int32_t part_pitch;
     int32_t piece;        // tokens of the vocabulary at a time (gradient)
     int32_t splits;       // of the hidden gradient's sum
+    int32_t plane_rows;   // of each split's plane
 };
 
 // G takes at most this many bytes at a time.
@@ -539,7 +643,8 @@ LossSpace loss_space(const LossArgs& a, const LaunchEnv& env, bool grad) {
         // few tiles: their sums are split, each part into a plane of its own
         const int64_t tiles = (int64_t)ceil_div(a.rows, kTileM) * ceil_div(a.dim, kTileN);
         s.splits = (int)std::max<int64_t>(1, std::min<int64_t>(env.num_sms / tiles, s.piece / kTileK / 4));
-        s.planes = take((size_t)s.splits * a.rows * a.dim * 4);
+        s.plane_rows = ceil_div(a.rows, kTileM) * kTileM;
+        s.planes = take((size_t)s.splits * s.plane_rows * s.pitch * 4);
     }
     s.end = at;
     return s;
@@ -621,8 +726,7 @@ cudaError_t launch_token_loss_grad(const LossArgs& a, const LaunchEnv& env, void
         g.column0 = v0;
         g.lse = a.lse;
         g.coef = coef;
-        g.out = (__nv_bfloat16*)(ws + s.grad);
-        g.ld = width;
+        if ((e = make_out_map(&g.to, ws + s.grad, a.rows, width, width)) != cudaSuccess) return e;
         g.err = a.err;
         if ((e = launch_product<kFoldGrad>(env, g, st)) != cudaSuccess) return e;
         Product d{};   // its part of the hidden gradient
@@ -630,7 +734,9 @@ cudaError_t launch_token_loss_grad(const LossArgs& a, const LaunchEnv& env, void
         if ((e = make_map(&d.b, wp, n, a.dim, wst, 64)) != cudaSuccess) return e;
         cut_product(d, a.rows, a.dim, n, s.splits);
         d.b_mn = 1;
-        d.planes = (float*)(ws + s.planes);
+        d.plane_rows = s.plane_rows;
+        e = make_plane_map(&d.to, ws + s.planes, (int64_t)s.splits * s.plane_rows, a.dim, s.pitch);
+        if (e != cudaSuccess) return e;
         d.add = v0 > 0;
         d.err = a.err;
         if ((e = launch_product<kFoldHidden>(env, d, st)) != cudaSuccess) return e;
@@ -639,17 +745,21 @@ cudaError_t launch_token_loss_grad(const LossArgs& a, const LaunchEnv& env, void
         if ((e = make_map(&g2.b, h, a.rows, a.dim, s.pitch, 64)) != cudaSuccess) return e;
         cut_product(g2, n, a.dim, a.rows, 1);
         g2.a_mn = g2.b_mn = 1;
-        g2.out = (__nv_bfloat16*)a.dweight + (int64_t)v0 * a.dweight_stride;
-        g2.ld = a.dweight_stride;
+        __nv_bfloat16* rows = (__nv_bfloat16*)a.dweight + (int64_t)v0 * a.dweight_stride;
+        if (tma_ready(a.dweight, a.dweight_stride)) {
+            if ((e = make_out_map(&g2.to, rows, n, a.dim, a.dweight_stride)) != cudaSuccess) return e;
+        } else {
+            g2.out = rows;
+            g2.ld = a.dweight_stride;
+        }
         g2.scale = scale;
-        g2.vec = tma_ready(a.dweight, a.dweight_stride);
         g2.err = a.err;
         if ((e = launch_product<kFoldWeight>(env, g2, st)) != cudaSuccess) return e;
     }
-    const int64_t cells = (int64_t)a.rows * a.dim;
+    const int64_t cells = (int64_t)a.rows * (s.pitch / 4);
     return launch_pdl(dhidden_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(cells, kPackThreads), env.num_sms * 8)),
-                      dim3(kPackThreads), 0, st, (const float*)(ws + s.planes), s.splits, a.rows, a.dim, (const float*)scale,
-                      (__nv_bfloat16*)a.dhidden, a.dhidden_stride);
+                      dim3(kPackThreads), 0, st, (const float*)(ws + s.planes), s.splits, (int64_t)s.plane_rows * s.pitch, a.rows,
+                      a.dim, (int32_t)s.pitch, (const float*)scale, (__nv_bfloat16*)a.dhidden, a.dhidden_stride);
 }
 
 }  // namespace domino

@@ -41,14 +41,18 @@ __device__ __forceinline__ uint64_t timer_ns() {
 
 // Waits for the phase `parity` of `bar` to end.  A wait ends after kWaitNs at
 // the latest, or once another role of the CTA has given up (*failed): it then
-// returns false with *failed set, and its caller leaves.
+// returns false with *failed set, and its caller leaves.  The clock is read once
+// in kWaitTries tries: reading it takes longer than most waits.
 constexpr uint64_t kWaitNs = 4000000000ull;
+constexpr uint32_t kWaitTries = 256;
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* failed) {
-    if (bar_try(bar, parity)) return true;
-    const uint64_t end = timer_ns() + kWaitNs;
-    while (!bar_try(bar, parity)) {
+    uint64_t end = 0;
+    for (uint32_t i = 1; !bar_try(bar, parity); ++i) {
+        if (i % kWaitTries) continue;
         if (*failed) return false;
-        if (timer_ns() > end) {
+        const uint64_t now = timer_ns();
+        if (end == 0) end = now + kWaitNs;
+        if (now > end) {
             *failed = 1u;
             return false;
         }
@@ -67,6 +71,28 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, i
 __device__ __forceinline__ void tma_prefetch_map(const CUtensorMap* map) {
     asm volatile("prefetch.tensormap [%0];\n" ::"l"(map) : "memory");
 }
+
+// A tile in shared memory at `src` to the box of the tensor with its corner at (x, y), or added to what stands there;
+// what lies outside of the tensor is left out.  x is a multiple of 16 bytes, both are inside of the tensor.
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, int32_t x, int32_t y, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];\n" ::"l"(map), "r"(x), "r"(y),
+                 "r"(src)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_add(const CUtensorMap* map, int32_t x, int32_t y, uint32_t src) {
+    asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];\n" ::"l"(map),
+                 "r"(x), "r"(y), "r"(src)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_commit() { asm volatile("cp.async.bulk.commit_group;\n" ::: "memory"); }
+// All but the last PENDING groups of this thread have read their shared memory.
+template <int PENDING>
+__device__ __forceinline__ void tma_wait_read() {
+    asm volatile("cp.async.bulk.wait_group.read %0;\n" ::"n"(PENDING) : "memory");
+}
+__device__ __forceinline__ void tma_wait_all() { asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory"); }
+// What this thread wrote to shared memory is seen by the copies issued after a barrier with it.
+__device__ __forceinline__ void tma_fence() { asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory"); }
 
 // Shared-memory descriptor of an operand tile in the 128-byte swizzle: start
 // address, leading and stride byte offsets (16-byte units), descriptor version
