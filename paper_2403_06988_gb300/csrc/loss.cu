@@ -32,16 +32,28 @@
 namespace domino {
 namespace {
 
-constexpr int kTileM = 128, kTileN = 256, kTileK = 64;
-constexpr int kStages = 4;
+// Tiles of a product: kRowsM rows of A a CTA and kTileN of B.  PAIR: two CTAs
+// make 2 * kRowsM rows and hold half of B each, so that a product's operands
+// take two thirds of the bytes.
+constexpr int kRowsM = 128, kTileN = 256, kTileK = 64;
 constexpr int kAccs = 2;                       // accumulators of kTileN columns: all of tensor memory
 constexpr int kTmemColumns = kAccs * kTileN;
-constexpr int kBytesA = kTileM * kTileK * 2, kBytesB = kTileN * kTileK * 2;
-constexpr int kStageBytes = kBytesA + kBytesB;
+template <bool PAIR>
+struct Tile {
+    static constexpr int kCtas = PAIR ? 2 : 1;
+    static constexpr int kM = kRowsM * kCtas;
+    static constexpr int kRowsB = kTileN / kCtas;      // a CTA's
+    static constexpr int kStages = PAIR ? 6 : 4;
+    static constexpr int kBytesA = kRowsM * kTileK * 2, kBytesB = kRowsB * kTileK * 2;
+    static constexpr int kStageBytes = kBytesA + kBytesB;
+};
+constexpr int kRingBytes = 196608;
+static_assert(Tile<false>::kStages * Tile<false>::kStageBytes == kRingBytes);
+static_assert(Tile<true>::kStages * Tile<true>::kStageBytes == kRingBytes);
 constexpr int kFoldWarps = 8;
-// Results leave through shared memory: 32 rows of 64 bytes, two a warp, in the 64-byte swizzle.
-constexpr int kOutBytes = 32 * 64;
-constexpr int kProductSmem = kStages * kStageBytes + kFoldWarps * 2 * kOutBytes + 1024;   // tiles lie on 1024-byte boundaries
+// Results leave through shared memory: 32 rows of 64 bytes a warp's buffer, in the 64-byte swizzle.
+constexpr int kOutBytes = 32 * 64, kOutBuffers = 16 / kFoldWarps;
+constexpr int kProductSmem = kRingBytes + kFoldWarps * kOutBuffers * kOutBytes + 1024;   // tiles lie on 1024-byte boundaries
 constexpr int kProductThreads = 128 + 32 * kFoldWarps;
 constexpr int kFoldColumns = kTileN / (kFoldWarps / 4);      // a warp's: 32 rows, half of the columns
 constexpr int kGroupM = 16;                    // row tiles that share a pass over the columns' tiles
@@ -102,12 +114,13 @@ __device__ __forceinline__ Item item_at(const Product& p, int32_t i) {
 }
 
 // An operand's tile of `rows` m or n and kTileK k, from (r0, k0) on.
+template <bool PAIR>
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, bool mn, int rows, int32_t r0,
                                           int32_t k0, uint32_t bar) {
     if (!mn) {
-        tma_load(dst, map, k0, r0, bar);
+        tma_load<PAIR>(dst, map, k0, r0, bar);
     } else {
-        for (int c = 0; c < rows; c += 64) tma_load(dst + c * kTileK * 2, map, r0 + c, k0, bar);
+        for (int c = 0; c < rows; c += 64) tma_load<PAIR>(dst + c * kTileK * 2, map, r0 + c, k0, bar);
     }
 }
 
@@ -141,10 +154,10 @@ struct Side {
 };
 
 template <int FOLD>
-__device__ __forceinline__ Side load_side(const Product& p, int32_t item, int row_in_tile, int half) {
+__device__ __forceinline__ Side load_side(const Product& p, int32_t item, int tile_m, int row_in_tile, int half) {
     Side s;
     const Item t = item_at(p, item);
-    const int32_t row = t.m * kTileM + row_in_tile, c0 = t.n * kTileN + half * kFoldColumns;
+    const int32_t row = t.m * tile_m + row_in_tile, c0 = t.n * kTileN + half * kFoldColumns;
     const bool on = row < p.m;
     s.target = on ? (int32_t)((uint32_t)__ldg(p.targets + row) - (uint32_t)p.column0) : -1;
     s.lse = FOLD == kFoldGrad && on ? p.lse[row] : 0.0f;
@@ -156,10 +169,10 @@ __device__ __forceinline__ Side load_side(const Product& p, int32_t item, int ro
 }
 
 // 16 words (64 bytes) of each lane's row to one of the warp's buffers, and from there to (x, y).
-// A buffer was read by its copy before it is written again: at most one copy is behind.
+// A buffer was read by its copy before it is written again.
 __device__ __forceinline__ void put_rows(const CUtensorMap* map, int32_t x, int32_t y, bool add, uint32_t buffer, int lane,
                                          const uint32_t* w) {
-    if (lane == 0) tma_wait_read<1>();
+    if (lane == 0) tma_wait_read<kOutBuffers - 1>();
     __syncwarp();
     const uint32_t row = buffer + lane * 64;
 #pragma unroll
@@ -176,13 +189,17 @@ __device__ __forceinline__ void put_rows(const CUtensorMap* map, int32_t x, int3
     }
 }
 
-template <int FOLD>
+template <int FOLD, bool PAIR>
 __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ Product p) {
+    using T = Tile<PAIR>;
+    constexpr int kStages = T::kStages;
     extern __shared__ unsigned char smem[];
     __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_acc_full[kAccs], s_acc_empty[kAccs], s_done;
     __shared__ uint32_t s_tmem, s_failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t tiles = (smem_addr(smem) + 1023u) & ~1023u;
+    const uint32_t rank = PAIR ? cluster_rank() : 0u;
+    const int32_t first = blockIdx.x / T::kCtas, step = gridDim.x / T::kCtas;   // items of this CTA or pair
     volatile uint32_t* failed = &s_failed;
     if (threadIdx.x == 0) {
         s_failed = 0u;
@@ -192,52 +209,55 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         }
         for (int s = 0; s < kAccs; ++s) {
             bar_init(smem_addr(&s_acc_full[s]), 1);
-            bar_init(smem_addr(&s_acc_empty[s]), kFoldWarps);
+            bar_init(smem_addr(&s_acc_empty[s]), kFoldWarps * T::kCtas);
         }
         bar_init(smem_addr(&s_done), 1);
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         tma_prefetch_map(&p.a);
         tma_prefetch_map(&p.b);
     }
-    if (warp == 2) tmem_alloc(smem_addr(&s_tmem), kTmemColumns);
+    if (warp == 2) tmem_alloc<PAIR>(smem_addr(&s_tmem), kTmemColumns);
     tcgen_before();
     __syncthreads();
+    if constexpr (PAIR) cluster_barrier();
     tcgen_after();
     const uint32_t tmem = s_tmem;
     pdl_wait();
     pdl_trigger();
 
-    if (warp == 0) {   // ---- loads
+    if (warp == 0) {   // ---- loads: each CTA its part of the tiles; the first CTA's barriers count the bytes of both
         if (lane == 0) {
             uint32_t loads = 0;
             bool ok = true;
-            for (int32_t i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
+            for (int32_t i = first; i < p.items && ok; i += step) {
                 const Item t = item_at(p, i);
+                const int32_t row_a = t.m * T::kM + rank * kRowsM, row_b = t.n * kTileN + rank * T::kRowsB;
                 for (int32_t k = t.k0; k < t.k1; ++k, ++loads) {
                     const uint32_t s = loads % kStages, turn = loads / kStages;
                     if (!(ok = bar_wait(smem_addr(&s_empty[s]), (turn & 1u) ^ 1u, failed))) break;
-                    const uint32_t full = smem_addr(&s_full[s]), a = tiles + s * kStageBytes;
-                    bar_expect(full, kStageBytes);
-                    load_tile(a, &p.a, p.a_mn, kTileM, t.m * kTileM, k * kTileK, full);
-                    load_tile(a + kBytesA, &p.b, p.b_mn, kTileN, t.n * kTileN, k * kTileK, full);
+                    const uint32_t mine = smem_addr(&s_full[s]), a = tiles + s * T::kStageBytes;
+                    const uint32_t full = PAIR ? in_cta(mine, 0) : mine;
+                    if (rank == 0) bar_expect(mine, T::kStageBytes * T::kCtas);
+                    load_tile<PAIR>(a, &p.a, p.a_mn, kRowsM, row_a, k * kTileK, full);
+                    load_tile<PAIR>(a + T::kBytesA, &p.b, p.b_mn, T::kRowsB, row_b, k * kTileK, full);
                 }
             }
             // given up: the loads on their way write into this CTA's memory
-            if (!ok)
-                for (uint32_t s = 0; s < kStages && s < loads; ++s) {
+            if (!ok && rank == 0)
+                for (uint32_t s = 0; s < (uint32_t)kStages && s < loads; ++s) {
                     const uint32_t last = loads - 1 - s;   // the stages' last loads
                     const uint64_t end = timer_ns() + kWaitNs;
                     while (!bar_try(smem_addr(&s_full[last % kStages]), (last / kStages) & 1u) && timer_ns() < end) {}
                 }
         }
     } else if (warp == 1) {   // ---- products
-        if (lane == 0) {
-            const uint32_t desc = mma_desc(kTileM, kTileN, p.a_mn, p.b_mn);
+        if (lane == 0 && rank == 0) {
+            const uint32_t desc = mma_desc(T::kM, kTileN, p.a_mn, p.b_mn);
             // 16 k further: 32 bytes along a row of a K-major tile, 16 rows of an MN-major one (16-byte units)
             const uint32_t step_a = p.a_mn ? 2048 / 16 : 32 / 16, step_b = p.b_mn ? 2048 / 16 : 32 / 16;
             uint32_t loads = 0, accs = 0;
             bool ok = true;
-            for (int32_t i = blockIdx.x; i < p.items && ok; i += gridDim.x, ++accs) {
+            for (int32_t i = first; i < p.items && ok; i += step, ++accs) {
                 const Item t = item_at(p, i);
                 const uint32_t s_acc = accs % kAccs, acc = tmem + s_acc * kTileN;
                 if (!(ok = bar_wait(smem_addr(&s_acc_empty[s_acc]), ((accs / kAccs) & 1u) ^ 1u, failed))) break;
@@ -246,38 +266,40 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                     const uint32_t s = loads % kStages;
                     if (!(ok = bar_wait(smem_addr(&s_full[s]), (loads / kStages) & 1u, failed))) break;
                     tcgen_after();
-                    const uint64_t a = operand_desc(tiles + s * kStageBytes, kTileK * 128);
-                    const uint64_t b = operand_desc(tiles + s * kStageBytes + kBytesA, kTileK * 128);
+                    const uint64_t a = operand_desc(tiles + s * T::kStageBytes, kTileK * 128);
+                    const uint64_t b = operand_desc(tiles + s * T::kStageBytes + T::kBytesA, kTileK * 128);
 #pragma unroll
                     for (int j = 0; j < kTileK / 16; ++j)
-                        mma_bf16(acc, a + (uint64_t)(j * step_a), b + (uint64_t)(j * step_b), desc, k > t.k0 || j > 0);
-                    mma_commit(smem_addr(&s_empty[s]));
+                        mma_bf16<PAIR>(acc, a + (uint64_t)(j * step_a), b + (uint64_t)(j * step_b), desc, k > t.k0 || j > 0);
+                    mma_commit<PAIR>(smem_addr(&s_empty[s]));
                 }
-                if (ok) mma_commit(smem_addr(&s_acc_full[s_acc]));
+                if (ok) mma_commit<PAIR>(smem_addr(&s_acc_full[s_acc]));
             }
-            // no product may be on its way when tensor memory is given back
-            mma_commit(smem_addr(&s_done));
-            const uint64_t end = timer_ns() + kWaitNs;
+            mma_commit<PAIR>(smem_addr(&s_done));
+        }
+        // no product, and no arrival at a barrier of this CTA, may be on its way when the CTA ends
+        if (lane == 0) {
+            const uint64_t end = timer_ns() + 3 * kWaitNs;
             while (!bar_try(smem_addr(&s_done), 0u) && timer_ns() < end) {}
         }
     } else if (warp >= 4) {   // ---- folds
         const int quarter = warp & 3, half = (warp - 4) >> 2;
-        const uint32_t buffers = tiles + kStages * kStageBytes + (warp - 4) * 2 * kOutBytes;
+        const uint32_t buffers = tiles + kRingBytes + (warp - 4) * kOutBuffers * kOutBytes;
+        const int row_in_tile = rank * kRowsM + quarter * 32 + lane;
         constexpr bool kTokens = FOLD == kFoldLogSum || FOLD == kFoldGrad;
         uint32_t accs = 0, puts = 0;
         Side next{};
-        if (kTokens && blockIdx.x < p.items) next = load_side<FOLD>(p, blockIdx.x, quarter * 32 + lane, half);
+        if (kTokens && first < p.items) next = load_side<FOLD>(p, first, T::kM, row_in_tile, half);
         float scale = 1.0f;
         if constexpr (FOLD == kFoldWeight) scale = *p.scale;
-        for (int32_t i = blockIdx.x; i < p.items; i += gridDim.x, ++accs) {
+        for (int32_t i = first; i < p.items; i += step, ++accs) {
             const Item t = item_at(p, i);
             const uint32_t s_acc = accs % kAccs;
-            const int32_t row0 = t.m * kTileM + quarter * 32, row = row0 + lane, c0 = t.n * kTileN + half * kFoldColumns;
+            const int32_t row = t.m * T::kM + row_in_tile, row0 = row - lane, c0 = t.n * kTileN + half * kFoldColumns;
             const bool on = row < p.m;
             // the next tile's are on their way while this one is folded
             const Side side = next;
-            if (kTokens && i + (int32_t)gridDim.x < p.items)
-                next = load_side<FOLD>(p, i + gridDim.x, quarter * 32 + lane, half);
+            if (kTokens && i + step < p.items) next = load_side<FOLD>(p, i + step, T::kM, row_in_tile, half);
             // the whole warp goes on or leaves: loads from tensor memory are a warp's
             if (!__all_sync(0xffffffffu, bar_wait(smem_addr(&s_acc_full[s_acc]), (accs / kAccs) & 1u, failed))) break;
             tcgen_after();
@@ -289,7 +311,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 if (c >= p.n && FOLD != kFoldGrad) break;   // the tile's columns beyond the last
                 float v[32];
                 tmem_load32(v, acc + 32 * j);
-                const uint32_t word = j == 0 ? side.word[0] : j == 1 ? side.word[1] : j == 2 ? side.word[2] : side.word[3];
+                uint32_t word = side.word[0];   // not by an index: the words stay in registers
+#pragma unroll
+                for (int k = 1; k < kFoldColumns / 32; ++k) word = j == k ? side.word[k] : word;
                 const uint32_t at = (uint32_t)side.target - (uint32_t)c;   // below 32: the target's place
                 if constexpr (FOLD == kFoldLogSum) {
                     if (__any_sync(0xffffffffu, at < 32u)) {
@@ -340,7 +364,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                     uint32_t w[16];
 #pragma unroll
                     for (int e = 0; e < 16; ++e) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-                    if (row0 < p.m) put_rows(&p.to, c, row0, false, buffers + (puts++ & 1u) * kOutBytes, lane, w);
+                    if (row0 < p.m) put_rows(&p.to, c, row0, false, buffers + (puts++ % kOutBuffers) * kOutBytes, lane, w);
                 } else if constexpr (FOLD == kFoldHidden) {
                     // a split of a short piece may have no products: its accumulator holds an earlier tile's
                     if (t.k0 < t.k1 || !p.add) {
@@ -351,7 +375,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                             for (int e = 0; e < 16; ++e) w[e] = t.k0 < t.k1 ? __float_as_uint(v[16 * h + e]) : 0u;
                             if (c + 16 * h < p.n)
                                 put_rows(&p.to, c + 16 * h, t.split * p.plane_rows + row0, p.add != 0,
-                                         buffers + (puts++ & 1u) * kOutBytes, lane, w);
+                                         buffers + (puts++ % kOutBuffers) * kOutBytes, lane, w);
                         }
                     }
                 } else {
@@ -361,7 +385,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                         uint32_t w[16];
 #pragma unroll
                         for (int e = 0; e < 16; ++e) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-                        if (row0 < p.m) put_rows(&p.to, c, row0, false, buffers + (puts++ & 1u) * kOutBytes, lane, w);
+                        if (row0 < p.m) put_rows(&p.to, c, row0, false, buffers + (puts++ % kOutBuffers) * kOutBytes, lane, w);
                     } else if (on) {
                         __nv_bfloat16* out = p.out + (int64_t)row * p.ld + c;
 #pragma unroll
@@ -375,15 +399,19 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             }
             tcgen_before();
             __syncwarp();
-            if (lane == 0) bar_arrive(smem_addr(&s_acc_empty[s_acc]));
+            if (lane == 0) {
+                if constexpr (PAIR) bar_arrive_cluster(in_cta(smem_addr(&s_acc_empty[s_acc]), 0));
+                else bar_arrive(smem_addr(&s_acc_empty[s_acc]));
+            }
         }
         if (lane == 0) tma_wait_all();
     }
     __syncwarp();
     tcgen_before();
     __syncthreads();
+    if constexpr (PAIR) cluster_barrier();   // neither CTA's memory or barriers are used by the other any more
     tcgen_after();
-    if (warp == 2) tmem_free(tmem, kTmemColumns);
+    if (warp == 2) tmem_free<PAIR>(tmem, kTmemColumns);
     if (threadIdx.x == 0 && *failed) atomicOr(p.err, DOMINO_DEVERR_INTERNAL);
 }
 
@@ -567,33 +595,39 @@ cudaError_t make_plane_map(CUtensorMap* map, void* base, int64_t rows, int64_t c
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-void cut_product(Product& p, int32_t m, int32_t n, int64_t k, int splits) {
+void cut_product(Product& p, bool pair, int32_t m, int32_t n, int64_t k, int splits) {
     p.m = m;
     p.n = n;
-    p.m_tiles = ceil_div(m, kTileM);
+    p.m_tiles = ceil_div(m, pair ? Tile<true>::kM : Tile<false>::kM);
     p.n_tiles = ceil_div(n, kTileN);
     p.k_blocks = ceil_div(k, kTileK);
     p.splits = splits;
     p.items = p.m_tiles * p.n_tiles * splits;
 }
 
-template <int FOLD>
+template <int FOLD, bool PAIR>
 cudaError_t product_smem_ready() {
     constexpr int kDevices = 64;
-    static std::atomic<bool> ready[kDevices];   // one array per fold
+    static std::atomic<bool> ready[kDevices];   // one array per kernel
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess || (dev < kDevices && ready[dev].load())) return e;
-    e = cudaFuncSetAttribute(product_kernel<FOLD>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
+    e = cudaFuncSetAttribute(product_kernel<FOLD, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
     if (e == cudaSuccess && dev < kDevices) ready[dev].store(true);
     return e;
 }
 
+template <int FOLD, bool PAIR>
+cudaError_t launch_product_t(const LaunchEnv& env, const Product& p, cudaStream_t st) {
+    if (cudaError_t e = product_smem_ready<FOLD, PAIR>(); e != cudaSuccess) return e;
+    constexpr int kCtas = Tile<PAIR>::kCtas;
+    const int at_once = std::max(1, env.num_sms / kCtas);
+    return launch_cluster(product_kernel<FOLD, PAIR>, dim3((unsigned)(std::min(p.items, at_once) * kCtas)), dim3(kProductThreads),
+                          kCtas, kProductSmem, st, p);
+}
 template <int FOLD>
-cudaError_t launch_product(const LaunchEnv& env, const Product& p, cudaStream_t st) {
-    if (cudaError_t e = product_smem_ready<FOLD>(); e != cudaSuccess) return e;
-    return launch_pdl(product_kernel<FOLD>, dim3((unsigned)std::min(p.items, env.num_sms)), dim3(kProductThreads),
-                      kProductSmem, st, p);
+cudaError_t launch_product(const LaunchEnv& env, bool pair, const Product& p, cudaStream_t st) {
+    return pair ? launch_product_t<FOLD, true>(env, p, st) : launch_product_t<FOLD, false>(env, p, st);
 }
 
 cudaError_t launch_pack(const LaunchEnv& env, const void* src, int64_t stride, int32_t rows, int32_t cols, void* dst,
@@ -608,6 +642,7 @@ bool tma_ready(const void* p, int64_t stride) { return reinterpret_cast<uintptr_
 // Where a call's parts lie in its workspace.
 struct LossSpace {
     size_t hidden, weight, part, target_logit, coef, scale, grad, planes, end;
+    bool pair;            // products by pairs of CTAs, in the rows of tokens
     int64_t pitch;        // of packed rows
     int32_t part_pitch;
     int32_t piece;        // tokens of the vocabulary at a time (gradient)
@@ -618,8 +653,20 @@ struct LossSpace {
 // G takes at most this many bytes at a time.
 constexpr int64_t kGradBytes = (int64_t)256 << 20;
 
+// Whether pairs of CTAs make the products with `rows` rows of tokens: their
+// tiles are 256 rows high, so not where that leaves a quarter or more of the
+// last of few tiles empty (GB300, us single / pairs, loss and gradient: 256 rows,
+// V = 128256, 4096 wide 208, 732 / 192, 656; 777 rows, V = 32003, 1024 wide 44,
+// 148 / 53, 151; 1024 rows, V = 65536, 1024 wide 94, 320 / 94, 287; 4096 rows, V =
+// 128256, 4096 wide 2440, 8420 / 2440, 7900).
+bool rows_in_pairs(int32_t rows) {
+    const int tiles = ceil_div(rows, kRowsM);
+    return tiles % 2 == 0 || tiles > 15;
+}
+
 LossSpace loss_space(const LossArgs& a, const LaunchEnv& env, bool grad) {
     LossSpace s{};
+    s.pair = rows_in_pairs(a.rows);
     s.pitch = (a.dim + 7) / 8 * 8;
     size_t at = 0;
     const auto take = [&](size_t n) {
@@ -641,9 +688,10 @@ LossSpace loss_space(const LossArgs& a, const LaunchEnv& env, bool grad) {
         s.piece = ceil_div(ceil_div(a.n_tokens, pieces), kTileN) * kTileN;
         s.grad = take((size_t)a.rows * s.piece * 2);
         // few tiles: their sums are split, each part into a plane of its own
-        const int64_t tiles = (int64_t)ceil_div(a.rows, kTileM) * ceil_div(a.dim, kTileN);
-        s.splits = (int)std::max<int64_t>(1, std::min<int64_t>(env.num_sms / tiles, s.piece / kTileK / 4));
-        s.plane_rows = ceil_div(a.rows, kTileM) * kTileM;
+        const int tile_m = s.pair ? Tile<true>::kM : Tile<false>::kM;
+        const int64_t tiles = (int64_t)ceil_div(a.rows, tile_m) * ceil_div(a.dim, kTileN);
+        s.splits = (int)std::max<int64_t>(1, std::min<int64_t>(env.num_sms / (s.pair ? 2 : 1) / tiles, s.piece / kTileK / 4));
+        s.plane_rows = ceil_div(a.rows, tile_m) * tile_m;
         s.planes = take((size_t)s.splits * s.plane_rows * s.pitch * 4);
     }
     s.end = at;
@@ -656,7 +704,7 @@ size_t loss_workspace(const LossArgs& a, const LaunchEnv& env, bool grad) { retu
 
 bool loss_fits(const LossArgs& a) {
     // tiles are counted in 32 bits
-    return (int64_t)ceil_div(a.rows, kTileM) * ceil_div(std::max(a.n_tokens, a.dim), kTileN) < ((int64_t)1 << 28);
+    return (int64_t)ceil_div(a.rows, kRowsM) * ceil_div(std::max(a.n_tokens, a.dim), kTileN) < ((int64_t)1 << 28);
 }
 
 cudaError_t launch_token_loss(const LossArgs& a, const LaunchEnv& env, void* space, cudaStream_t st) {
@@ -677,9 +725,9 @@ cudaError_t launch_token_loss(const LossArgs& a, const LaunchEnv& env, void* spa
     }
     if (e != cudaSuccess) return e;
     Product p{};
-    if ((e = make_map(&p.a, h, a.rows, a.dim, hs, kTileM)) != cudaSuccess) return e;
-    if ((e = make_map(&p.b, w, a.n_tokens, a.dim, wst, kTileN)) != cudaSuccess) return e;
-    cut_product(p, a.rows, a.n_tokens, a.dim, 1);
+    if ((e = make_map(&p.a, h, a.rows, a.dim, hs, kRowsM)) != cudaSuccess) return e;
+    if ((e = make_map(&p.b, w, a.n_tokens, a.dim, wst, s.pair ? kTileN / 2 : kTileN)) != cudaSuccess) return e;
+    cut_product(p, s.pair, a.rows, a.n_tokens, a.dim, 1);
     p.mask = a.mask;
     p.mask_words = (a.n_tokens + 31) / 32;
     p.targets = a.targets;
@@ -687,7 +735,7 @@ cudaError_t launch_token_loss(const LossArgs& a, const LaunchEnv& env, void* spa
     p.part_pitch = s.part_pitch;
     p.target_logit = (float*)(ws + s.target_logit);
     p.err = a.err;
-    if ((e = launch_product<kFoldLogSum>(env, p, st)) != cudaSuccess) return e;
+    if ((e = launch_product<kFoldLogSum>(env, s.pair, p, st)) != cudaSuccess) return e;
     return launch_pdl(loss_kernel, dim3((unsigned)ceil_div(a.rows, kMergeThreads / 32)), dim3(kMergeThreads), 0, st,
                       (const float2*)p.part, s.part_pitch, s.part_pitch, (const float*)p.target_logit, a.targets, a.mask,
                       a.rows, a.n_tokens, a.loss, a.lse, a.err);
@@ -717,9 +765,9 @@ cudaError_t launch_token_loss_grad(const LossArgs& a, const LaunchEnv& env, void
         const int32_t n = std::min(s.piece, a.n_tokens - v0), width = ceil_div(n, kTileN) * kTileN;
         const char* wp = w + (int64_t)v0 * wst * 2;
         Product g{};   // G of the piece, [rows][width]
-        if ((e = make_map(&g.a, h, a.rows, a.dim, s.pitch, kTileM)) != cudaSuccess) return e;
-        if ((e = make_map(&g.b, wp, n, a.dim, wst, kTileN)) != cudaSuccess) return e;
-        cut_product(g, a.rows, n, a.dim, 1);
+        if ((e = make_map(&g.a, h, a.rows, a.dim, s.pitch, kRowsM)) != cudaSuccess) return e;
+        if ((e = make_map(&g.b, wp, n, a.dim, wst, s.pair ? kTileN / 2 : kTileN)) != cudaSuccess) return e;
+        cut_product(g, s.pair, a.rows, n, a.dim, 1);
         g.mask = a.mask ? a.mask + v0 / 32 : nullptr;
         g.mask_words = words;
         g.targets = a.targets;
@@ -728,22 +776,23 @@ cudaError_t launch_token_loss_grad(const LossArgs& a, const LaunchEnv& env, void
         g.coef = coef;
         if ((e = make_out_map(&g.to, ws + s.grad, a.rows, width, width)) != cudaSuccess) return e;
         g.err = a.err;
-        if ((e = launch_product<kFoldGrad>(env, g, st)) != cudaSuccess) return e;
+        if ((e = launch_product<kFoldGrad>(env, s.pair, g, st)) != cudaSuccess) return e;
         Product d{};   // its part of the hidden gradient
-        if ((e = make_map(&d.a, ws + s.grad, a.rows, width, width, kTileM)) != cudaSuccess) return e;
+        if ((e = make_map(&d.a, ws + s.grad, a.rows, width, width, kRowsM)) != cudaSuccess) return e;
         if ((e = make_map(&d.b, wp, n, a.dim, wst, 64)) != cudaSuccess) return e;
-        cut_product(d, a.rows, a.dim, n, s.splits);
+        cut_product(d, s.pair, a.rows, a.dim, n, s.splits);
         d.b_mn = 1;
         d.plane_rows = s.plane_rows;
         e = make_plane_map(&d.to, ws + s.planes, (int64_t)s.splits * s.plane_rows, a.dim, s.pitch);
         if (e != cudaSuccess) return e;
         d.add = v0 > 0;
         d.err = a.err;
-        if ((e = launch_product<kFoldHidden>(env, d, st)) != cudaSuccess) return e;
+        if ((e = launch_product<kFoldHidden>(env, s.pair, d, st)) != cudaSuccess) return e;
+        const bool pair_w = n > kRowsM;
         Product g2{};   // the piece's rows of the weight's gradient
         if ((e = make_map(&g2.a, ws + s.grad, a.rows, width, width, 64)) != cudaSuccess) return e;
         if ((e = make_map(&g2.b, h, a.rows, a.dim, s.pitch, 64)) != cudaSuccess) return e;
-        cut_product(g2, n, a.dim, a.rows, 1);
+        cut_product(g2, pair_w, n, a.dim, a.rows, 1);
         g2.a_mn = g2.b_mn = 1;
         __nv_bfloat16* rows = (__nv_bfloat16*)a.dweight + (int64_t)v0 * a.dweight_stride;
         if (tma_ready(a.dweight, a.dweight_stride)) {
@@ -754,7 +803,7 @@ cudaError_t launch_token_loss_grad(const LossArgs& a, const LaunchEnv& env, void
         }
         g2.scale = scale;
         g2.err = a.err;
-        if ((e = launch_product<kFoldWeight>(env, g2, st)) != cudaSuccess) return e;
+        if ((e = launch_product<kFoldWeight>(env, pair_w, g2, st)) != cudaSuccess) return e;
     }
     const int64_t cells = (int64_t)a.rows * (s.pitch / 4);
     return launch_pdl(dhidden_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(cells, kPackThreads), env.num_sms * 8)),
