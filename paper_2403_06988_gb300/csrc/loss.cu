@@ -658,16 +658,18 @@ constexpr int64_t kGradBytes = (int64_t)256 << 20;
 // last of few tiles empty (GB300, us single / pairs, loss and gradient: 256 rows,
 // V = 128256, 4096 wide 208, 732 / 192, 656; 777 rows, V = 32003, 1024 wide 44,
 // 148 / 53, 151; 1024 rows, V = 65536, 1024 wide 94, 320 / 94, 287; 4096 rows, V =
-// 128256, 4096 wide 2440, 8420 / 2440, 7900).
-bool rows_in_pairs(int32_t rows) {
+// 128256, 4096 wide 2440, 8420 / 2440, 7900).  Rows off 128-byte lines (each of
+// TMA's 128 bytes takes two lines) gain more by reading less: 777 rows, 1000 wide 66,
+// 186 / 58, 168.
+bool rows_in_pairs(int32_t rows, bool off_lines) {
     const int tiles = ceil_div(rows, kRowsM);
-    return tiles % 2 == 0 || tiles > 15;
+    return tiles % 2 == 0 || tiles > 15 || (tiles > 1 && off_lines);
 }
 
 LossSpace loss_space(const LossArgs& a, const LaunchEnv& env, bool grad) {
     LossSpace s{};
-    s.pair = rows_in_pairs(a.rows);
     s.pitch = (a.dim + 7) / 8 * 8;
+    s.pair = rows_in_pairs(a.rows, s.pitch % 64 != 0);
     size_t at = 0;
     const auto take = [&](size_t n) {
         const size_t p = at;
