@@ -15,67 +15,64 @@ from . import _binding as B
 from ._binding import DominoError, DTYPE_BF16, DTYPE_F32  # noqa: F401
 
 
+_T = None        # torch, and its types' codes, once a method below has been called
+_CODES = {}
+
+
 def _torch():
-    import torch
-    return torch
+    global _T
+    if _T is None:
+        import torch
+        _CODES.update({torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32})
+        _T = torch
+    return _T
 
 
-def _dtype(x) -> int:
-    torch = _torch()
-    if x.dtype == torch.bfloat16:
-        return DTYPE_BF16
-    if x.dtype == torch.float32:
-        return DTYPE_F32
-    raise TypeError("float32 or bfloat16 expected")
-
-
-def _rows(x, what, dtype=None, cols=None, rows=None):
-    """x, a matrix of contiguous rows (of `dtype`, with `cols` columns and `rows` rows where given)."""
-    if x.dim() != 2 or (cols is not None and x.shape[1] != cols) or (rows is not None and x.shape[0] != rows):
-        raise ValueError(f"{what}: shape {tuple(x.shape)}")
-    if dtype is not None and x.dtype != dtype:
-        raise TypeError(f"{what} must be {dtype}")
-    if x.shape[1] > 1 and x.stride(1) != 1:
+def _matrix(x, device, what):
+    """(rows, columns, elements from a row to the next, type code) of a matrix of contiguous rows on `device`."""
+    if x.dim() != 2:
+        raise ValueError(f"{what}: a matrix expected, not {tuple(x.shape)}")
+    rows, cols = x.shape
+    step, one = x.stride()
+    if one != 1 and cols > 1:
         raise ValueError(f"{what} rows must be contiguous")
-    return x
+    code = _CODES.get(x.dtype)
+    if code is None:
+        raise TypeError(f"{what} must be float32 or bfloat16")
+    if x.get_device() != device:
+        raise ValueError(f"{what} must be on the handle's device")
+    return rows, cols, step if rows > 1 else cols, code
 
 
-def _step(x) -> int:
-    """Elements from a row to the next; of at most one row, its length."""
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+def _like(x, device, what, rows, cols, code):
+    """Elements from a row of x to the next; x is a matrix of this shape and type."""
+    got = _matrix(x, device, what)
+    if got[0] != rows or got[1] != cols:
+        raise ValueError(f"{what}: shape {(rows, cols)} expected, not {got[:2]}")
+    if got[3] != code:
+        raise TypeError(f"{what} must be of the inputs' type")
+    return got[2]
 
 
-def _ints(x, shape, what):
-    if x.dtype != _torch().int32:
-        raise TypeError(f"{what} must be int32")
-    if tuple(x.shape) != tuple(shape) or not x.is_contiguous():
-        raise ValueError(f"{what}: {tuple(shape)} contiguous expected")
-
-
-def _floats(x, n, what):
-    if x.dtype != _torch().float32:
-        raise TypeError(f"{what} must be float32")
+def _words(x, device, dtype, n, what):
+    """The address of n contiguous values of a 4-byte type."""
+    if x.dtype is not dtype:
+        raise TypeError(f"{what} must be {dtype}")
     if x.numel() != n or not x.is_contiguous():
-        raise ValueError(f"{what}: {n} contiguous values expected")
-    return x
+        raise ValueError(f"{what}: {n} contiguous values expected, not {tuple(x.shape)}")
+    if x.get_device() != device:
+        raise ValueError(f"{what} must be on the handle's device")
+    return x.data_ptr()
 
 
-def _mask(mask, rows, n_tokens):
-    if mask is not None and (tuple(mask.shape) != (rows, (n_tokens + 31) // 32) or mask.element_size() != 4
-                             or not mask.is_contiguous()):
+def _mask_words(mask, device, rows, n_tokens):
+    if mask is None:
+        return None
+    if mask.shape != (rows, (n_tokens + 31) >> 5) or mask.element_size() != 4 or not mask.is_contiguous():
         raise ValueError("mask: one contiguous row of ceil(n_tokens / 32) 32-bit words per row expected")
-
-
-def _distill_args(logits, teacher, ids, mask):
-    _rows(logits, "logits")
-    rows, V = logits.shape
-    _rows(teacher, "teacher", rows=rows)
-    k = teacher.shape[1]
-    if not teacher.is_contiguous():
-        raise ValueError("teacher must be contiguous")
-    _ints(ids, (rows, k), "ids")
-    _mask(mask, rows, V)
-    return rows, V, k
+    if mask.get_device() != device:
+        raise ValueError("mask must be on the handle's device")
+    return mask.data_ptr()
 
 
 class Domino:
@@ -257,92 +254,114 @@ class Domino:
         return so
 
     # -- losses over the vocabulary, the embedding (no loaded vocabulary needed) -----
+    def _floats(self, out, i, n, like, what):
+        """out[i], or a new fp32 tensor of n values, and its address."""
+        x = None if out is None else out[i]
+        if x is None:
+            x = self._empty(n, _T.float32, like.device)
+            return x, x.data_ptr()
+        return x, _words(x, self.device, _T.float32, n, what)
+
+    def _loss_inputs(self, hidden, weight, targets, mask):
+        torch, dev = _torch(), self.device
+        rows, dim, hs, code = _matrix(hidden, dev, "hidden")
+        V, wd, ws, wcode = _matrix(weight, dev, "weight")
+        if wd != dim:
+            raise ValueError(f"weight: {dim} columns expected, not {wd}")
+        if wcode != code:
+            raise TypeError("weight must be of hidden's type")
+        return (self.h, hidden.data_ptr(), hs, weight.data_ptr(), ws, code, rows, dim, V,
+                _mask_words(mask, dev, rows, V), _words(targets, dev, torch.int32, rows, "targets"))
+
     def token_loss(self, hidden, weight, targets, mask=None, out=None, stream=None) -> Tuple:
         """Cross entropy of `targets` under the masked softmax of hidden @ weight.T, the logits never kept: (loss,
         lse), fp32 [rows].  hidden [rows, dim], weight [n_tokens, dim] bf16; targets int32 (below 0: none); mask as
         step_mask's or None.  out: (loss, lse) to write to."""
-        hidden, weight = _rows(hidden, "hidden"), _rows(weight, "weight", hidden.dtype, hidden.shape[1])
-        rows = hidden.shape[0]
-        _ints(targets, (rows,), "targets")
-        _mask(mask, rows, weight.shape[0])
-        loss, lse = out if out is not None else (None, None)
-        if loss is None:
-            loss = self._empty(rows, _torch().float32, hidden.device)
-        if lse is None:
-            lse = self._empty(rows, _torch().float32, hidden.device)
-        B.domino_token_loss(self.h, hidden.data_ptr(), _step(hidden), weight.data_ptr(), _step(weight), _dtype(hidden),
-                            rows, hidden.shape[1], weight.shape[0], mask, targets, _floats(loss, rows, "loss"),
-                            _floats(lse, rows, "lse"), stream)
+        args = self._loss_inputs(hidden, weight, targets, mask)
+        loss, pl = self._floats(out, 0, args[6], hidden, "loss")
+        lse, pz = self._floats(out, 1, args[6], hidden, "lse")
+        B.domino_token_loss(*args, pl, pz, stream)
         return loss, lse
 
     def token_loss_grad(self, hidden, weight, targets, lse, grad_loss, mask=None, out=None, stream=None) -> Tuple:
         """(dhidden, dweight) of sum(grad_loss * loss), lse as token_loss returned it; in the inputs' type."""
-        hidden, weight = _rows(hidden, "hidden"), _rows(weight, "weight", hidden.dtype, hidden.shape[1])
-        rows = hidden.shape[0]
-        _ints(targets, (rows,), "targets")
-        _mask(mask, rows, weight.shape[0])
+        args = self._loss_inputs(hidden, weight, targets, mask)
+        code, rows, dim, V = args[5:9]
         dh, dw = out if out is not None else (None, None)
+        hs = ws = dim
         if dh is None:
-            dh = self._empty(tuple(hidden.shape), hidden.dtype, hidden.device)
+            dh = self._empty((rows, dim), hidden.dtype, hidden.device)
+        else:
+            hs = _like(dh, self.device, "dhidden", rows, dim, code)
         if dw is None:
-            dw = self._empty(tuple(weight.shape), weight.dtype, weight.device)
-        _rows(dh, "dhidden", hidden.dtype, hidden.shape[1], rows)
-        _rows(dw, "dweight", weight.dtype, weight.shape[1], weight.shape[0])
-        B.domino_token_loss_grad(self.h, hidden.data_ptr(), _step(hidden), weight.data_ptr(), _step(weight),
-                                 _dtype(hidden), rows, hidden.shape[1], weight.shape[0], mask, targets,
-                                 _floats(lse, rows, "lse"), _floats(grad_loss, rows, "grad_loss"), dh.data_ptr(),
-                                 _step(dh), dw.data_ptr(), _step(dw), stream)
+            dw = self._empty((V, dim), weight.dtype, weight.device)
+        else:
+            ws = _like(dw, self.device, "dweight", V, dim, code)
+        B.domino_token_loss_grad(*args, _words(lse, self.device, _T.float32, rows, "lse"),
+                                 _words(grad_loss, self.device, _T.float32, rows, "grad_loss"), dh.data_ptr(), hs,
+                                 dw.data_ptr(), ws, stream)
         return dh, dw
+
+    def _distill_inputs(self, logits, teacher, ids, temperature, mask):
+        torch, dev = _torch(), self.device
+        rows, V, step, code = _matrix(logits, dev, "logits")
+        trows, k, tstep, tcode = _matrix(teacher, dev, "teacher")
+        if trows != rows or tstep != k:
+            raise ValueError(f"teacher: {rows} contiguous rows expected")
+        if ids.shape != teacher.shape:
+            raise ValueError("ids must have the teacher's shape")
+        return (self.h, logits.data_ptr(), code, rows, step, V, _mask_words(mask, dev, rows, V), teacher.data_ptr(),
+                tcode, _words(ids, dev, torch.int32, rows * k, "ids"), k, temperature)
 
     def distill_loss(self, logits, teacher, ids, temperature: float = 1.0, mask=None, out=None, stream=None) -> Tuple:
         """Divergence of the teacher's top logits (teacher, ids [rows, k]; ids below 0: no entry) from the masked
         softmax of logits / temperature, times temperature^2: (loss, lse), fp32 [rows]."""
-        rows, V, k = _distill_args(logits, teacher, ids, mask)
-        loss, lse = out if out is not None else (None, None)
-        if loss is None:
-            loss = self._empty(rows, _torch().float32, logits.device)
-        if lse is None:
-            lse = self._empty(rows, _torch().float32, logits.device)
-        B.domino_distill_loss(self.h, logits.data_ptr(), _dtype(logits), rows, _step(logits), V, mask, teacher,
-                              _dtype(teacher), ids, k, temperature, _floats(loss, rows, "loss"),
-                              _floats(lse, rows, "lse"), stream)
+        args = self._distill_inputs(logits, teacher, ids, temperature, mask)
+        loss, pl = self._floats(out, 0, args[3], logits, "loss")
+        lse, pz = self._floats(out, 1, args[3], logits, "lse")
+        B.domino_distill_loss(*args, pl, pz, stream)
         return loss, lse
 
     def distill_grad(self, logits, teacher, ids, temperature: float, lse, grad_loss, mask=None, out=None, stream=None):
         """d sum(grad_loss * loss) / d logits, in the logits' type; out may be `logits` itself."""
-        rows, V, k = _distill_args(logits, teacher, ids, mask)
+        args = self._distill_inputs(logits, teacher, ids, temperature, mask)
+        rows, V = args[3], args[5]
+        step = V
         if out is None:
             out = self._empty((rows, V), logits.dtype, logits.device)
-        _rows(out, "out", logits.dtype, V, rows)
-        B.domino_distill_grad(self.h, logits.data_ptr(), _dtype(logits), rows, _step(logits), V, mask, teacher,
-                              _dtype(teacher), ids, k, temperature, _floats(lse, rows, "lse"),
-                              _floats(grad_loss, rows, "grad_loss"), out.data_ptr(), _step(out), stream)
+        else:
+            step = _like(out, self.device, "out", rows, V, args[2])
+        B.domino_distill_grad(*args, _words(lse, self.device, _T.float32, rows, "lse"),
+                              _words(grad_loss, self.device, _T.float32, rows, "grad_loss"), out.data_ptr(), step, stream)
         return out
 
     def embed(self, tokens, weight, scale: float = 1.0, out=None, stream=None):
         """scale * weight[tokens], zeros for tokens below 0: [n, dim] of the weight's type."""
-        weight = _rows(weight, "weight")
-        n, dim = tokens.shape[0], weight.shape[1]
-        _ints(tokens, (n,), "tokens")
+        torch, dev = _torch(), self.device
+        V, dim, ws, code = _matrix(weight, dev, "weight")
+        n = tokens.numel()
+        pt = _words(tokens, dev, torch.int32, n, "tokens")
+        step = dim
         if out is None:
             out = self._empty((n, dim), weight.dtype, weight.device)
-        _rows(out, "out", weight.dtype, dim, n)
-        B.domino_embed(self.h, tokens, n, weight.data_ptr(), _step(weight), _dtype(weight), weight.shape[0], dim, scale,
-                       out.data_ptr(), _step(out), stream)
+        else:
+            step = _like(out, dev, "out", n, dim, code)
+        B.domino_embed(self.h, pt, n, weight.data_ptr(), ws, code, V, dim, scale, out.data_ptr(), step, stream)
         return out
 
     def embed_grad(self, tokens, grad, n_tokens: int, scale: float = 1.0, into=None, stream=None):
         """Gradient of the table [n_tokens, dim]: scale * the sums of grad's rows by token.  into: a gradient that the
         sums are added to (the loss's, for a table that is its weight too)."""
-        grad = _rows(grad, "grad")
-        n, dim = grad.shape
-        _ints(tokens, (n,), "tokens")
-        dw = into
+        torch, dev = _torch(), self.device
+        n, dim, gs, code = _matrix(grad, dev, "grad")
+        pt = _words(tokens, dev, torch.int32, n, "tokens")
+        dw, step = into, dim
         if dw is None:
             dw = self._empty((n_tokens, dim), grad.dtype, grad.device)
-        _rows(dw, "into", grad.dtype, dim, n_tokens)
-        B.domino_embed_grad(self.h, tokens, n, grad.data_ptr(), _step(grad), _dtype(grad), n_tokens, dim, scale,
-                            0 if into is None else 1, dw.data_ptr(), _step(dw), stream)
+        else:
+            step = _like(dw, dev, "into", n_tokens, dim, code)
+        B.domino_embed_grad(self.h, pt, n, grad.data_ptr(), gs, code, n_tokens, dim, scale, 0 if into is None else 1,
+                            dw.data_ptr(), step, stream)
         return dw
 
     def device_error(self, stream=None) -> int:

@@ -322,52 +322,65 @@ def domino_mask_logits_noalloc(logits_dev, dtype: int, batch: int, n_tokens: int
         _ptr(argmax_dev), _ptr(lse_dev), _ptr(logprobs_dev), _stream(stream)))
 
 
+def _address(x):
+    return x if x is None or type(x) is int else _ptr(x)
+
+
 def domino_token_loss(h: int, hidden_dev, hidden_stride: int, weight_dev, weight_stride: int, dtype: int, rows: int,
                       dim: int, n_tokens: int, mask_dev, targets_dev, loss_dev, lse_dev=None, stream=None) -> None:
-    _check("domino_token_loss", lib().domino_token_loss(
-        h, _ptr(hidden_dev), int(hidden_stride), _ptr(weight_dev), int(weight_stride), int(dtype), int(rows), int(dim),
-        int(n_tokens), _ptr(mask_dev), _ptr(targets_dev), _ptr(loss_dev), _ptr(lse_dev), _stream(stream)))
+    rc = lib().domino_token_loss(
+        h, _address(hidden_dev), hidden_stride, _address(weight_dev), weight_stride, dtype, rows, dim, n_tokens,
+        _address(mask_dev), _address(targets_dev), _address(loss_dev), _address(lse_dev), _stream(stream))
+    if rc:
+        _check("domino_token_loss", rc)
 
 
 def domino_token_loss_grad(h: int, hidden_dev, hidden_stride: int, weight_dev, weight_stride: int, dtype: int,
                            rows: int, dim: int, n_tokens: int, mask_dev, targets_dev, lse_dev, grad_loss_dev,
                            dhidden_dev, dhidden_stride: int, dweight_dev, dweight_stride: int, stream=None) -> None:
-    _check("domino_token_loss_grad", lib().domino_token_loss_grad(
-        h, _ptr(hidden_dev), int(hidden_stride), _ptr(weight_dev), int(weight_stride), int(dtype), int(rows), int(dim),
-        int(n_tokens), _ptr(mask_dev), _ptr(targets_dev), _ptr(lse_dev), _ptr(grad_loss_dev), _ptr(dhidden_dev),
-        int(dhidden_stride), _ptr(dweight_dev), int(dweight_stride), _stream(stream)))
+    rc = lib().domino_token_loss_grad(
+        h, _address(hidden_dev), hidden_stride, _address(weight_dev), weight_stride, dtype, rows, dim, n_tokens,
+        _address(mask_dev), _address(targets_dev), _address(lse_dev), _address(grad_loss_dev), _address(dhidden_dev),
+        dhidden_stride, _address(dweight_dev), dweight_stride, _stream(stream))
+    if rc:
+        _check("domino_token_loss_grad", rc)
 
 
 def domino_distill_loss(h: int, logits_dev, dtype: int, rows: int, row_stride_elems: int, n_tokens: int, mask_dev,
                         teacher_dev, teacher_dtype: int, ids_dev, k: int, temperature: float, loss_dev, lse_dev=None,
                         stream=None) -> None:
-    _check("domino_distill_loss", lib().domino_distill_loss(
-        h, _ptr(logits_dev), int(dtype), int(rows), int(row_stride_elems), int(n_tokens), _ptr(mask_dev),
-        _ptr(teacher_dev), int(teacher_dtype), _ptr(ids_dev), int(k), float(temperature), _ptr(loss_dev),
-        _ptr(lse_dev), _stream(stream)))
+    rc = lib().domino_distill_loss(
+        h, _address(logits_dev), dtype, rows, row_stride_elems, n_tokens, _address(mask_dev), _address(teacher_dev),
+        teacher_dtype, _address(ids_dev), k, temperature, _address(loss_dev), _address(lse_dev), _stream(stream))
+    if rc:
+        _check("domino_distill_loss", rc)
 
 
 def domino_distill_grad(h: int, logits_dev, dtype: int, rows: int, row_stride_elems: int, n_tokens: int, mask_dev,
                         teacher_dev, teacher_dtype: int, ids_dev, k: int, temperature: float, lse_dev, grad_loss_dev,
                         dlogits_dev, dlogits_stride: int, stream=None) -> None:
-    _check("domino_distill_grad", lib().domino_distill_grad(
-        h, _ptr(logits_dev), int(dtype), int(rows), int(row_stride_elems), int(n_tokens), _ptr(mask_dev),
-        _ptr(teacher_dev), int(teacher_dtype), _ptr(ids_dev), int(k), float(temperature), _ptr(lse_dev),
-        _ptr(grad_loss_dev), _ptr(dlogits_dev), int(dlogits_stride), _stream(stream)))
+    rc = lib().domino_distill_grad(
+        h, _address(logits_dev), dtype, rows, row_stride_elems, n_tokens, _address(mask_dev), _address(teacher_dev),
+        teacher_dtype, _address(ids_dev), k, temperature, _address(lse_dev), _address(grad_loss_dev),
+        _address(dlogits_dev), dlogits_stride, _stream(stream))
+    if rc:
+        _check("domino_distill_grad", rc)
 
 
 def domino_embed(h: int, tokens_dev, n: int, weight_dev, weight_stride: int, dtype: int, n_tokens: int, dim: int,
                  scale: float, out_dev, out_stride: int, stream=None) -> None:
-    _check("domino_embed", lib().domino_embed(
-        h, _ptr(tokens_dev), int(n), _ptr(weight_dev), int(weight_stride), int(dtype), int(n_tokens), int(dim),
-        float(scale), _ptr(out_dev), int(out_stride), _stream(stream)))
+    rc = lib().domino_embed(h, _address(tokens_dev), n, _address(weight_dev), weight_stride, dtype, n_tokens, dim, scale,
+                            _address(out_dev), out_stride, _stream(stream))
+    if rc:
+        _check("domino_embed", rc)
 
 
 def domino_embed_grad(h: int, tokens_dev, n: int, grad_dev, grad_stride: int, dtype: int, n_tokens: int, dim: int,
                       scale: float, accumulate: int, dweight_dev, dweight_stride: int, stream=None) -> None:
-    _check("domino_embed_grad", lib().domino_embed_grad(
-        h, _ptr(tokens_dev), int(n), _ptr(grad_dev), int(grad_stride), int(dtype), int(n_tokens), int(dim),
-        float(scale), int(accumulate), _ptr(dweight_dev), int(dweight_stride), _stream(stream)))
+    rc = lib().domino_embed_grad(h, _address(tokens_dev), n, _address(grad_dev), grad_stride, dtype, n_tokens, dim,
+                                 scale, accumulate, _address(dweight_dev), dweight_stride, _stream(stream))
+    if rc:
+        _check("domino_embed_grad", rc)
 
 
 def domino_get_device_error(h: int, stream=None) -> int:
