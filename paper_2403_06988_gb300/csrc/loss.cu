@@ -18,7 +18,7 @@
 //                 memory, eight warps that fold one accumulator while the next
 //                 is filled.  What it does with a tile is its Fold.
 // loss_kernel     merges a row's partials into lse and loss.
-// coef_kernel, pack_kernel, dhidden_kernel: the rows' coefficients, operands
+// prep_kernel, dhidden_kernel: the rows' coefficients and operands
 //                 laid out for TMA, the sum of the hidden gradient's parts.
 #include <cuda_bf16.h>
 
@@ -32,30 +32,33 @@
 namespace domino {
 namespace {
 
-// Tiles of a product: kRowsM rows of A a CTA and kTileN of B.  PAIR: two CTAs
-// make 2 * kRowsM rows and hold half of B each, so that a product's operands
-// take two thirds of the bytes.
-constexpr int kRowsM = 128, kTileN = 256, kTileK = 64;
-constexpr int kAccs = 2;                       // accumulators of kTileN columns: all of tensor memory
-constexpr int kTmemColumns = kAccs * kTileN;
-template <bool PAIR>
+// Tiles of a product: kRowsM rows of A a CTA and N of B.  PAIR: two CTAs make
+// 2 * kRowsM rows and hold half of B each, so that a product's operands take two
+// thirds of the bytes.
+constexpr int kRowsM = 128, kTileK = 64, kWideN = 256, kNarrowN = 64;
+constexpr int kAccs = 2;                       // accumulators of N columns: of 256, all of tensor memory
+constexpr int kRingBytes = 196608;             // of operand tiles on their way
+constexpr int kFoldWarps = 8;
+template <bool PAIR, int N>
 struct Tile {
     static constexpr int kCtas = PAIR ? 2 : 1;
-    static constexpr int kM = kRowsM * kCtas;
-    static constexpr int kRowsB = kTileN / kCtas;      // a CTA's
-    static constexpr int kStages = PAIR ? 6 : 4;
+    static constexpr int kM = kRowsM * kCtas, kN = N;
+    static constexpr int kRowsB = N / kCtas;           // a CTA's
     static constexpr int kBytesA = kRowsM * kTileK * 2, kBytesB = kRowsB * kTileK * 2;
-    static constexpr int kStageBytes = kBytesA + kBytesB;
+    static constexpr int kStageBytes = kBytesA + kBytesB, kStages = kRingBytes / kStageBytes;
+    static constexpr int kColumns = N / (kFoldWarps / 4);   // a fold warp's: 32 rows, half of the columns
+    static_assert(kStages * kStageBytes == kRingBytes && kColumns % 32 == 0);
 };
-constexpr int kRingBytes = 196608;
-static_assert(Tile<false>::kStages * Tile<false>::kStageBytes == kRingBytes);
-static_assert(Tile<true>::kStages * Tile<true>::kStageBytes == kRingBytes);
-constexpr int kFoldWarps = 8;
+// Which tiles a launch takes: 256 x 256 of two CTAs, 128 x 256, 128 x 64.
+enum Shape : int { kPair = 0, kWide = 1, kNarrow = 2 };
+int shape_m(Shape s) { return s == kPair ? 2 * kRowsM : kRowsM; }
+int shape_n(Shape s) { return s == kNarrow ? kNarrowN : kWideN; }
+int shape_box(Shape s) { return s == kWide ? kWideN : s == kPair ? kWideN / 2 : kNarrowN; }   // rows of B a CTA loads
+
 // Results leave through shared memory: 32 rows of 64 bytes a warp's buffer, in the 64-byte swizzle.
 constexpr int kOutBytes = 32 * 64, kOutBuffers = 16 / kFoldWarps;
 constexpr int kProductSmem = kRingBytes + kFoldWarps * kOutBuffers * kOutBytes + 1024;   // tiles lie on 1024-byte boundaries
 constexpr int kProductThreads = 128 + 32 * kFoldWarps;
-constexpr int kFoldColumns = kTileN / (kFoldWarps / 4);      // a warp's: 32 rows, half of the columns
 constexpr int kGroupM = 16;                    // row tiles that share a pass over the columns' tiles
 
 // What becomes of a tile of products.
@@ -147,39 +150,45 @@ __device__ __forceinline__ float2 mul2(float2 a, float b) {
 }
 
 // What a warp's lane needs beside the products of its row in a tile.
+template <int COLUMNS>
 struct Side {
-    uint32_t word[kFoldColumns / 32];   // allowed tokens
+    uint32_t word[COLUMNS / 32];        // allowed tokens
     int32_t target;                     // its column
     float lse, coef;
 };
 
-template <int FOLD>
-__device__ __forceinline__ Side load_side(const Product& p, int32_t item, int tile_m, int row_in_tile, int half) {
-    Side s;
+template <int FOLD, typename T>
+__device__ __forceinline__ Side<T::kColumns> load_side(const Product& p, int32_t item, int row_in_tile, int half) {
+    Side<T::kColumns> s;
     const Item t = item_at(p, item);
-    const int32_t row = t.m * tile_m + row_in_tile, c0 = t.n * kTileN + half * kFoldColumns;
+    const int32_t row = t.m * T::kM + row_in_tile, c0 = t.n * T::kN + half * T::kColumns;
     const bool on = row < p.m;
     s.target = on ? (int32_t)((uint32_t)__ldg(p.targets + row) - (uint32_t)p.column0) : -1;
     s.lse = FOLD == kFoldGrad && on ? p.lse[row] : 0.0f;
     s.coef = FOLD == kFoldGrad && on ? p.coef[row] : 0.0f;
     const uint32_t* mrow = p.mask && on ? p.mask + (int64_t)row * p.mask_words : nullptr;
 #pragma unroll
-    for (int j = 0; j < kFoldColumns / 32; ++j) s.word[j] = on ? allowed_word(mrow, c0 + 32 * j, p.n) : 0u;
+    for (int j = 0; j < T::kColumns / 32; ++j) s.word[j] = on ? allowed_word(mrow, c0 + 32 * j, p.n) : 0u;
     return s;
 }
 
-// 16 words (64 bytes) of each lane's row to one of the warp's buffers, and from there to (x, y).
-// A buffer was read by its copy before it is written again.
-__device__ __forceinline__ void put_rows(const CUtensorMap* map, int32_t x, int32_t y, bool add, uint32_t buffer, int lane,
-                                         const uint32_t* w) {
-    if (lane == 0) tma_wait_read<kOutBuffers - 1>();
-    __syncwarp();
+// 16 words (64 bytes) of each lane's row to a buffer.
+__device__ __forceinline__ void put_words(uint32_t buffer, int lane, const uint32_t* w) {
     const uint32_t row = buffer + lane * 64;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(row + ((i ^ ((lane >> 1) & 3)) << 4)), "r"(w[4 * i]),
                      "r"(w[4 * i + 1]), "r"(w[4 * i + 2]), "r"(w[4 * i + 3])
                      : "memory");
+}
+
+// They, to one of the warp's buffers, and from there to (x, y).
+// A buffer was read by its copy before it is written again.
+__device__ __forceinline__ void put_rows(const CUtensorMap* map, int32_t x, int32_t y, bool add, uint32_t buffer, int lane,
+                                         const uint32_t* w) {
+    if (lane == 0) tma_wait_read<kOutBuffers - 1>();
+    __syncwarp();
+    put_words(buffer, lane, w);
     tma_fence();
     __syncwarp();
     if (lane == 0) {
@@ -189,10 +198,10 @@ __device__ __forceinline__ void put_rows(const CUtensorMap* map, int32_t x, int3
     }
 }
 
-template <int FOLD, bool PAIR>
+template <int FOLD, bool PAIR, int N>
 __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ Product p) {
-    using T = Tile<PAIR>;
-    constexpr int kStages = T::kStages;
+    using T = Tile<PAIR, N>;
+    constexpr int kStages = T::kStages, kColumns = T::kColumns, kTmemColumns = kAccs * N;
     extern __shared__ unsigned char smem[];
     __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_acc_full[kAccs], s_acc_empty[kAccs], s_done;
     __shared__ uint32_t s_tmem, s_failed;
@@ -231,7 +240,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             bool ok = true;
             for (int32_t i = first; i < p.items && ok; i += step) {
                 const Item t = item_at(p, i);
-                const int32_t row_a = t.m * T::kM + rank * kRowsM, row_b = t.n * kTileN + rank * T::kRowsB;
+                const int32_t row_a = t.m * T::kM + rank * kRowsM, row_b = t.n * N + rank * T::kRowsB;
                 for (int32_t k = t.k0; k < t.k1; ++k, ++loads) {
                     const uint32_t s = loads % kStages, turn = loads / kStages;
                     if (!(ok = bar_wait(smem_addr(&s_empty[s]), (turn & 1u) ^ 1u, failed))) break;
@@ -252,14 +261,14 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         }
     } else if (warp == 1) {   // ---- products
         if (lane == 0 && rank == 0) {
-            const uint32_t desc = mma_desc(T::kM, kTileN, p.a_mn, p.b_mn);
+            const uint32_t desc = mma_desc(T::kM, N, p.a_mn, p.b_mn);
             // 16 k further: 32 bytes along a row of a K-major tile, 16 rows of an MN-major one (16-byte units)
             const uint32_t step_a = p.a_mn ? 2048 / 16 : 32 / 16, step_b = p.b_mn ? 2048 / 16 : 32 / 16;
             uint32_t loads = 0, accs = 0;
             bool ok = true;
             for (int32_t i = first; i < p.items && ok; i += step, ++accs) {
                 const Item t = item_at(p, i);
-                const uint32_t s_acc = accs % kAccs, acc = tmem + s_acc * kTileN;
+                const uint32_t s_acc = accs % kAccs, acc = tmem + s_acc * N;
                 if (!(ok = bar_wait(smem_addr(&s_acc_empty[s_acc]), ((accs / kAccs) & 1u) ^ 1u, failed))) break;
                 tcgen_after();
                 for (int32_t k = t.k0; k < t.k1; ++k, ++loads) {
@@ -288,32 +297,32 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         const int row_in_tile = rank * kRowsM + quarter * 32 + lane;
         constexpr bool kTokens = FOLD == kFoldLogSum || FOLD == kFoldGrad;
         uint32_t accs = 0, puts = 0;
-        Side next{};
-        if (kTokens && first < p.items) next = load_side<FOLD>(p, first, T::kM, row_in_tile, half);
+        Side<kColumns> next{};
+        if (kTokens && first < p.items) next = load_side<FOLD, T>(p, first, row_in_tile, half);
         float scale = 1.0f;
         if constexpr (FOLD == kFoldWeight) scale = *p.scale;
         for (int32_t i = first; i < p.items; i += step, ++accs) {
             const Item t = item_at(p, i);
             const uint32_t s_acc = accs % kAccs;
-            const int32_t row = t.m * T::kM + row_in_tile, row0 = row - lane, c0 = t.n * kTileN + half * kFoldColumns;
+            const int32_t row = t.m * T::kM + row_in_tile, row0 = row - lane, c0 = t.n * N + half * kColumns;
             const bool on = row < p.m;
             // the next tile's are on their way while this one is folded
-            const Side side = next;
-            if (kTokens && i + step < p.items) next = load_side<FOLD>(p, i + step, T::kM, row_in_tile, half);
+            const Side<kColumns> side = next;
+            if (kTokens && i + step < p.items) next = load_side<FOLD, T>(p, i + step, row_in_tile, half);
             // the whole warp goes on or leaves: loads from tensor memory are a warp's
             if (!__all_sync(0xffffffffu, bar_wait(smem_addr(&s_acc_full[s_acc]), (accs / kAccs) & 1u, failed))) break;
             tcgen_after();
-            const uint32_t acc = tmem + s_acc * kTileN + half * kFoldColumns + ((uint32_t)(quarter * 32) << 16);
+            const uint32_t acc = tmem + s_acc * N + half * kColumns + ((uint32_t)(quarter * 32) << 16);
             float m = -INFINITY, sum = 0.0f;
 #pragma unroll 1
-            for (int j = 0; j < kFoldColumns / 32; ++j) {
+            for (int j = 0; j < kColumns / 32; ++j) {
                 const int32_t c = c0 + 32 * j;
                 if (c >= p.n && FOLD != kFoldGrad) break;   // the tile's columns beyond the last
                 float v[32];
                 tmem_load32(v, acc + 32 * j);
                 uint32_t word = side.word[0];   // not by an index: the words stay in registers
 #pragma unroll
-                for (int k = 1; k < kFoldColumns / 32; ++k) word = j == k ? side.word[k] : word;
+                for (int k = 1; k < kColumns / 32; ++k) word = j == k ? side.word[k] : word;
                 const uint32_t at = (uint32_t)side.target - (uint32_t)c;   // below 32: the target's place
                 if constexpr (FOLD == kFoldLogSum) {
                     if (__any_sync(0xffffffffu, at < 32u)) {
@@ -381,21 +390,30 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 } else {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] *= scale;
+                    uint32_t w[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
                     if (!p.out) {
-                        uint32_t w[16];
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
                         if (row0 < p.m) put_rows(&p.to, c, row0, false, buffers + (puts++ % kOutBuffers) * kOutBytes, lane, w);
-                    } else if (on) {
-                        __nv_bfloat16* out = p.out + (int64_t)row * p.ld + c;
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (c + e < p.n) out[e] = __float2bfloat16_rn(v[e]);
+                    } else {   // a row after the other, a column a lane
+                        const uint32_t buffer = buffers;
+                        __syncwarp();
+                        put_words(buffer, lane, w);
+                        __syncwarp();
+                        const uint32_t chunk = (uint32_t)lane >> 3, byte = (lane & 7) * 2;
+                        for (int r = 0; r < 32 && row0 + r < p.m; ++r) {
+                            uint16_t x;
+                            asm volatile("ld.shared.u16 %0, [%1];\n"
+                                         : "=h"(x)
+                                         : "r"(buffer + r * 64 + ((chunk ^ ((r >> 1) & 3)) << 4) + byte)
+                                         : "memory");
+                            if (c + lane < p.n) reinterpret_cast<uint16_t*>(p.out + (int64_t)(row0 + r) * p.ld)[c + lane] = x;
+                        }
                     }
                 }
             }
             if constexpr (FOLD == kFoldLogSum) {
-                if (on) p.part[(int64_t)row * p.part_pitch + t.n * (kTileN / kFoldColumns) + half] = make_float2(m, sum);
+                if (on) p.part[(int64_t)row * p.part_pitch + t.n * (N / kColumns) + half] = make_float2(m, sum);
             }
             tcgen_before();
             __syncwarp();
@@ -467,23 +485,76 @@ __global__ void __launch_bounds__(kMergeThreads)
     }
 }
 
-constexpr int kCoefThreads = 1024;
+constexpr int kPackThreads = 256;
 
-// The rows' coefficients over the largest finite one's magnitude: what G is
-// rounded from.  G is kept in bf16, so a coefficient that all rows share (a
-// mean's 1 / rows) would otherwise be off by one rounding, the same in every
-// entry; the scale is given back in fp32.
-__global__ void __launch_bounds__(kCoefThreads)
-    coef_kernel(const int32_t* targets, const uint32_t* mask, const float* grad_loss, int32_t rows, int32_t V, float* coef,
-                float* scale, uint32_t* err) {
-    __shared__ float s_top[kCoefThreads / 32];
-    pdl_wait();
-    pdl_trigger();
+// Rows of bf16 to be laid out in rows of `pitch` (a multiple of 8: what TMA can
+// read).  GRAD: rows without a gradient become zeros, so that what stands in them
+// (a padding's NaN) meets no other row.
+struct Pack {
+    const __nv_bfloat16* src;
+    int64_t stride;
+    int32_t rows, cols;
+    __nv_bfloat16* dst;
+    int64_t pitch;
+    bool aligned;                  // rows of src begin on 16-byte boundaries
+};
+
+// Eight values from column c on; zeros beyond the last column.  Rows off 16-byte
+// boundaries are read in the 16-byte blocks that hold the values.
+__device__ __forceinline__ uint4 read_eight(const Pack& p, const __nv_bfloat16* from, int32_t c) {
+    if (c + 8 <= p.cols) {
+        if (p.aligned) return __ldg(reinterpret_cast<const uint4*>(from + c));
+        const uintptr_t at = reinterpret_cast<uintptr_t>(from + c);
+        const uint4* block = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
+        const uint32_t off = (uint32_t)(at & 15) / 2;
+        const uint4 a = __ldg(block);
+        if (off == 0) return a;
+        const uint4 b = __ldg(block + 1);
+        uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = off & 4 ? w[i + 2] : w[i];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = off & 2 ? w[i + 1] : w[i];
+        const uint32_t shift = off & 1 ? 16 : 0;
+        return make_uint4(__funnelshift_r(w[0], w[1], shift), __funnelshift_r(w[1], w[2], shift),
+                          __funnelshift_r(w[2], w[3], shift), __funnelshift_r(w[3], w[4], shift));
+    }
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (c + i < p.cols) w[i / 2] |= (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(from + c + i)) << (16 * (i & 1));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+struct Prep {
+    Pack pack[2];                  // hidden, weight; rows 0: none
+    int32_t ctas[2];               // of each
+    // gradient: the rows' coefficients, by one CTA more, the first
+    bool grad;
+    const int32_t* targets;
+    const uint32_t* mask;
+    const float* grad_loss;
+    int32_t rows, n_tokens;
+    float* coef;
+    float* scale;
+    uint32_t* err;
+};
+
+__device__ __forceinline__ float row_coef(const Prep& p, int32_t t, uint32_t* report) {
+    bool excluded;
+    return has_target(p.targets, p.mask, (p.n_tokens + 31) / 32, p.n_tokens, t, report, &excluded) ? __ldg(p.grad_loss + t) : 0.0f;
+}
+
+// Coefficients over the largest finite one's magnitude: what G is rounded from.
+// G is kept in bf16, so a coefficient that all rows share (a mean's 1 / rows)
+// would otherwise be off by one rounding, the same in every entry; the scale is
+// given back in fp32.
+__device__ void make_coefs(const Prep& p) {
+    __shared__ float s_top[kPackThreads / 32];
     float top = 0.0f;
-    for (int32_t t = threadIdx.x; t < rows; t += kCoefThreads) {
-        bool excluded;
-        const float c = has_target(targets, mask, (V + 31) / 32, V, t, err, &excluded) ? __ldg(grad_loss + t) : 0.0f;
-        coef[t] = c;
+    for (int32_t t = threadIdx.x; t < p.rows; t += kPackThreads) {
+        const float c = row_coef(p, t, p.err);
+        p.coef[t] = c;
         if (fabsf(c) <= FLT_MAX) top = fmaxf(top, fabsf(c));
     }
 #pragma unroll
@@ -491,51 +562,70 @@ __global__ void __launch_bounds__(kCoefThreads)
     if ((threadIdx.x & 31) == 0) s_top[threadIdx.x >> 5] = top;
     __syncthreads();
     top = 0.0f;
-    for (int w = 0; w < kCoefThreads / 32; ++w) top = fmaxf(top, s_top[w]);
+    for (int w = 0; w < kPackThreads / 32; ++w) top = fmaxf(top, s_top[w]);
     if (top == 0.0f) top = 1.0f;
-    if (threadIdx.x == 0) *scale = top;
-    for (int32_t t = threadIdx.x; t < rows; t += kCoefThreads) coef[t] = coef[t] / top;
+    if (threadIdx.x == 0) *p.scale = top;
+    for (int32_t t = threadIdx.x; t < p.rows; t += kPackThreads) p.coef[t] = p.coef[t] / top;
 }
 
-constexpr int kPackThreads = 256;
-
-// Rows of bf16 into rows of `pitch` (a multiple of 8: what TMA can read).
-// coef: rows whose coefficient is 0 become zeros, so that what stands in rows
-// without a gradient (a padding's NaN) meets no other row.
-__global__ void __launch_bounds__(kPackThreads)
-    pack_kernel(const __nv_bfloat16* src, int64_t stride, int32_t rows, int32_t cols, __nv_bfloat16* dst, int64_t pitch,
-                const float* coef, bool vec) {
+__global__ void __launch_bounds__(kPackThreads) prep_kernel(const __grid_constant__ Prep p) {
     pdl_wait();
     pdl_trigger();
-    for (int32_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        const bool zero = coef && coef[r] == 0.0f;
-        const __nv_bfloat16* from = src + (int64_t)r * stride;
-        __nv_bfloat16* to = dst + (int64_t)r * pitch;
-        if (vec) {
-            for (int32_t c = threadIdx.x * 8; c < cols; c += kPackThreads * 8)
-                *reinterpret_cast<uint4*>(to + c) = zero ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(from + c));
-        } else {
-            for (int32_t c = threadIdx.x; c < cols; c += kPackThreads) to[c] = zero ? __float2bfloat16_rn(0.0f) : from[c];
-        }
+    int32_t cta = blockIdx.x;
+    if (p.grad && cta-- == 0) return make_coefs(p);
+    const bool second = cta >= p.ctas[0];
+    const Pack& k = p.pack[second];
+    if (second) cta -= p.ctas[0];
+    const uint32_t vectors = (uint32_t)(k.pitch / 8);   // of a row
+    const int64_t n = (int64_t)k.rows * vectors, step = (int64_t)p.ctas[second] * kPackThreads;
+    for (int64_t i = (int64_t)cta * kPackThreads + threadIdx.x; i < n; i += step) {
+        const int32_t r = n <= UINT_MAX ? (int32_t)((uint32_t)i / vectors) : (int32_t)(i / vectors);
+        const int32_t c = (int32_t)(i - (int64_t)r * vectors) * 8;
+        const bool zero = p.grad && !second && row_coef(p, r, nullptr) == 0.0f;
+        *reinterpret_cast<uint4*>(k.dst + r * k.pitch + c) =
+            zero ? make_uint4(0, 0, 0, 0) : read_eight(k, k.src + r * k.stride, c);
     }
 }
 
-// dhidden = scale * the sum of the planes, in their order.
+// dhidden = scale * the sum of the planes.  PARTS threads share a vector's planes
+// (a chain of up to 76 loads would take longer than the rest of a small call).
+template <int PARTS>
 __global__ void __launch_bounds__(kPackThreads)
     dhidden_kernel(const float* planes, int32_t splits, int64_t plane, int32_t rows, int32_t cols, int32_t pitch,
                    const float* scale, __nv_bfloat16* out, int64_t ld) {
+    constexpr int kVectors = kPackThreads / PARTS;   // a CTA's
+    __shared__ float4 s_sum[PARTS][kVectors];
     pdl_wait();
     pdl_trigger();
     const int32_t vectors = pitch / 4;   // of a row of a plane
     const int64_t n = (int64_t)rows * vectors;
+    const int part = threadIdx.x / kVectors, at = threadIdx.x - part * kVectors;
+    const int k0 = splits * part / PARTS, k1 = splits * (part + 1) / PARTS;
     const float s = *scale;
-    for (int64_t i = (int64_t)blockIdx.x * kPackThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kPackThreads) {
-        const int32_t r = (int32_t)(i / vectors), c = (int32_t)(i - (int64_t)r * vectors) * 4;
+    for (int64_t i0 = (int64_t)blockIdx.x * kVectors; i0 < n; i0 += (int64_t)gridDim.x * kVectors) {
+        const int64_t i = i0 + at;
+        const int32_t r = n <= UINT_MAX ? (int32_t)((uint32_t)i / (uint32_t)vectors) : (int32_t)(i / vectors);
+        const int32_t c = (int32_t)(i - (int64_t)r * vectors) * 4;
         float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int k = 0; k < splits; ++k) {
-            const float4 x = *reinterpret_cast<const float4*>(planes + k * plane + (int64_t)r * pitch + c);
-            v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+        if (i < n) {
+#pragma unroll 4
+            for (int k = k0; k < k1; ++k) {
+                const float4 x = *reinterpret_cast<const float4*>(planes + k * plane + (int64_t)r * pitch + c);
+                v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+            }
         }
+        if constexpr (PARTS > 1) {
+            s_sum[part][at] = v;
+            __syncthreads();
+            if (part == 0)
+#pragma unroll
+                for (int k = 1; k < PARTS; ++k) {
+                    const float4 x = s_sum[k][at];
+                    v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+                }
+            __syncthreads();
+        }
+        if (part || i >= n) continue;
         __nv_bfloat16* to = out + (int64_t)r * ld + c;
         const uint32_t lo = pack_bf16(s * v.x, s * v.y), hi = pack_bf16(s * v.z, s * v.w);
         if (c + 4 <= cols && (reinterpret_cast<uintptr_t>(to) & 7) == 0) {
@@ -595,46 +685,49 @@ cudaError_t make_plane_map(CUtensorMap* map, void* base, int64_t rows, int64_t c
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-void cut_product(Product& p, bool pair, int32_t m, int32_t n, int64_t k, int splits) {
+void cut_product(Product& p, Shape shape, int32_t m, int32_t n, int64_t k, int splits) {
     p.m = m;
     p.n = n;
-    p.m_tiles = ceil_div(m, pair ? Tile<true>::kM : Tile<false>::kM);
-    p.n_tiles = ceil_div(n, kTileN);
+    p.m_tiles = ceil_div(m, shape_m(shape));
+    p.n_tiles = ceil_div(n, shape_n(shape));
     p.k_blocks = ceil_div(k, kTileK);
     p.splits = splits;
     p.items = p.m_tiles * p.n_tiles * splits;
 }
 
-template <int FOLD, bool PAIR>
+template <int FOLD, bool PAIR, int N>
 cudaError_t product_smem_ready() {
     constexpr int kDevices = 64;
     static std::atomic<bool> ready[kDevices];   // one array per kernel
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess || (dev < kDevices && ready[dev].load())) return e;
-    e = cudaFuncSetAttribute(product_kernel<FOLD, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
+    e = cudaFuncSetAttribute(product_kernel<FOLD, PAIR, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
     if (e == cudaSuccess && dev < kDevices) ready[dev].store(true);
     return e;
 }
 
-template <int FOLD, bool PAIR>
+template <int FOLD, bool PAIR, int N>
 cudaError_t launch_product_t(const LaunchEnv& env, const Product& p, cudaStream_t st) {
-    if (cudaError_t e = product_smem_ready<FOLD, PAIR>(); e != cudaSuccess) return e;
-    constexpr int kCtas = Tile<PAIR>::kCtas;
+    if (cudaError_t e = product_smem_ready<FOLD, PAIR, N>(); e != cudaSuccess) return e;
+    constexpr int kCtas = Tile<PAIR, N>::kCtas;
     const int at_once = std::max(1, env.num_sms / kCtas);
-    return launch_cluster(product_kernel<FOLD, PAIR>, dim3((unsigned)(std::min(p.items, at_once) * kCtas)), dim3(kProductThreads),
-                          kCtas, kProductSmem, st, p);
+    return launch_cluster(product_kernel<FOLD, PAIR, N>, dim3((unsigned)(std::min(p.items, at_once) * kCtas)),
+                          dim3(kProductThreads), kCtas, kProductSmem, st, p);
 }
 template <int FOLD>
-cudaError_t launch_product(const LaunchEnv& env, bool pair, const Product& p, cudaStream_t st) {
-    return pair ? launch_product_t<FOLD, true>(env, p, st) : launch_product_t<FOLD, false>(env, p, st);
+cudaError_t launch_product(const LaunchEnv& env, Shape shape, const Product& p, cudaStream_t st) {
+    if constexpr (FOLD == kFoldLogSum || FOLD == kFoldGrad)
+        if (shape == kNarrow) return launch_product_t<FOLD, false, kNarrowN>(env, p, st);
+    return shape == kPair ? launch_product_t<FOLD, true, kWideN>(env, p, st) : launch_product_t<FOLD, false, kWideN>(env, p, st);
 }
 
-cudaError_t launch_pack(const LaunchEnv& env, const void* src, int64_t stride, int32_t rows, int32_t cols, void* dst,
-                        int64_t pitch, const float* coef, cudaStream_t st) {
-    const bool vec = reinterpret_cast<uintptr_t>(src) % 16 == 0 && stride % 8 == 0 && cols % 8 == 0;
-    return launch_pdl(pack_kernel, dim3((unsigned)std::min(rows, env.num_sms * 8)), dim3(kPackThreads), 0, st,
-                      (const __nv_bfloat16*)src, stride, rows, cols, (__nv_bfloat16*)dst, pitch, coef, vec);
+cudaError_t launch_prep(const LaunchEnv& env, Prep& p, cudaStream_t st) {
+    for (int i = 0; i < 2; ++i) {
+        const Pack& k = p.pack[i];
+        p.ctas[i] = (int)std::min<int64_t>((k.rows * (k.pitch / 8) + kPackThreads - 1) / kPackThreads, env.num_sms * 8);
+    }
+    return launch_pdl(prep_kernel, dim3((unsigned)(p.grad + p.ctas[0] + p.ctas[1])), dim3(kPackThreads), 0, st, p);
 }
 
 bool tma_ready(const void* p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0; }
@@ -642,8 +735,8 @@ bool tma_ready(const void* p, int64_t stride) { return reinterpret_cast<uintptr_
 // Where a call's parts lie in its workspace.
 struct LossSpace {
     size_t hidden, weight, part, target_logit, coef, scale, grad, planes, end;
-    bool pair;            // products by pairs of CTAs, in the rows of tokens
     int64_t pitch;        // of packed rows
+    Shape logits, sums;   // the products' tiles
     int32_t part_pitch;
     int32_t piece;        // tokens of the vocabulary at a time (gradient)
     int32_t splits;       // of the hidden gradient's sum
@@ -653,23 +746,26 @@ struct LossSpace {
 // G takes at most this many bytes at a time.
 constexpr int64_t kGradBytes = (int64_t)256 << 20;
 
-// Whether pairs of CTAs make the products with `rows` rows of tokens: their
-// tiles are 256 rows high, so not where that leaves a quarter or more of the
-// last of few tiles empty (GB300, us single / pairs, loss and gradient: 256 rows,
-// V = 128256, 4096 wide 208, 732 / 192, 656; 777 rows, V = 32003, 1024 wide 44,
-// 148 / 53, 151; 1024 rows, V = 65536, 1024 wide 94, 320 / 94, 287; 4096 rows, V =
+// The tiles of the logits of `rows` rows and `n` tokens.  Pairs of CTAs have
+// tiles of 256 rows: not where that leaves a quarter or more of the last of few
+// tiles empty (GB300, us single / pairs, loss and gradient: 256 rows, V =
+// 128256, 4096 wide 208, 732 / 192, 656; 777 rows, V = 32003, 1024 wide 44, 148 /
+// 53, 151; 1024 rows, V = 65536, 1024 wide 94, 320 / 94, 287; 4096 rows, V =
 // 128256, 4096 wide 2440, 8420 / 2440, 7900).  Rows off 128-byte lines (each of
 // TMA's 128 bytes takes two lines) gain more by reading less: 777 rows, 1000 wide 66,
-// 186 / 58, 168.
-bool rows_in_pairs(int32_t rows, bool off_lines) {
+// 186 / 58, 168.  Narrow tiles where every SM has at most one: a k block takes
+// them nearly as long as wide ones (us wide / narrow: 300 rows, V = 2000, 256 wide 8.2,
+// 23.4 / 6.6, 21.7; 64 rows, V = 8000, 4096 wide 25.2, 68.7 / 24.9, 59.0; two rounds of
+// them, 64 rows, V = 12000, 512 wide 9.2, 28.0 / 12.0, 30.5).
+Shape logits_shape(const LaunchEnv& env, int32_t rows, int64_t n, bool off_lines) {
     const int tiles = ceil_div(rows, kRowsM);
-    return tiles % 2 == 0 || tiles > 15 || (tiles > 1 && off_lines);
+    if ((int64_t)tiles * ceil_div(n, kNarrowN) <= env.num_sms) return kNarrow;
+    return tiles % 2 == 0 || tiles > 15 || (tiles > 1 && off_lines) ? kPair : kWide;
 }
 
 LossSpace loss_space(const LossArgs& a, const LaunchEnv& env, bool grad) {
     LossSpace s{};
     s.pitch = (a.dim + 7) / 8 * 8;
-    s.pair = rows_in_pairs(a.rows, s.pitch % 64 != 0);
     size_t at = 0;
     const auto take = [&](size_t n) {
         const size_t p = at;
@@ -679,57 +775,72 @@ LossSpace loss_space(const LossArgs& a, const LaunchEnv& env, bool grad) {
     if (grad || !tma_ready(a.hidden, a.hidden_stride)) s.hidden = take((size_t)a.rows * s.pitch * 2);
     if (!tma_ready(a.weight, a.weight_stride)) s.weight = take((size_t)a.n_tokens * s.pitch * 2);
     if (!grad) {
-        s.part_pitch = ceil_div(a.n_tokens, kTileN) * (kTileN / kFoldColumns);
+        s.logits = logits_shape(env, a.rows, a.n_tokens, s.pitch % 64 != 0);
+        s.part_pitch = ceil_div(a.n_tokens, shape_n(s.logits)) * (kFoldWarps / 4);
         s.part = take((size_t)a.rows * s.part_pitch * sizeof(float2));
         s.target_logit = take((size_t)a.rows * 4);
     } else {
         s.coef = take((size_t)a.rows * 4);
         s.scale = take(4);
-        const int64_t most = std::max<int64_t>(kTileN, kGradBytes / 2 / a.rows / kTileN * kTileN);
+        const int64_t most = std::max<int64_t>(kWideN, kGradBytes / 2 / a.rows / kWideN * kWideN);
         const int pieces = ceil_div(a.n_tokens, most);
-        s.piece = ceil_div(ceil_div(a.n_tokens, pieces), kTileN) * kTileN;
+        s.piece = ceil_div(ceil_div(a.n_tokens, pieces), kWideN) * kWideN;
+        s.logits = logits_shape(env, a.rows, s.piece, s.pitch % 64 != 0);
         s.grad = take((size_t)a.rows * s.piece * 2);
+        s.sums = a.rows > kRowsM ? kPair : kWide;
         // few tiles: their sums are split, each part into a plane of its own
-        const int tile_m = s.pair ? Tile<true>::kM : Tile<false>::kM;
-        const int64_t tiles = (int64_t)ceil_div(a.rows, tile_m) * ceil_div(a.dim, kTileN);
-        s.splits = (int)std::max<int64_t>(1, std::min<int64_t>(env.num_sms / (s.pair ? 2 : 1) / tiles, s.piece / kTileK / 4));
-        s.plane_rows = ceil_div(a.rows, tile_m) * tile_m;
+        const int64_t tiles = (int64_t)ceil_div(a.rows, shape_m(s.sums)) * ceil_div(a.dim, kWideN);
+        s.splits = (int)std::max<int64_t>(1, std::min<int64_t>(env.num_sms / (s.sums == kPair ? 2 : 1) / tiles, s.piece / kTileK / 4));
+        s.plane_rows = ceil_div(a.rows, shape_m(s.sums)) * shape_m(s.sums);
         s.planes = take((size_t)s.splits * s.plane_rows * s.pitch * 4);
     }
     s.end = at;
     return s;
 }
 
+// The weight (and without a gradient the hidden rows) as TMA can read it: in place, or to be laid out by `prep`.
+struct Operand {
+    const void* p;
+    int64_t stride;
+};
+Operand operand(Pack& pack, const void* p, int64_t stride, int32_t rows, int32_t cols, void* to, int64_t pitch, bool always) {
+    const bool ready = tma_ready(p, stride);
+    if (ready && !always) return {p, stride};
+    pack = Pack{(const __nv_bfloat16*)p, stride, rows, cols, (__nv_bfloat16*)to, pitch, ready};
+    return {to, pitch};
+}
+
 }  // namespace
 
-size_t loss_workspace(const LossArgs& a, const LaunchEnv& env, bool grad) { return loss_space(a, env, grad).end; }
+size_t loss_workspace(const LossArgs& a, const LaunchEnv& env, bool grad) {
+    return a.rows <= kFewRows ? few_workspace(a, env, grad) : loss_space(a, env, grad).end;
+}
+
+cudaError_t launch_loss_merge(const LossArgs& a, const float2* part, int32_t parts, const float* target_logit,
+                              cudaStream_t st) {
+    return launch_pdl(loss_kernel, dim3((unsigned)ceil_div(a.rows, kMergeThreads / 32)), dim3(kMergeThreads), 0, st, part,
+                      parts, parts, target_logit, a.targets, a.mask, a.rows, a.n_tokens, a.loss, a.lse, a.err);
+}
 
 bool loss_fits(const LossArgs& a) {
     // tiles are counted in 32 bits
-    return (int64_t)ceil_div(a.rows, kRowsM) * ceil_div(std::max(a.n_tokens, a.dim), kTileN) < ((int64_t)1 << 28);
+    return (int64_t)ceil_div(a.rows, kRowsM) * ceil_div(std::max(a.n_tokens, a.dim), kNarrowN) < ((int64_t)1 << 28);
 }
 
 cudaError_t launch_token_loss(const LossArgs& a, const LaunchEnv& env, void* space, cudaStream_t st) {
+    if (a.rows <= kFewRows) return launch_few_loss(a, env, space, st);
     const LossSpace s = loss_space(a, env, false);
     char* ws = (char*)space;
+    Prep prep{};
+    const Operand h = operand(prep.pack[0], a.hidden, a.hidden_stride, a.rows, a.dim, ws + s.hidden, s.pitch, false);
+    const Operand w = operand(prep.pack[1], a.weight, a.weight_stride, a.n_tokens, a.dim, ws + s.weight, s.pitch, false);
     cudaError_t e = cudaSuccess;
-    const void *h = a.hidden, *w = a.weight;
-    int64_t hs = a.hidden_stride, wst = a.weight_stride;
-    if (!tma_ready(h, hs)) {
-        e = launch_pack(env, h, hs, a.rows, a.dim, ws + s.hidden, s.pitch, nullptr, st);
-        h = ws + s.hidden;
-        hs = s.pitch;
-    }
-    if (e == cudaSuccess && !tma_ready(w, wst)) {
-        e = launch_pack(env, w, wst, a.n_tokens, a.dim, ws + s.weight, s.pitch, nullptr, st);
-        w = ws + s.weight;
-        wst = s.pitch;
-    }
+    if (prep.pack[0].rows || prep.pack[1].rows) e = launch_prep(env, prep, st);
     if (e != cudaSuccess) return e;
     Product p{};
-    if ((e = make_map(&p.a, h, a.rows, a.dim, hs, kRowsM)) != cudaSuccess) return e;
-    if ((e = make_map(&p.b, w, a.n_tokens, a.dim, wst, s.pair ? kTileN / 2 : kTileN)) != cudaSuccess) return e;
-    cut_product(p, s.pair, a.rows, a.n_tokens, a.dim, 1);
+    if ((e = make_map(&p.a, h.p, a.rows, a.dim, h.stride, kRowsM)) != cudaSuccess) return e;
+    if ((e = make_map(&p.b, w.p, a.n_tokens, a.dim, w.stride, shape_box(s.logits))) != cudaSuccess) return e;
+    cut_product(p, s.logits, a.rows, a.n_tokens, a.dim, 1);
     p.mask = a.mask;
     p.mask_words = (a.n_tokens + 31) / 32;
     p.targets = a.targets;
@@ -737,64 +848,60 @@ cudaError_t launch_token_loss(const LossArgs& a, const LaunchEnv& env, void* spa
     p.part_pitch = s.part_pitch;
     p.target_logit = (float*)(ws + s.target_logit);
     p.err = a.err;
-    if ((e = launch_product<kFoldLogSum>(env, s.pair, p, st)) != cudaSuccess) return e;
-    return launch_pdl(loss_kernel, dim3((unsigned)ceil_div(a.rows, kMergeThreads / 32)), dim3(kMergeThreads), 0, st,
-                      (const float2*)p.part, s.part_pitch, s.part_pitch, (const float*)p.target_logit, a.targets, a.mask,
-                      a.rows, a.n_tokens, a.loss, a.lse, a.err);
+    if ((e = launch_product<kFoldLogSum>(env, s.logits, p, st)) != cudaSuccess) return e;
+    return launch_loss_merge(a, p.part, s.part_pitch, p.target_logit, st);
 }
 
 cudaError_t launch_token_loss_grad(const LossArgs& a, const LaunchEnv& env, void* space, cudaStream_t st) {
+    if (a.rows <= kFewRows) return launch_few_loss_grad(a, env, space, st);
     const LossSpace s = loss_space(a, env, true);
     char* ws = (char*)space;
-    float* coef = (float*)(ws + s.coef);
-    float* scale = (float*)(ws + s.scale);
-    cudaError_t e = launch_pdl(coef_kernel, dim3(1), dim3(kCoefThreads), 0, st, a.targets, a.mask, a.grad_loss, a.rows,
-                               a.n_tokens, coef, scale, a.err);
+    Prep prep{};
+    const Operand h = operand(prep.pack[0], a.hidden, a.hidden_stride, a.rows, a.dim, ws + s.hidden, s.pitch, true);
+    const Operand w = operand(prep.pack[1], a.weight, a.weight_stride, a.n_tokens, a.dim, ws + s.weight, s.pitch, false);
+    prep.grad = true;
+    prep.targets = a.targets;
+    prep.mask = a.mask;
+    prep.grad_loss = a.grad_loss;
+    prep.rows = a.rows;
+    prep.n_tokens = a.n_tokens;
+    prep.coef = (float*)(ws + s.coef);
+    prep.scale = (float*)(ws + s.scale);
+    prep.err = a.err;
+    cudaError_t e = launch_prep(env, prep, st);
     if (e != cudaSuccess) return e;
-    if ((e = launch_pack(env, a.hidden, a.hidden_stride, a.rows, a.dim, ws + s.hidden, s.pitch, coef, st)) != cudaSuccess)
-        return e;
-    const void* h = ws + s.hidden;
-    const char* w = (const char*)a.weight;
-    int64_t wst = a.weight_stride;
-    if (!tma_ready(w, wst)) {
-        e = launch_pack(env, w, wst, a.n_tokens, a.dim, ws + s.weight, s.pitch, nullptr, st);
-        if (e != cudaSuccess) return e;
-        w = ws + s.weight;
-        wst = s.pitch;
-    }
-    const int64_t words = (a.n_tokens + 31) / 32;
     for (int32_t v0 = 0; v0 < a.n_tokens; v0 += s.piece) {
-        const int32_t n = std::min(s.piece, a.n_tokens - v0), width = ceil_div(n, kTileN) * kTileN;
-        const char* wp = w + (int64_t)v0 * wst * 2;
+        const int32_t n = std::min(s.piece, a.n_tokens - v0), width = ceil_div(n, kWideN) * kWideN;
+        const char* wp = (const char*)w.p + (int64_t)v0 * w.stride * 2;
         Product g{};   // G of the piece, [rows][width]
-        if ((e = make_map(&g.a, h, a.rows, a.dim, s.pitch, kRowsM)) != cudaSuccess) return e;
-        if ((e = make_map(&g.b, wp, n, a.dim, wst, s.pair ? kTileN / 2 : kTileN)) != cudaSuccess) return e;
-        cut_product(g, s.pair, a.rows, n, a.dim, 1);
+        if ((e = make_map(&g.a, h.p, a.rows, a.dim, h.stride, kRowsM)) != cudaSuccess) return e;
+        if ((e = make_map(&g.b, wp, n, a.dim, w.stride, shape_box(s.logits))) != cudaSuccess) return e;
+        cut_product(g, s.logits, a.rows, n, a.dim, 1);
         g.mask = a.mask ? a.mask + v0 / 32 : nullptr;
-        g.mask_words = words;
+        g.mask_words = (a.n_tokens + 31) / 32;
         g.targets = a.targets;
         g.column0 = v0;
         g.lse = a.lse;
-        g.coef = coef;
+        g.coef = prep.coef;
         if ((e = make_out_map(&g.to, ws + s.grad, a.rows, width, width)) != cudaSuccess) return e;
         g.err = a.err;
-        if ((e = launch_product<kFoldGrad>(env, s.pair, g, st)) != cudaSuccess) return e;
+        if ((e = launch_product<kFoldGrad>(env, s.logits, g, st)) != cudaSuccess) return e;
         Product d{};   // its part of the hidden gradient
         if ((e = make_map(&d.a, ws + s.grad, a.rows, width, width, kRowsM)) != cudaSuccess) return e;
-        if ((e = make_map(&d.b, wp, n, a.dim, wst, 64)) != cudaSuccess) return e;
-        cut_product(d, s.pair, a.rows, a.dim, n, s.splits);
+        if ((e = make_map(&d.b, wp, n, a.dim, w.stride, 64)) != cudaSuccess) return e;
+        cut_product(d, s.sums, a.rows, a.dim, n, s.splits);
         d.b_mn = 1;
         d.plane_rows = s.plane_rows;
         e = make_plane_map(&d.to, ws + s.planes, (int64_t)s.splits * s.plane_rows, a.dim, s.pitch);
         if (e != cudaSuccess) return e;
         d.add = v0 > 0;
         d.err = a.err;
-        if ((e = launch_product<kFoldHidden>(env, s.pair, d, st)) != cudaSuccess) return e;
-        const bool pair_w = n > kRowsM;
+        if ((e = launch_product<kFoldHidden>(env, s.sums, d, st)) != cudaSuccess) return e;
+        const Shape shape_w = n > kRowsM ? kPair : kWide;
         Product g2{};   // the piece's rows of the weight's gradient
         if ((e = make_map(&g2.a, ws + s.grad, a.rows, width, width, 64)) != cudaSuccess) return e;
-        if ((e = make_map(&g2.b, h, a.rows, a.dim, s.pitch, 64)) != cudaSuccess) return e;
-        cut_product(g2, pair_w, n, a.dim, a.rows, 1);
+        if ((e = make_map(&g2.b, h.p, a.rows, a.dim, h.stride, 64)) != cudaSuccess) return e;
+        cut_product(g2, shape_w, n, a.dim, a.rows, 1);
         g2.a_mn = g2.b_mn = 1;
         __nv_bfloat16* rows = (__nv_bfloat16*)a.dweight + (int64_t)v0 * a.dweight_stride;
         if (tma_ready(a.dweight, a.dweight_stride)) {
@@ -803,14 +910,16 @@ cudaError_t launch_token_loss_grad(const LossArgs& a, const LaunchEnv& env, void
             g2.out = rows;
             g2.ld = a.dweight_stride;
         }
-        g2.scale = scale;
+        g2.scale = prep.scale;
         g2.err = a.err;
-        if ((e = launch_product<kFoldWeight>(env, pair_w, g2, st)) != cudaSuccess) return e;
+        if ((e = launch_product<kFoldWeight>(env, shape_w, g2, st)) != cudaSuccess) return e;
     }
+    const int parts = s.splits >= 8 ? 8 : 1;
     const int64_t cells = (int64_t)a.rows * (s.pitch / 4);
-    return launch_pdl(dhidden_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(cells, kPackThreads), env.num_sms * 8)),
+    return launch_pdl(parts > 1 ? dhidden_kernel<8> : dhidden_kernel<1>,
+                      dim3((unsigned)std::min<int64_t>(ceil_div(cells, kPackThreads / parts), env.num_sms * 8)),
                       dim3(kPackThreads), 0, st, (const float*)(ws + s.planes), s.splits, (int64_t)s.plane_rows * s.pitch, a.rows,
-                      a.dim, (int32_t)s.pitch, (const float*)scale, (__nv_bfloat16*)a.dhidden, a.dhidden_stride);
+                      a.dim, (int32_t)s.pitch, (const float*)prep.scale, (__nv_bfloat16*)a.dhidden, a.dhidden_stride);
 }
 
 }  // namespace domino

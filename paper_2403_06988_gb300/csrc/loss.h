@@ -26,6 +26,14 @@ bool loss_fits(const LossArgs& a);
 size_t loss_workspace(const LossArgs& a, const LaunchEnv& env, bool grad);
 cudaError_t launch_token_loss(const LossArgs& a, const LaunchEnv& env, void* space, cudaStream_t st);
 cudaError_t launch_token_loss_grad(const LossArgs& a, const LaunchEnv& env, void* space, cudaStream_t st);
+// Up to kFewRows rows (loss_few.cu).
+constexpr int kFewRows = 4;
+size_t few_workspace(const LossArgs& a, const LaunchEnv& env, bool grad);
+cudaError_t launch_few_loss(const LossArgs& a, const LaunchEnv& env, void* space, cudaStream_t st);
+cudaError_t launch_few_loss_grad(const LossArgs& a, const LaunchEnv& env, void* space, cudaStream_t st);
+// Rows' partials (max, sum of exp against it), `parts` each, into loss and lse.
+cudaError_t launch_loss_merge(const LossArgs& a, const float2* part, int32_t parts, const float* target_logit,
+                              cudaStream_t st);
 
 // Divergence of a teacher's top logits from the masked softmax of a row.
 struct DistillArgs {
