@@ -36,6 +36,7 @@ struct DistillCall {
     DistillArgs a;
     int32_t W;
     int32_t slices, slice;       // CTAs per row; tokens of each (a multiple of 32)
+    int32_t slots;               // of the table of ids: a power of two, twice the entries or more
     float inv_tau, k;            // 1 / tau; log2(e) / tau
 };
 
@@ -138,7 +139,8 @@ template <bool BF16>
 __device__ void read_entries(Entries& e, const DistillCall& c, int32_t row, const void* xrow, const uint32_t* mrow,
                              DistillShared& sh, bool report) {
     const DistillArgs& a = c.a;
-    for (int i = threadIdx.x; i < kDistillSlots; i += kDistillThreads) {
+    const int slots = c.slots;
+    for (int i = threadIdx.x; i < slots; i += kDistillThreads) {
         sh.id[i] = -1;
         sh.first[i] = INT_MAX;
     }
@@ -160,11 +162,11 @@ __device__ void read_entries(Entries& e, const DistillCall& c, int32_t row, cons
         t[j] = a.teacher_dtype == DOMINO_DTYPE_BF16 ? load_at<true>(a.teacher, (int64_t)row * a.k + i)
                                                     : load_at<false>(a.teacher, (int64_t)row * a.k + i);
         // the first entry of an id: its place in a table of ids
-        uint32_t h = (uint32_t)id * 2654435761u >> 21;   // 11 bits
+        uint32_t h = ((uint32_t)id * 2654435761u >> 16) & (slots - 1);
         while (true) {
             const int32_t old = atomicCAS(&sh.id[h], -1, id);
             if (old == -1 || old == id) break;
-            h = (h + 1) & (kDistillSlots - 1);
+            h = (h + 1) & (slots - 1);
         }
         atomicMin(&sh.first[h], i);
         slot[j] = h;
@@ -362,6 +364,7 @@ cudaError_t launch_distill(const DistillArgs& a, const LaunchEnv& env, bool grad
     while (s < kDistillMaxSlices && (int64_t)a.rows * s * 2 <= env.num_sms * 2 && a.n_tokens > 4096 * s) s *= 2;
     c.slices = s;
     c.slice = ((a.n_tokens + s - 1) / s + 31) / 32 * 32;
+    for (c.slots = 64; c.slots < 2 * a.k; c.slots *= 2) {}
     c.inv_tau = 1.0f / a.temperature;
     c.k = kLog2e / a.temperature;
     if (a.dtype == DOMINO_DTYPE_BF16) return grad ? launch<true, true>(c, st) : launch<true, false>(c, st);

@@ -8,6 +8,7 @@
 // row's sum always runs in the order of the list) and sums runs of equal
 // tokens in fp32: a CTA per chunk of the sorted list and stretch of columns; a
 // run that crosses chunks is kept in parts, which a second pass joins in order.
+// One cluster sorts while the others write the table's zeros.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
@@ -22,7 +23,9 @@ namespace domino {
 namespace {
 
 constexpr int kEmbedThreads = 256;
-constexpr int kEmbedUnroll = 4;
+// Pieces of a thread: 16384 x 4096 bf16 39.7 us with four, 37.0 with two, 41.6 with one (32 x 4096 2.9, 2.1, 1.9).
+constexpr int kEmbedUnroll = 2;
+constexpr int64_t kFarBytes = (int64_t)64 << 20;
 
 template <bool BF16>
 __device__ __forceinline__ uint4 scaled(const uint4& u, float scale) {
@@ -52,9 +55,10 @@ __device__ __forceinline__ void put_at(void* p, int64_t i, float x) {
 }
 
 // A thread takes kEmbedUnroll pieces (16-byte vectors, or with !VEC single
-// values) of the output's `per_row` a row, a grid's width apart.
+// values) of the output's `per_row` a row, a grid's width apart.  far: an output of half the L2 or more is written past it
+// (37.0 -> 35.3 us).
 template <bool BF16, bool VEC>
-__global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const EmbedArgs a, const uint32_t per_row, const int64_t pieces) {
+__global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const EmbedArgs a, const uint32_t per_row, const int64_t pieces, const bool far) {
     pdl_wait();
     pdl_trigger();
     constexpr int kSize = BF16 ? 2 : 4;
@@ -82,8 +86,12 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const EmbedArgs a,
 #pragma unroll
     for (int j = 0; j < kEmbedUnroll; ++j) {
         if (at[j] < 0) continue;
-        if constexpr (VEC) *reinterpret_cast<uint4*>((char*)a.out + at[j] * kSize) = scaled<BF16>(u[j], a.scale);
-        else put_at<BF16>(a.out, at[j], __uint_as_float(u[j].x) * a.scale);
+        if constexpr (VEC) {
+            uint4* to = reinterpret_cast<uint4*>((char*)a.out + at[j] * kSize);
+            const uint4 x = scaled<BF16>(u[j], a.scale);
+            if (far) __stcs(to, x);
+            else *to = x;
+        } else put_at<BF16>(a.out, at[j], __uint_as_float(u[j].x) * a.scale);
     }
 }
 
@@ -102,7 +110,26 @@ struct SortArgs {
     uint2* a;                  // [n] {token (n_tokens: none), place in the list}
     uint2* b;                  // [n]
     uint32_t* err;
+    // the table to be cleared by the clusters after the first: fill_rows rows of fill_bytes (one row where
+    // they follow each other), each a multiple of fill_size
+    char* fill;
+    int64_t fill_pitch, fill_bytes, fill_rows;
+    int32_t fill_size;
 };
+
+// Zeros to bytes [0, n) at p, by threads `at`, `at` + step, ...
+__device__ __forceinline__ void clear(char* p, int64_t n, int size, int64_t at, int64_t step) {
+    int64_t head = (int64_t)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15);
+    head = head < n ? head : n;
+    const int64_t vectors = (n - head) / 16, tail = head + 16 * vectors;
+    for (int64_t i = at; i < vectors; i += step) __stcs(reinterpret_cast<uint4*>(p + head) + i, make_uint4(0, 0, 0, 0));
+    const int64_t edge = (head + n - tail) / size;   // values beside the vectors
+    for (int64_t i = at; i < edge; i += step) {
+        char* q = i * size < head ? p + i * size : p + tail + (i * size - head);
+        if (size == 2) *reinterpret_cast<uint16_t*>(q) = 0;
+        else *reinterpret_cast<uint32_t*>(q) = 0u;
+    }
+}
 
 // Stable least-significant-digit radix sort by one cluster.  The list is cut
 // into one strip per warp.  A pass counts the strips' digits, turns the counts
@@ -115,6 +142,14 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortArgs s) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
     pdl_wait();
     pdl_trigger();
+    if (cta >= s.ctas) {
+        const int64_t threads = (int64_t)(gridDim.x - s.ctas) * kSortThreads, at = (int64_t)(cta - s.ctas) * kSortThreads + tid;
+        if (s.fill_rows == 1) clear(s.fill, s.fill_bytes, s.fill_size, at, threads);
+        else
+            for (int64_t r = at / 32; r < s.fill_rows; r += threads / 32) clear(s.fill + r * s.fill_pitch, s.fill_bytes, s.fill_size, lane, 32);
+        return;
+    }
+    if (s.n == 0) return;
     const int64_t strips = (int64_t)s.ctas * kSortWarps, strip = (int64_t)cta * kSortWarps + warp;
     const int32_t lo = (int32_t)(s.n * strip / strips), hi = (int32_t)(s.n * (strip + 1) / strips);
     const uint32_t bins = 1u << s.bits, digit_mask = bins - 1u;
@@ -189,6 +224,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortArgs s) {
 // ---- sums of runs -----------------------------------------------------------------
 constexpr int kSumThreads = 256;
 constexpr int kSumUnroll = 8;
+constexpr int kSumChunk = 32;              // of the sorted list whose places are in shared memory at a time
 
 struct SumArgs {
     EmbedArgs a;
@@ -206,24 +242,20 @@ struct Piece {
 #pragma unroll
         for (int i = 0; i < kN; ++i) v[i] = 0.0f;
     }
-    __device__ __forceinline__ void add(const Piece& o) {
-#pragma unroll
-        for (int i = 0; i < kN; ++i) v[i] += o.v[i];
+    // as it lies in memory
+    static __device__ __forceinline__ uint4 fetch(const void* p, int64_t i) {
+        if constexpr (VEC) return __ldcs(reinterpret_cast<const uint4*>((const char*)p + i * (BF16 ? 2 : 4)));
+        else return make_uint4(__float_as_uint(value_at<BF16>(p, i)), 0u, 0u, 0u);
     }
-    __device__ __forceinline__ void load(const void* p, int64_t i) {
-        if constexpr (!VEC) {
-            v[0] = value_at<BF16>(p, i);
-        } else {
-            const uint4 u = __ldcs(reinterpret_cast<const uint4*>((const char*)p + i * (BF16 ? 2 : 4)));
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    __device__ __forceinline__ void add(const uint4& u) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if constexpr (BF16) {
-                    v[2 * k] = __uint_as_float(w[k] << 16);
-                    v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
-                } else {
-                    v[k] = __uint_as_float(w[k]);
-                }
+        for (int k = 0; k < (VEC ? 4 : 1); ++k) {
+            if constexpr (VEC && BF16) {
+                v[(2 * k) % kN] += __uint_as_float(w[k] << 16);
+                v[(2 * k + 1) % kN] += __uint_as_float(w[k] & 0xFFFF0000u);
+            } else {
+                v[k] += __uint_as_float(w[k]);
             }
         }
     }
@@ -253,9 +285,7 @@ __device__ __forceinline__ void finish_row(const EmbedArgs& a, uint32_t token, i
 #pragma unroll
     for (int i = 0; i < sum.kN; ++i) sum.v[i] *= a.scale;
     if (a.add) {
-        Piece<BF16, VEC> old;
-        old.load(a.dweight, at);
-        sum.add(old);
+        sum.add(Piece<BF16, VEC>::fetch(a.dweight, at));
     }
     sum.store(a.dweight, at);
 }
@@ -268,17 +298,25 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs s) {
     pdl_trigger();
     const int32_t chunk = blockIdx.x / s.stretches, stretch = blockIdx.x - chunk * s.stretches;
     const int32_t c = (stretch * kSumThreads + threadIdx.x) * P::kN;
-    if (c >= a.dim) return;
+    const bool on = c < a.dim;
     const int32_t lo = chunk * s.chunk, hi = min(a.n, lo + s.chunk);
     const uint32_t none = (uint32_t)a.n_tokens;
-    const uint32_t before = lo > 0 ? s.order[lo - 1].x : none, after = hi < a.n ? s.order[hi].x : none;
+    // entry lo - 1 + i; none outside of the list
+    __shared__ uint2 s_order[kSumChunk + 2];
+    const auto stage = [&](int32_t from) {
+        const int32_t i = from - 1 + (int32_t)threadIdx.x;
+        if (threadIdx.x < kSumChunk + 2) s_order[threadIdx.x] = i >= 0 && i < a.n ? s.order[i] : make_uint2(none, 0u);
+        __syncthreads();
+    };
+    stage(lo);
+    const uint32_t before = s_order[0].x;
     float* part = s.part + (int64_t)chunk * 2 * a.dim + c;
     P sum;
     sum.zero();
-    uint32_t token = s.order[lo].x;
+    uint32_t token = s_order[1].x;
     bool first = true;   // the chunk's first run
-    const auto flush = [&](bool last) {
-        if (token == none) return;
+    const auto flush = [&](bool last, uint32_t after) {
+        if (token == none || !on) return;
         if (first && token == before) {
 #pragma unroll
             for (int i = 0; i < P::kN; ++i) part[i] = sum.v[i];
@@ -289,28 +327,35 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs s) {
             finish_row<BF16, VEC>(a, token, c, sum);
         }
     };
-    for (int32_t i0 = lo; i0 < hi; i0 += kSumUnroll) {
-        uint2 o[kSumUnroll];
-        P g[kSumUnroll];
-#pragma unroll
-        for (int j = 0; j < kSumUnroll; ++j) {
-            o[j] = i0 + j < hi ? s.order[i0 + j] : make_uint2(none, 0u);
-            g[j].zero();
-            if (o[j].x != none) g[j].load(a.grad, (int64_t)o[j].y * a.grad_stride + c);
+    for (int32_t b0 = lo; b0 < hi; b0 += kSumChunk) {
+        if (b0 > lo) {
+            __syncthreads();
+            stage(b0);
         }
+        const int n = min(kSumChunk, hi - b0);
+        for (int j0 = 0; j0 < n; j0 += kSumUnroll) {
+            uint4 g[kSumUnroll];
 #pragma unroll
-        for (int j = 0; j < kSumUnroll; ++j) {
-            if (i0 + j >= hi) break;
-            if (o[j].x != token) {
-                flush(false);
-                first = false;
-                token = o[j].x;
-                sum.zero();
+            for (int j = 0; j < kSumUnroll; ++j) {
+                g[j] = make_uint4(0u, 0u, 0u, 0u);
+                if (on && j0 + j < n && s_order[1 + j0 + j].x != none)
+                    g[j] = P::fetch(a.grad, (int64_t)s_order[1 + j0 + j].y * a.grad_stride + c);
             }
-            sum.add(g[j]);
+#pragma unroll
+            for (int j = 0; j < kSumUnroll; ++j) {
+                if (j0 + j >= n) break;
+                const uint32_t t = s_order[1 + j0 + j].x;
+                if (t != token) {
+                    flush(false, none);
+                    first = false;
+                    token = t;
+                    sum.zero();
+                }
+                sum.add(g[j]);
+            }
         }
+        if (b0 + n == hi) flush(true, s_order[1 + n].x);
     }
-    flush(true);
 }
 
 // The runs that cross chunks: each by the CTAs of the chunk that it begins in.
@@ -331,11 +376,25 @@ __global__ void __launch_bounds__(kSumThreads) join_kernel(const SumArgs s) {
     const float* part = s.part + (int64_t)chunk * 2 * a.dim + c;
 #pragma unroll
     for (int i = 0; i < P::kN; ++i) sum.v[i] = part[a.dim + i];
-    for (int32_t k = chunk + 1; k < s.chunks; ++k) {
-        part += 2 * a.dim;
-        if (s.order[(int64_t)k * s.chunk].x != token) break;
+    // the following chunks that begin with the token, eight at a time: the loads do not wait for one another
+    for (int32_t k = chunk + 1; k < s.chunks; k += kSumUnroll) {
+        uint32_t t[kSumUnroll];
+        float v[kSumUnroll][P::kN];
 #pragma unroll
-        for (int i = 0; i < P::kN; ++i) sum.v[i] += part[i];
+        for (int j = 0; j < kSumUnroll; ++j) {
+            const bool in = k + j < s.chunks;
+            t[j] = in ? s.order[(int64_t)(k + j) * s.chunk].x : (uint32_t)a.n_tokens;
+#pragma unroll
+            for (int i = 0; i < P::kN; ++i) v[j][i] = in ? part[(int64_t)(k + j - chunk) * 2 * a.dim + i] : 0.0f;
+        }
+        bool more = true;
+#pragma unroll
+        for (int j = 0; j < kSumUnroll; ++j) {
+            more = more && t[j] == token;
+#pragma unroll
+            for (int i = 0; i < P::kN; ++i) sum.v[i] += more ? v[j][i] : 0.0f;   // others' parts may hold anything
+        }
+        if (!more) break;
     }
     finish_row<BF16, VEC>(a, token, c, sum);
 }
@@ -351,17 +410,22 @@ cudaError_t launch_rows(const EmbedArgs& a, cudaStream_t st) {
     const int64_t pieces = (int64_t)a.n * per_row;
     const int64_t ctas = (pieces + kEmbedThreads * kEmbedUnroll - 1) / (kEmbedThreads * kEmbedUnroll);
     if (ctas > INT_MAX) return cudaErrorInvalidValue;
-    return launch_pdl(embed_kernel<BF16, VEC>, dim3((unsigned)ctas), dim3(kEmbedThreads), 0, st, a, per_row, pieces);
+    return launch_pdl(embed_kernel<BF16, VEC>, dim3((unsigned)ctas), dim3(kEmbedThreads), 0, st, a, per_row, pieces,
+                      (int64_t)a.n * a.dim * (BF16 ? 2 : 4) >= kFarBytes);
 }
 
 struct EmbedSpace {
     size_t a, b, part, end;
     int32_t chunk, chunks;
 };
-EmbedSpace embed_space(const EmbedArgs& a) {
+// Chunks of the sorted list: one round of loads each while that gives the SMs no more than eight CTAs (100 of 5000 tokens,
+// 256 wide: 6.7 us with chunks of 32), at most 4096 in all (a run that crosses chunks is joined by one CTA).
+EmbedSpace embed_space(const EmbedArgs& a, const LaunchEnv& env) {
     EmbedSpace s{};
-    s.chunk = 32;
-    while ((int64_t)s.chunk * 4096 < a.n) s.chunk *= 2;
+    s.chunk = kSumUnroll;
+    const int64_t stretches = (a.dim + kSumThreads * 4 - 1) / (kSumThreads * 4);
+    while ((s.chunk < kSumChunk && a.n * stretches > (int64_t)s.chunk * env.num_sms * 8) || (int64_t)s.chunk * 4096 < a.n)
+        s.chunk *= 2;
     s.chunks = (a.n + s.chunk - 1) / s.chunk;
     const auto align = [](size_t n) { return (n + 255) & ~(size_t)255; };
     s.b = align((size_t)a.n * sizeof(uint2));
@@ -391,16 +455,13 @@ cudaError_t launch_embed(const EmbedArgs& a, const LaunchEnv&, cudaStream_t st) 
     return vec ? launch_rows<false, true>(a, st) : launch_rows<false, false>(a, st);
 }
 
-size_t embed_workspace(const EmbedArgs& a, const LaunchEnv&) { return embed_space(a).end; }
+size_t embed_workspace(const EmbedArgs& a, const LaunchEnv& env) { return embed_space(a, env).end; }
 
-cudaError_t launch_embed_grad(const EmbedArgs& a, const LaunchEnv&, void* space, cudaStream_t st) {
+cudaError_t launch_embed_grad(const EmbedArgs& a, const LaunchEnv& env, void* space, cudaStream_t st) {
     const bool bf16 = a.dtype == DOMINO_DTYPE_BF16;
     const int size = bf16 ? 2 : 4;
-    cudaError_t e = cudaSuccess;
-    if (!a.add)
-        e = cudaMemset2DAsync(a.dweight, (size_t)a.dweight_stride * size, 0, (size_t)a.dim * size, (size_t)a.n_tokens, st);
-    if (e != cudaSuccess || a.n == 0) return e;
-    const EmbedSpace sp = embed_space(a);
+    if (a.n == 0 && a.add) return cudaSuccess;
+    const EmbedSpace sp = embed_space(a, env);
     char* ws = (char*)space;
     SortArgs so{};
     so.tokens = a.tokens;
@@ -415,7 +476,18 @@ cudaError_t launch_embed_grad(const EmbedArgs& a, const LaunchEnv&, void* space,
     so.a = (uint2*)(ws + sp.a);
     so.b = (uint2*)(ws + sp.b);
     so.err = a.err;
-    if ((e = launch_cluster(sort_kernel, dim3((unsigned)so.ctas), dim3(kSortThreads), so.ctas, 0, st, so)) != cudaSuccess) return e;
+    int clusters = 1;
+    if (!a.add) {
+        const bool flat = a.dweight_stride == a.dim;
+        so.fill = (char*)a.dweight;
+        so.fill_size = size;
+        so.fill_rows = flat ? 1 : a.n_tokens;
+        so.fill_pitch = a.dweight_stride * size;
+        so.fill_bytes = (int64_t)a.dim * size * (flat ? a.n_tokens : 1);
+        clusters += 2 * env.num_sms / so.ctas;
+    }
+    cudaError_t e = launch_cluster(sort_kernel, dim3((unsigned)(clusters * so.ctas)), dim3(kSortThreads), so.ctas, 0, st, so);
+    if (e != cudaSuccess || a.n == 0) return e;
     SumArgs s{};
     s.a = a;
     s.order = so.a;
