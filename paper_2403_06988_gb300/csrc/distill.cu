@@ -17,8 +17,8 @@
 
 #include <algorithm>
 
+#include "decode.cuh"
 #include "loss.h"
-#include "walk_common.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -28,7 +28,10 @@ namespace {
 constexpr int kDistillThreads = 512;
 constexpr int kDistillWarps = kDistillThreads / 32;
 constexpr int kDistillMaxSlices = 8;
-constexpr int kDistillUnroll = 4;
+// Two vectors a thread and four CTAs an SM (us of the loss, and of both; 2048 rows, V = 128256 bf16 / 301 rows, V = 50001, masks): 99,
+// 271 / 12.4, 25.8; four vectors and three CTAs 100, 267 / 15.5, 30.3; one vector 112, 295 / 12.4, 28.2; four and the
+// next four on their way, which leaves room for fewer warps, 190, 358 / 18.0, 31.0.
+constexpr int kDistillCtas = 4, kDistillUnroll = 2;
 constexpr int kDistillSlots = 2 * kDistillMaxK;                        // of the table of ids
 constexpr int kDistillEntries = kDistillMaxK / kDistillThreads;        // a thread's
 
@@ -203,6 +206,34 @@ __device__ void read_entries(Entries& e, const DistillCall& c, int32_t row, cons
         }
 }
 
+__device__ __forceinline__ float2 scale2(float2 a, float b) { return fma2(a, b, 0.0f); }
+
+// The vectors that a thread reads together, and which of their tokens are allowed.
+template <bool BF16>
+struct Batch {
+    uint4 u[kDistillUnroll];
+    uint32_t bits[kDistillUnroll];
+    // vectors n = i, i + kDistillThreads, ... of the slice's, the first at token `head`
+    template <bool KEEP>
+    __device__ __forceinline__ void load(const char* xrow, const uint32_t* mrow, int32_t head, int32_t vectors, int32_t i, bool any) {
+        constexpr int kN = Vec<BF16>::kN;
+#pragma unroll
+        for (int j = 0; j < kDistillUnroll; ++j) {
+            const int32_t n = i + j * kDistillThreads;
+            bits[j] = n < vectors && any ? allowed_bits(mrow, head + n * kN, kN) : 0u;
+            u[j] = make_uint4(0, 0, 0, 0);
+            const uint4* p = reinterpret_cast<const uint4*>(xrow + (int64_t)(head + n * kN) * (BF16 ? 2 : 4));
+            if (bits[j]) u[j] = KEEP ? *p : __ldcs(p);
+        }
+    }
+    __device__ __forceinline__ bool full() const {
+        uint32_t all = bits[0];
+#pragma unroll
+        for (int j = 1; j < kDistillUnroll; ++j) all &= bits[j];
+        return all == (1u << Vec<BF16>::kN) - 1u;
+    }
+};
+
 // Tokens [t0, t1) of a row in vectors on the 16-byte boundaries of `base`:
 // [t0, head) and [tail, t1) lie outside of them.
 struct Cut {
@@ -219,12 +250,13 @@ __device__ __forceinline__ Cut cut_slice(const void* base, int32_t t0, int32_t t
 }
 
 template <bool BF16, bool GRAD>
-__global__ void __launch_bounds__(kDistillThreads) distill_kernel(const __grid_constant__ DistillCall c) {
+__global__ void __launch_bounds__(kDistillThreads, kDistillCtas) distill_kernel(const __grid_constant__ DistillCall c) {
     __shared__ DistillShared sh;
     const DistillArgs& a = c.a;
     constexpr int kN = Vec<BF16>::kN, kSize = BF16 ? 2 : 4;
     const int tid = threadIdx.x;
-    const int32_t row = blockIdx.x / c.slices, slice = blockIdx.x - row * c.slices;
+    // the gradient begins with the rows that the loss has read last: they may still be in L2
+    const int32_t at = blockIdx.x / c.slices, slice = blockIdx.x - at * c.slices, row = GRAD ? a.rows - 1 - at : at;
     pdl_wait();
     pdl_trigger();
     const char* xrow = (const char*)a.logits + (int64_t)row * a.stride * kSize;
@@ -241,33 +273,39 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const __grid_c
         };
         for (int32_t t = t0 + tid; t < cut.head; t += kDistillThreads) fold1(t);
         for (int32_t t = cut.tail + tid; t < t1; t += kDistillThreads) fold1(t);
-        for (int32_t i = tid; i < vectors; i += kDistillThreads * kDistillUnroll) {
-            uint32_t bits[kDistillUnroll];
-            uint4 u[kDistillUnroll];
+        constexpr int32_t kStep = kDistillThreads * kDistillUnroll;
+        for (int32_t i = tid; i < vectors; i += kStep) {
+            Batch<BF16> now;
+            now.template load<true>(xrow, mrow, cut.head, vectors, i, true);
+            Vec<BF16> x[kDistillUnroll];
+            float top = acc.x;
+            const bool full = now.full();
 #pragma unroll
             for (int j = 0; j < kDistillUnroll; ++j) {
-                const int32_t n = i + j * kDistillThreads;
-                bits[j] = n < vectors ? allowed_bits(mrow, cut.head + n * kN, kN) : 0u;
-                u[j] = make_uint4(0, 0, 0, 0);
-                if (bits[j]) u[j] = __ldcs(reinterpret_cast<const uint4*>(xrow + (int64_t)(cut.head + n * kN) * kSize));
-            }
+                x[j].set(now.u[j]);
+                if (!full) {
 #pragma unroll
-            for (int j = 0; j < kDistillUnroll; ++j) {
-                if (!bits[j]) continue;
-                Vec<BF16> x;
-                x.set(u[j]);
-                float top = acc.x;
-#pragma unroll
-                for (int b = 0; b < kN; ++b) {
-                    if (!((bits[j] >> b) & 1u)) x.v[b] = -INFINITY;
-                    top = fmaxf(top, x.v[b]);
+                    for (int b = 0; b < kN; ++b) x[j].v[b] = (now.bits[j] >> b) & 1u ? x[j].v[b] : -INFINITY;
                 }
-                const float ref = sum_ref(top);
-                acc.y *= ex2((acc.x - ref) * c.k);
 #pragma unroll
-                for (int b = 0; b < kN; ++b) acc.y += ex2((x.v[b] - ref) * c.k);
-                acc.x = top;
+                for (int b = 0; b < kN; b += 2) top = fmaxf(fmaxf(top, x[j].v[b]), x[j].v[b + 1]);
             }
+            const float ref = sum_ref(top);
+            const float2 nref = make_float2(-ref, -ref);
+            float2 s0 = make_float2(acc.y * ex2((acc.x - ref) * c.k), 0.0f), s1 = make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int j = 0; j < kDistillUnroll; ++j) {
+                if (now.bits[j] == 0u) continue;
+#pragma unroll
+                for (int b = 0; b < kN; b += 4) {
+                    const float2 d0 = scale2(add2(make_float2(x[j].v[b], x[j].v[b + 1]), nref), c.k);
+                    const float2 d1 = scale2(add2(make_float2(x[j].v[b + 2], x[j].v[b + 3]), nref), c.k);
+                    s0 = add2(s0, make_float2(ex2(d0.x), ex2(d0.y)));
+                    s1 = add2(s1, make_float2(ex2(d1.x), ex2(d1.y)));
+                }
+            }
+            s0 = add2(s0, s1);
+            acc = make_float2(top, s0.x + s0.y);
         }
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1)
@@ -309,7 +347,7 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const __grid_c
         // the entries' logits have been read by every CTA of the row before any is written over
         if (c.slices > 1) cg::this_cluster().sync();
         const float g = e.any ? __ldg(a.grad_loss + row) * a.temperature : 0.0f;
-        const auto grad = [&](float x) { return g * ex2((x * c.inv_tau - lse) * kLog2e); };
+        const auto grad = [&](float x) { return g * ex2(fmaf(x, c.inv_tau, -lse) * kLog2e); };
         const auto grad1 = [&](int32_t t) {
             store_at<BF16>(drow, t, g != 0.0f && allowed_bits(mrow, t, 1) ? grad(load_at<BF16>(xrow, t)) : 0.0f);
         };
@@ -318,25 +356,34 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const __grid_c
         const int32_t head = same ? cut.head : t1, tail = same ? cut.tail : t1;
         for (int32_t t = t0 + tid; t < head; t += kDistillThreads) grad1(t);
         for (int32_t t = tail + tid; t < t1; t += kDistillThreads) grad1(t);
-        for (int32_t i = tid; same && i < vectors; i += kDistillThreads * kDistillUnroll) {
-            uint32_t bits[kDistillUnroll];
-            uint4 u[kDistillUnroll];
-#pragma unroll
-            for (int j = 0; j < kDistillUnroll; ++j) {
-                const int32_t n = i + j * kDistillThreads;
-                bits[j] = n < vectors && g != 0.0f ? allowed_bits(mrow, cut.head + n * kN, kN) : 0u;
-                u[j] = make_uint4(0, 0, 0, 0);
-                if (bits[j]) u[j] = __ldcs(reinterpret_cast<const uint4*>(xrow + (int64_t)(cut.head + n * kN) * kSize));
-            }
+        constexpr int32_t kStep = kDistillThreads * kDistillUnroll;
+        const bool any = g != 0.0f;
+        for (int32_t i = tid; same && i < vectors; i += kStep) {
+            Batch<BF16> now;
+            now.template load<false>(xrow, mrow, cut.head, vectors, i, any);
+            const bool full = now.full();
 #pragma unroll
             for (int j = 0; j < kDistillUnroll; ++j) {
                 const int32_t n = i + j * kDistillThreads;
                 if (n >= vectors) break;
-                Vec<BF16> x;
-                x.set(u[j]);
+                uint4 out = make_uint4(0, 0, 0, 0);
+                if (now.bits[j]) {
+                    Vec<BF16> x;
+                    x.set(now.u[j]);
 #pragma unroll
-                for (int b = 0; b < kN; ++b) x.v[b] = (bits[j] >> b) & 1u ? grad(x.v[b]) : 0.0f;
-                __stcs(reinterpret_cast<uint4*>(drow + (int64_t)(cut.head + n * kN) * kSize), x.get());
+                    for (int b = 0; b < kN; b += 2) {
+                        const float2 d = scale2(fma2(make_float2(x.v[b], x.v[b + 1]), c.inv_tau, -lse), kLog2e);
+                        const float2 q = scale2(make_float2(ex2(d.x), ex2(d.y)), g);
+                        x.v[b] = q.x;
+                        x.v[b + 1] = q.y;
+                    }
+                    if (!full) {
+#pragma unroll
+                        for (int b = 0; b < kN; ++b) x.v[b] = (now.bits[j] >> b) & 1u ? x.v[b] : 0.0f;
+                    }
+                    out = x.get();
+                }
+                __stcs(reinterpret_cast<uint4*>(drow + (int64_t)(cut.head + n * kN) * kSize), out);
             }
         }
         __syncthreads();
@@ -344,7 +391,7 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const __grid_c
 #pragma unroll
         for (int j = 0; j < kDistillEntries; ++j)
             if (e.id[j] >= t0 && e.id[j] < t1 && g != 0.0f)
-                store_at<BF16>(drow, e.id[j], g * (ex2((e.x[j] * c.inv_tau - lse) * kLog2e) - e.p[j]));
+                store_at<BF16>(drow, e.id[j], g * (ex2(fmaf(e.x[j], c.inv_tau, -lse) * kLog2e) - e.p[j]));
     }
 }
 
