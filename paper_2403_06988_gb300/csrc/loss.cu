@@ -401,13 +401,18 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                         put_words(buffer, lane, w);
                         __syncwarp();
                         const uint32_t chunk = (uint32_t)lane >> 3, byte = (lane & 7) * 2;
-                        for (int r = 0; r < 32 && row0 + r < p.m; ++r) {
-                            uint16_t x;
-                            asm volatile("ld.shared.u16 %0, [%1];\n"
-                                         : "=h"(x)
-                                         : "r"(buffer + r * 64 + ((chunk ^ ((r >> 1) & 3)) << 4) + byte)
-                                         : "memory");
-                            if (c + lane < p.n) reinterpret_cast<uint16_t*>(p.out + (int64_t)(row0 + r) * p.ld)[c + lane] = x;
+#pragma unroll
+                        for (int r0 = 0; r0 < 32; r0 += 8) {
+                            uint16_t x[8];
+#pragma unroll
+                            for (int r = r0; r < r0 + 8; ++r)
+                                asm volatile("ld.shared.u16 %0, [%1];\n"
+                                             : "=h"(x[r - r0])
+                                             : "r"(buffer + r * 64 + ((chunk ^ ((r >> 1) & 3)) << 4) + byte));
+#pragma unroll
+                            for (int r = r0; r < r0 + 8; ++r)
+                                if (row0 + r < p.m && c + lane < p.n)
+                                    reinterpret_cast<uint16_t*>(p.out + (int64_t)(row0 + r) * p.ld)[c + lane] = x[r - r0];
                         }
                     }
                 }

@@ -35,26 +35,52 @@ struct FewCall {
     float* g;                             // [rows][n_tokens]
 };
 
-// kN consecutive bf16 of a row as fp32.
-template <bool VEC>
+// Eight consecutive bf16 of a row as fp32, zeros beyond the row's end.  ALIGNED:
+// rows begin on 16-byte boundaries and have whole vectors.  Else they are read in
+// the 16-byte blocks that hold the values, and shifted.
+constexpr int kN = 8;
+template <bool ALIGNED>
 struct Cols {
-    static constexpr int kN = VEC ? 8 : 1;
-    uint4 u;
-    __device__ __forceinline__ void zero() { u = make_uint4(0, 0, 0, 0); }
-    __device__ __forceinline__ void load(const __nv_bfloat16* p) {
-        if constexpr (VEC) u = __ldg(reinterpret_cast<const uint4*>(p));
-        else u.x = (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(p)) << 16;
+    uint4 u, v;
+    uint32_t off, n;
+    __device__ __forceinline__ void zero() {
+        u = v = make_uint4(0, 0, 0, 0);
+        off = 0;
+        n = kN;
+    }
+    // left: values from p to the row's end, at least one
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, int32_t left) {
+        if constexpr (ALIGNED) {
+            u = __ldg(reinterpret_cast<const uint4*>(p));
+        } else {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+            const uint4* block = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
+            off = (uint32_t)(at & 15) / 2;
+            n = (uint32_t)min(left, kN);
+            u = __ldg(block);
+            v = make_uint4(0, 0, 0, 0);
+            if (off + n > kN) v = __ldg(block + 1);
+        }
     }
     __device__ __forceinline__ void get(float (&f)[kN]) const {
-        if constexpr (VEC) {
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+        if constexpr (!ALIGNED) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                f[2 * i] = __uint_as_float(w[i] << 16);
-                f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-            }
-        } else {
-            f[0] = __uint_as_float(u.x);
+            for (int i = 0; i < 6; ++i) w[i] = off & 4 ? w[i + 2] : w[i];
+#pragma unroll
+            for (int i = 0; i < 5; ++i) w[i] = off & 2 ? w[i + 1] : w[i];
+            const uint32_t shift = off & 1 ? 16 : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], shift);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __uint_as_float(w[i] << 16);
+            f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        }
+        if constexpr (!ALIGNED) {
+#pragma unroll
+            for (int i = 0; i < kN; ++i) f[i] = (uint32_t)i < n ? f[i] : 0.0f;
         }
     }
 };
@@ -74,13 +100,11 @@ __device__ __forceinline__ float transpose_sum(float (&acc)[32], int lane) {
 }
 
 // TN rows of tokens (those beyond the call's are not read).  SINGLE: blocks of one token, whose loads are unrolled along
-// the row; else blocks of up to 32 / TN.
-template <int TN, bool SINGLE, bool VEC>
+// the row; else blocks of up to 32 / TN, four weight rows together.
+template <int TN, bool SINGLE, bool ALIGNED>
 __global__ void __launch_bounds__(kFewThreads, 2) few_logits_kernel(const __grid_constant__ FewCall c) {
     constexpr int kR = 32 / TN;                              // lane l: row l / kR, token l % kR of the block
-    constexpr int kRows = SINGLE ? 1 : kR < kFewLoads ? kR : kFewLoads;   // weight rows read together
-    constexpr int kSteps = SINGLE ? kFewLoads : kFewLoads / kRows;
-    constexpr int kN = Cols<VEC>::kN;
+    constexpr int kRows = SINGLE ? 1 : 4, kSteps = (ALIGNED ? kFewLoads : kFewLoads / 2) / kRows;
     __shared__ float2 s_part[kFewWarps][TN];
     const LossArgs& a = c.a;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -118,28 +142,33 @@ __global__ void __launch_bounds__(kFewThreads, 2) few_logits_kernel(const __grid
         for (int r0 = 0; r0 < (SINGLE ? 1 : kR); r0 += kRows) {
             if (!((need >> r0) & ((1u << kRows) - 1u))) continue;
             for (int32_t c0 = lane * kN; c0 < a.dim; c0 += 32 * kN * kSteps) {
-                Cols<VEC> w[kSteps][kRows];
+                Cols<ALIGNED> w[kSteps][kRows];
 #pragma unroll
                 for (int u = 0; u < kSteps; ++u)
 #pragma unroll
                     for (int k = 0; k < kRows; ++k) {
+                        const int32_t at = c0 + u * 32 * kN;
                         w[u][k].zero();
-                        if (c0 + u * 32 * kN < a.dim && ((need >> (r0 + k)) & 1u))
-                            w[u][k].load(weight + (int64_t)(v0 + r0 + k) * a.weight_stride + c0 + u * 32 * kN);
+                        if (at < a.dim && ((need >> (r0 + k)) & 1u))
+                            w[u][k].load(weight + (int64_t)(v0 + r0 + k) * a.weight_stride + at, a.dim - at);
                     }
 #pragma unroll
                 for (int u = 0; u < kSteps; ++u) {
-                    if (c0 + u * 32 * kN >= a.dim) break;
+                    const int32_t at = c0 + u * 32 * kN;
+                    if (at >= a.dim) break;
+                    Cols<ALIGNED> h[TN];
+#pragma unroll
+                    for (int i = 0; i < TN; ++i) {
+                        h[i].zero();
+                        if (i < a.rows) h[i].load(hidden + i * a.hidden_stride + at, a.dim - at);
+                    }
                     float x[kRows][kN];
 #pragma unroll
                     for (int k = 0; k < kRows; ++k) w[u][k].get(x[k]);
 #pragma unroll
                     for (int i = 0; i < TN; ++i) {
-                        if (i >= a.rows) break;
-                        Cols<VEC> hv;
-                        hv.load(hidden + i * a.hidden_stride + c0 + u * 32 * kN);
                         float y[kN];
-                        hv.get(y);
+                        h[i].get(y);
 #pragma unroll
                         for (int k = 0; k < kRows; ++k)
 #pragma unroll
@@ -148,7 +177,20 @@ __global__ void __launch_bounds__(kFewThreads, 2) few_logits_kernel(const __grid
                 }
             }
         }
-        const float x = need ? transpose_sum(acc, lane) : 0.0f;
+        float x = 0.0f;
+        if (need) {
+            if constexpr (SINGLE) {
+#pragma unroll
+                for (int i = 0; i < TN; ++i) {
+                    float s = acc[i * kR];
+#pragma unroll
+                    for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+                    x = t == i ? s : x;
+                }
+            } else {
+                x = transpose_sum(acc, lane);
+            }
+        }
         if (c.grad) {
             if (here) c.g[(int64_t)t * a.n_tokens + v] = ok ? coef * (exp_diff(x, lse) - (v == target ? 1.0f : 0.0f)) : 0.0f;
         } else if (ok) {
@@ -177,45 +219,85 @@ __global__ void __launch_bounds__(kFewThreads, 2) few_logits_kernel(const __grid
 
 constexpr int kSumsThreads = 128;
 constexpr int kSumsTokens = 64;           // whose G lies in shared memory at a time
-constexpr int kSumsLoads = 4;
+constexpr int kSumsLoads = 8;
 
 struct FewSums {
     LossArgs a;
     const float* g;                       // [rows][n_tokens]
     int32_t strip;                        // tokens of a CTA
-    float* planes;                        // [strips][rows][dim]
-    bool vec_out;
+    int32_t pitch;                        // of the planes' rows, a multiple of kN
+    float* planes;                        // [strips][rows][pitch]
+    bool aligned_out;
 };
 
-template <int TN, bool VEC>
+// A warp's 256 consecutive values (eight a lane, `left` of lane 0's to the row's end) to a row of bf16 at any
+// alignment: in the 16-byte blocks that lie in them, each lane's from its own values and the lane's before it, and one
+// by one at the two ends.
+__device__ __forceinline__ void store_any(__nv_bfloat16* to, const uint32_t (&w)[4], int32_t left, int lane) {
+    // to, left: this lane's
+    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(to) & 15) / 2;
+    uint32_t x[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[i] = __shfl_up_sync(0xffffffffu, w[i], 1);
+        x[4 + i] = w[i];
+    }
+    // values 8 - off.. of the 16 are the block at `to` rounded down
+    const uint32_t from = 8 - off;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = from & 8 ? x[i + 4] : x[i];
+#pragma unroll
+    for (int i = 0; i < 6; ++i) x[i] = from & 4 ? x[i + 2] : x[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) x[i] = from & 2 ? x[i + 1] : x[i];
+    const uint32_t shift = from & 1 ? 16 : 0;
+    const uint4 block = make_uint4(__funnelshift_r(x[0], x[1], shift), __funnelshift_r(x[1], x[2], shift),
+                                   __funnelshift_r(x[2], x[3], shift), __funnelshift_r(x[3], x[4], shift));
+    unsigned short* p = reinterpret_cast<unsigned short*>(to);
+    const int32_t n = left < kN ? (left < 0 ? 0 : left) : kN;             // this lane's values
+    const bool whole = (off == 0 || lane > 0) && left >= (int32_t)(kN - off);   // the block ends in the row
+    if (whole) *reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(to) & ~(uintptr_t)15) = block;
+    // beside the blocks: lane 0's first, what the next block would hold of the last lane's or of the row's last values
+    const bool next_whole = lane < 31 && left - kN >= (int32_t)(kN - off) && off > 0;
+#pragma unroll
+    for (int e = 0; e < kN; ++e) {
+        const bool in_mine = e < (int)(kN - off);   // else in the next lane's block
+        const bool one = in_mine ? !whole : !next_whole;
+        if (e < n && one) p[e] = (unsigned short)(w[e / 2] >> (16 * (e & 1)));
+    }
+}
+
+template <int TN, bool ALIGNED>
 __global__ void __launch_bounds__(kSumsThreads) few_sums_kernel(const __grid_constant__ FewSums c) {
-    constexpr int kN = Cols<VEC>::kN;
     __shared__ float s_g[kSumsTokens][TN];
     const LossArgs& a = c.a;
     const __nv_bfloat16* weight = (const __nv_bfloat16*)a.weight;
     __nv_bfloat16* dweight = (__nv_bfloat16*)a.dweight;
     pdl_wait();
     pdl_trigger();
-    const int32_t col = (blockIdx.y * kSumsThreads + threadIdx.x) * kN;
-    const bool on = col < a.dim;
+    const int lane = threadIdx.x & 31;
+    const int32_t col = (blockIdx.y * kSumsThreads + threadIdx.x) * kN, left = a.dim - col;
+    const bool on = left > 0;
     const int32_t lo = blockIdx.x * c.strip, hi = min(a.n_tokens, lo + c.strip);
     // rows without a gradient have no part in dweight, whatever they hold: their G is 0
-    Cols<VEC> h[TN];
-    float acc[TN][kN];
+    float h[TN][kN], acc[TN][kN];
 #pragma unroll
-    for (int i = 0; i < TN; ++i) {
-        h[i].zero();
+    for (int i = 0; i < TN; ++i)
 #pragma unroll
-        for (int e = 0; e < kN; ++e) acc[i][e] = 0.0f;
-    }
+        for (int e = 0; e < kN; ++e) h[i][e] = acc[i][e] = 0.0f;
 #pragma unroll
     for (int i = 0; i < TN; ++i) {
         if (i >= a.rows || !on) break;
         const int32_t y = __ldg(a.targets + i);
         const bool given = y >= 0 && y < a.n_tokens &&
                            (!a.mask || (__ldg(a.mask + (int64_t)i * ((a.n_tokens + 31) / 32) + (y >> 5)) >> (y & 31)) & 1u);
-        if (given && __ldg(a.grad_loss + i) != 0.0f) h[i].load((const __nv_bfloat16*)a.hidden + i * a.hidden_stride + col);
+        if (given && __ldg(a.grad_loss + i) != 0.0f) {
+            Cols<ALIGNED> x;
+            x.load((const __nv_bfloat16*)a.hidden + i * a.hidden_stride + col, left);
+            x.get(h[i]);
+        }
     }
+    constexpr int kLoads = ALIGNED ? kSumsLoads : kSumsLoads / 2;
     for (int32_t v0 = lo; v0 < hi; v0 += kSumsTokens) {
         __syncthreads();
         for (int k = threadIdx.x; k < kSumsTokens * TN; k += kSumsThreads) {
@@ -223,54 +305,51 @@ __global__ void __launch_bounds__(kSumsThreads) few_sums_kernel(const __grid_con
             s_g[v][i] = i < a.rows && v0 + v < hi ? c.g[(int64_t)i * a.n_tokens + v0 + v] : 0.0f;
         }
         __syncthreads();
-        if (!on) continue;
         const int n = min(kSumsTokens, hi - v0);
-        for (int k0 = 0; k0 < n; k0 += kSumsLoads) {
-            Cols<VEC> w[kSumsLoads];
-            bool any[kSumsLoads];
+        for (int k0 = 0; k0 < n; k0 += kLoads) {
+            Cols<ALIGNED> w[kLoads];
+            uint32_t any = 0;
 #pragma unroll
-            for (int j = 0; j < kSumsLoads; ++j) {
-                any[j] = false;
+            for (int j = 0; j < kLoads; ++j) {
                 w[j].zero();
                 if (k0 + j < n) {
+                    bool some = false;
 #pragma unroll
-                    for (int i = 0; i < TN; ++i) any[j] |= s_g[k0 + j][i] != 0.0f;
-                    if (any[j]) w[j].load(weight + (int64_t)(v0 + k0 + j) * a.weight_stride + col);
+                    for (int i = 0; i < TN; ++i) some |= s_g[k0 + j][i] != 0.0f;
+                    any |= (some ? 1u : 0u) << j;
+                    if (some && on) w[j].load(weight + (int64_t)(v0 + k0 + j) * a.weight_stride + col, left);
                 }
             }
 #pragma unroll
-            for (int j = 0; j < kSumsLoads; ++j) {
+            for (int j = 0; j < kLoads; ++j) {
                 if (k0 + j >= n) break;
                 float out[kN];
 #pragma unroll
                 for (int e = 0; e < kN; ++e) out[e] = 0.0f;
-                if (any[j]) {
+                if ((any >> j) & 1u) {
                     float x[kN];
                     w[j].get(x);
 #pragma unroll
                     for (int i = 0; i < TN; ++i) {
                         const float g = s_g[k0 + j][i];
-                        float y[kN];
-                        h[i].get(y);
 #pragma unroll
                         for (int e = 0; e < kN; ++e) {
                             acc[i][e] = fmaf(g, x[e], acc[i][e]);
-                            out[e] = fmaf(g, y[e], out[e]);
+                            out[e] = fmaf(g, h[i][e], out[e]);
                         }
                     }
                 }
+                uint32_t o[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const __nv_bfloat162 p = __floats2bfloat162_rn(out[2 * e], out[2 * e + 1]);
+                    o[e] = *reinterpret_cast<const uint32_t*>(&p);
+                }
                 __nv_bfloat16* to = dweight + (int64_t)(v0 + k0 + j) * a.dweight_stride + col;
-                if (VEC && c.vec_out) {
-                    uint32_t o[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const __nv_bfloat162 p = __floats2bfloat162_rn(out[(2 * e) % kN], out[(2 * e + 1) % kN]);
-                        o[e] = *reinterpret_cast<const uint32_t*>(&p);
-                    }
-                    __stcs(reinterpret_cast<uint4*>(to), make_uint4(o[0], o[1], o[2], o[3]));
+                if (c.aligned_out) {
+                    if (on) __stcs(reinterpret_cast<uint4*>(to), make_uint4(o[0], o[1], o[2], o[3]));
                 } else {
-#pragma unroll
-                    for (int e = 0; e < kN; ++e) to[e] = __float2bfloat16_rn(out[e]);
+                    store_any(to, o, left, lane);
                 }
             }
         }
@@ -279,16 +358,16 @@ __global__ void __launch_bounds__(kSumsThreads) few_sums_kernel(const __grid_con
 #pragma unroll
     for (int i = 0; i < TN; ++i) {
         if (i >= a.rows) break;
-        float* plane = c.planes + ((int64_t)blockIdx.x * a.rows + i) * a.dim + col;
-#pragma unroll
-        for (int e = 0; e < kN; ++e) plane[e] = acc[i][e];
+        float4* plane = reinterpret_cast<float4*>(c.planes + ((int64_t)blockIdx.x * a.rows + i) * c.pitch + col);
+        plane[0] = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+        plane[1] = make_float4(acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
     }
 }
 
-constexpr int kHiddenThreads = 256, kHiddenParts = 8;   // a column's strips are shared by 8 threads
+constexpr int kHiddenThreads = 1024, kHiddenParts = kHiddenThreads / 32;   // that share a column's strips
 
 __global__ void __launch_bounds__(kHiddenThreads)
-    few_hidden_kernel(const float* planes, int32_t strips, int32_t rows, int32_t dim, __nv_bfloat16* out, int64_t ld) {
+    few_hidden_kernel(const float* planes, int32_t strips, int32_t rows, int32_t dim, int32_t pitch, __nv_bfloat16* out, int64_t ld) {
     __shared__ float s_sum[kHiddenParts][32];
     pdl_wait();
     pdl_trigger();
@@ -298,7 +377,7 @@ __global__ void __launch_bounds__(kHiddenThreads)
     if (col < dim) {
         const int32_t lo = (int32_t)((int64_t)strips * part / kHiddenParts), hi = (int32_t)((int64_t)strips * (part + 1) / kHiddenParts);
 #pragma unroll 8
-        for (int32_t s = lo; s < hi; ++s) sum += planes[((int64_t)s * rows + i) * dim + col];
+        for (int32_t s = lo; s < hi; ++s) sum += planes[((int64_t)s * rows + i) * pitch + col];
     }
     s_sum[part][lane] = sum;
     __syncthreads();
@@ -313,13 +392,14 @@ __global__ void __launch_bounds__(kHiddenThreads)
 bool rows_aligned(const void* p, int64_t stride, int32_t dim) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0 && dim % 8 == 0;
 }
+// Both operands' rows on 16-byte boundaries, in whole vectors.
 bool vectors(const LossArgs& a) {
     return rows_aligned(a.hidden, a.hidden_stride, a.dim) && rows_aligned(a.weight, a.weight_stride, a.dim);
 }
 
 struct FewSpace {
     int padded;              // rows, to 1, 2 or 4
-    int32_t block, blocks, ctas, strip, strips;
+    int32_t block, blocks, ctas, strip, strips, pitch;
     size_t target_logit, g, planes, end;
 };
 
@@ -330,7 +410,7 @@ FewSpace few_space(const LossArgs& a, const LaunchEnv& env, bool grad) {
     const int most = 32 / s.padded, warps = env.num_sms * 2 * kFewWarps;
     s.block = most;
     while (s.block > 1 && a.n_tokens / s.block < warps) s.block /= 2;
-    if (s.block < std::min(most, kFewLoads)) s.block = 1;
+    if (s.block < 4) s.block = 1;
     s.blocks = (a.n_tokens + s.block - 1) / s.block;
     s.ctas = std::min((s.blocks + kFewWarps - 1) / kFewWarps, env.num_sms * 2);
     size_t at = 0;
@@ -343,12 +423,13 @@ FewSpace few_space(const LossArgs& a, const LaunchEnv& env, bool grad) {
         take((size_t)a.rows * s.ctas * sizeof(float2));   // part, at 0
         s.target_logit = take((size_t)a.rows * 4);
     } else {
-        const int stretches = (a.dim + kSumsThreads * (vectors(a) ? 8 : 1) - 1) / (kSumsThreads * (vectors(a) ? 8 : 1));
-        const int want = std::max(1, env.num_sms * 6 / stretches);
+        const int stretches = (a.dim + kSumsThreads * kN - 1) / (kSumsThreads * kN);
+        const int want = std::max(1, env.num_sms * 4 / stretches);
+        s.pitch = (a.dim + kN - 1) / kN * kN;
         s.strip = std::max(16, (a.n_tokens + want - 1) / want);
         s.strips = (a.n_tokens + s.strip - 1) / s.strip;
         s.g = take((size_t)a.rows * a.n_tokens * 4);
-        s.planes = take((size_t)s.strips * a.rows * a.dim * 4);
+        s.planes = take((size_t)s.strips * a.rows * s.pitch * 4);
     }
     s.end = at;
     return s;
@@ -412,9 +493,10 @@ cudaError_t launch_few_loss_grad(const LossArgs& a, const LaunchEnv& env, void* 
     f.g = c.g;
     f.strip = s.strip;
     f.planes = (float*)((char*)space + s.planes);
-    f.vec_out = rows_aligned(a.dweight, a.dweight_stride, a.dim);
+    f.pitch = s.pitch;
+    f.aligned_out = rows_aligned(a.dweight, a.dweight_stride, a.dim);
     const bool vec = vectors(a);
-    const int width = kSumsThreads * (vec ? 8 : 1);
+    const int width = kSumsThreads * kN;
     const dim3 grid((unsigned)s.strips, (unsigned)((a.dim + width - 1) / width));
     cudaError_t e;
     switch (s.padded) {
@@ -424,7 +506,7 @@ cudaError_t launch_few_loss_grad(const LossArgs& a, const LaunchEnv& env, void* 
     }
     if (e != cudaSuccess) return e;
     return launch_pdl(few_hidden_kernel, dim3((unsigned)((a.dim + 31) / 32), (unsigned)a.rows), dim3(kHiddenThreads), 0, st,
-                      (const float*)f.planes, s.strips, a.rows, a.dim, (__nv_bfloat16*)a.dhidden, a.dhidden_stride);
+                      (const float*)f.planes, s.strips, a.rows, a.dim, s.pitch, (__nv_bfloat16*)a.dhidden, a.dhidden_stride);
 }
 
 }  // namespace domino
