@@ -193,13 +193,17 @@ def walk_stats(name: str):
         return None
 
 
+# sources that no kernel of a decode step or a precompute is built from
+OTHER_SOURCES = ("loss.cu", "loss_few.cu", "loss.h", "tcgen05.cuh", "distill.cu", "embed.cu")
+
+
 def csrc_digest() -> str:
-    """sha256 (first 16 hex digits) over the device sources, in name order."""
+    """sha256 (first 16 hex digits) over the decode path's device sources, in name order."""
     import hashlib
     d = os.path.join(ROOT, "paper_2403_06988_gb300", "csrc")
     hs = hashlib.sha256()
     for fn in sorted(os.listdir(d)):
-        if fn.endswith((".cu", ".cuh", ".h")):
+        if fn.endswith((".cu", ".cuh", ".h")) and fn not in OTHER_SOURCES:
             hs.update(fn.encode())
             with open(os.path.join(d, fn), "rb") as f:
                 hs.update(f.read())
