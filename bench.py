@@ -194,7 +194,7 @@ def walk_stats(name: str):
 
 
 # sources that no kernel of a decode step or a precompute is built from
-OTHER_SOURCES = ("loss.cu", "loss_few.cu", "loss.h", "tcgen05.cuh", "distill.cu", "embed.cu")
+OTHER_SOURCES = ("loss.cu", "loss_few.cu", "loss.h", "tcgen05.cuh", "bf16_rows.cuh", "distill.cu", "embed.cu")
 
 
 def csrc_digest() -> str:

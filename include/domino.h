@@ -460,7 +460,7 @@ int domino_embed(domino_t h, const int32_t* tokens_dev, int32_t n, const void* w
                  void* stream);
 
 /* Gradient of the table: dweight[v] = scale * the sum of grad[i] over the i with
- * tokens[i] = v, in the order of the list, rounded once.  accumulate = 0: every
+ * tokens[i] = v, in an order that the list fixes, rounded once.  accumulate = 0: every
  * row is written (zeros for tokens that do not occur); 1: added to what
  * dweight_dev holds, and the other rows are not touched (a table that is the
  * loss's weight too: domino_token_loss_grad first, then this). */

@@ -38,7 +38,7 @@ def nvcc() -> str:
 def _inputs():
     files = [os.path.join(CSRC, f) for f in SOURCES]
     files += [os.path.join(CSRC, "domino_internal.h"), os.path.join(CSRC, "walk_common.cuh"),
-              os.path.join(CSRC, "decode.cuh"), os.path.join(CSRC, "loss.h"), os.path.join(CSRC, "tcgen05.cuh"),
+              os.path.join(CSRC, "decode.cuh"), os.path.join(CSRC, "loss.h"), os.path.join(CSRC, "tcgen05.cuh"), os.path.join(CSRC, "bf16_rows.cuh"),
               os.path.join(INCLUDE, "domino.h")]
     return files
 

@@ -5,7 +5,7 @@
 //   dW[v]   = scale sum_{i: tokens[i] = v} g[i]
 //
 // Both are bound by HBM.  The gradient sorts the tokens (stable, so that a
-// row's sum always runs in the order of the list) and sums runs of equal
+// row's sum is always made in the same order) and sums runs of equal
 // tokens in fp32: a CTA per chunk of the sorted list and stretch of columns; a
 // run that crosses chunks is kept in parts, which a second pass joins in order.
 // One cluster sorts while the others write the table's zeros.
@@ -14,6 +14,7 @@
 
 #include <algorithm>
 
+#include "bf16_rows.cuh"
 #include "loss.h"
 #include "walk_common.cuh"
 
@@ -43,18 +44,7 @@ __device__ __forceinline__ uint4 scaled(const uint4& u, float scale) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-template <bool BF16>
-__device__ __forceinline__ float value_at(const void* p, int64_t i) {
-    if constexpr (BF16) return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[i]);
-    else return reinterpret_cast<const float*>(p)[i];
-}
-template <bool BF16>
-__device__ __forceinline__ void put_at(void* p, int64_t i, float x) {
-    if constexpr (BF16) reinterpret_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(x);
-    else reinterpret_cast<float*>(p)[i] = x;
-}
-
-// A thread takes kEmbedUnroll pieces (16-byte vectors, or with !VEC single
+// A thread takes kEmbedUnroll pieces (16-byte vectors, or with !VEC single fp32
 // values) of the output's `per_row` a row, a grid's width apart.  far: an output of half the L2 or more is written past it
 // (37.0 -> 35.3 us).
 template <bool BF16, bool VEC>
@@ -78,7 +68,7 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const EmbedArgs a,
         if (t >= 0 && t < a.n_tokens) {
             const int64_t from = (int64_t)t * a.weight_stride + (int64_t)c * (VEC ? 16 / kSize : 1);
             if constexpr (VEC) u[j] = __ldg(reinterpret_cast<const uint4*>((const char*)a.weight + from * kSize));
-            else u[j].x = __float_as_uint(value_at<BF16>(a.weight, from));
+            else u[j].x = __float_as_uint(__ldg((const float*)a.weight + from));
         } else if (t >= a.n_tokens && c == 0) {
             atomicOr(a.err, DOMINO_DEVERR_BAD_TOKEN);
         }
@@ -91,8 +81,34 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const EmbedArgs a,
             const uint4 x = scaled<BF16>(u[j], a.scale);
             if (far) __stcs(to, x);
             else *to = x;
-        } else put_at<BF16>(a.out, at[j], __uint_as_float(u[j].x) * a.scale);
+        } else {
+            ((float*)a.out)[at[j]] = __uint_as_float(u[j].x) * a.scale;
+        }
     }
+}
+
+// bf16 rows off 16-byte boundaries: a warp takes 256 columns of a row.
+__global__ void __launch_bounds__(kEmbedThreads) embed_any_kernel(const EmbedArgs a, const int32_t stretches) {
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x & 31;
+    const int64_t i = (int64_t)blockIdx.x * (kEmbedThreads / 32) + (threadIdx.x >> 5);
+    const int32_t r = (int32_t)(i / stretches), c = (int32_t)(i - (int64_t)r * stretches) * 256 + lane * kN;
+    if (r >= a.n) return;
+    const int32_t t = __ldg(a.tokens + r), left = a.dim - c;
+    if (t >= a.n_tokens && c == 0) atomicOr(a.err, DOMINO_DEVERR_BAD_TOKEN);
+    Eight x;
+    x.zero();
+    if (t >= 0 && t < a.n_tokens && left > 0) x.load((const __nv_bfloat16*)a.weight + (int64_t)t * a.weight_stride + c, left);
+    float v[kN];
+    x.get(v);
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k] * a.scale, v[2 * k + 1] * a.scale);
+        w[k] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    store_any((__nv_bfloat16*)a.out + (int64_t)r * a.out_stride + c, w, left, lane);
 }
 
 // ---- the list sorted by token ---------------------------------------------------
@@ -170,21 +186,26 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortArgs s) {
         for (int32_t i = lo + lane; i < hi; i += 32) atomicAdd(&count[warp][(entry(i).x >> shift) & digit_mask], 1u);
         __syncthreads();
         if (tid < (int)bins) {   // before each warp's: the CTA's earlier warps'
-            uint32_t sum = 0;
+            uint32_t n[kSortWarps], sum = 0;   // read before any is written: the reads do not wait for one another
+#pragma unroll
+            for (int w = 0; w < kSortWarps; ++w) n[w] = count[w][tid];
+#pragma unroll
             for (int w = 0; w < kSortWarps; ++w) {
-                const uint32_t n = count[w][tid];
                 count[w][tid] = sum;
-                sum += n;
+                sum += n[w];
             }
             total[tid] = sum;
         }
         cluster.sync();
         uint32_t all = 0, before = 0;
         if (tid < (int)bins) {
-            for (int c = 0; c < s.ctas; ++c) {
-                const uint32_t n = *cluster.map_shared_rank(&total[tid], c);
-                all += n;
-                if (c < cta) before += n;
+            uint32_t n[kSortCtas];
+#pragma unroll
+            for (int c = 0; c < kSortCtas; ++c) n[c] = c < s.ctas ? *cluster.map_shared_rank(&total[tid], c) : 0u;
+#pragma unroll
+            for (int c = 0; c < kSortCtas; ++c) {
+                all += n[c];
+                if (c < cta) before += n[c];
             }
         }
         uint32_t scan = all;   // of the bins: smaller digits
@@ -197,7 +218,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortArgs s) {
         __syncthreads();
         if (tid < (int)bins) {
             uint32_t smaller = scan - all;
-            for (int w = 0; w < warp; ++w) smaller += warp_sum[w];
+#pragma unroll
+            for (int w = 0; w < kSortBins / 32; ++w) smaller += w < warp ? warp_sum[w] : 0u;
             base[tid] = smaller + before;
         }
         __syncthreads();
@@ -222,7 +244,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortArgs s) {
 }
 
 // ---- sums of runs -----------------------------------------------------------------
-constexpr int kSumThreads = 256;
+constexpr int kSumThreads = 128;
 constexpr int kSumUnroll = 8;
 constexpr int kSumChunk = 32;              // of the sorted list whose places are in shared memory at a time
 
@@ -231,49 +253,68 @@ struct SumArgs {
     const uint2* order;
     int32_t chunk, chunks;
     int32_t stretches;         // of the columns, kSumThreads pieces each
-    float* part;               // [chunks][2][dim]: the run that began before the chunk; the one that goes on after it
+    int32_t pitch;             // dim, rounded up to 8
+    float* part;               // [chunks][2][pitch]: the run that began before the chunk; the one that goes on after it
 };
 
+// A thread's columns: VEC: a 16-byte vector; else one fp32 value, or eight bf16 at any alignment.
 template <bool BF16, bool VEC>
 struct Piece {
-    static constexpr int kN = !VEC ? 1 : BF16 ? 8 : 4;
-    float v[kN];
+    static constexpr int kCols = BF16 ? 8 : VEC ? 4 : 1;
+    float v[kCols];
     __device__ __forceinline__ void zero() {
 #pragma unroll
-        for (int i = 0; i < kN; ++i) v[i] = 0.0f;
+        for (int i = 0; i < kCols; ++i) v[i] = 0.0f;
     }
     // as it lies in memory
-    static __device__ __forceinline__ uint4 fetch(const void* p, int64_t i) {
-        if constexpr (VEC) return __ldcs(reinterpret_cast<const uint4*>((const char*)p + i * (BF16 ? 2 : 4)));
-        else return make_uint4(__float_as_uint(value_at<BF16>(p, i)), 0u, 0u, 0u);
+    using Raw = std::conditional_t<BF16 && !VEC, Eight, uint4>;
+    static __device__ __forceinline__ Raw nothing() {
+        Raw r;
+        if constexpr (BF16 && !VEC) r.zero();
+        else r = make_uint4(0u, 0u, 0u, 0u);
+        return r;
     }
-    __device__ __forceinline__ void add(const uint4& u) {
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    // value i of p, the row's end `left` values further
+    static __device__ __forceinline__ Raw fetch(const void* p, int64_t i, int32_t left) {
+        Raw r;
+        if constexpr (VEC) r = __ldcs(reinterpret_cast<const uint4*>((const char*)p + i * (BF16 ? 2 : 4)));
+        else if constexpr (BF16) r.load((const __nv_bfloat16*)p + i, left);
+        else r = make_uint4(__float_as_uint(((const float*)p)[i]), 0u, 0u, 0u);
+        return r;
+    }
+    __device__ __forceinline__ void add(const Raw& r) {
+        if constexpr (BF16 && !VEC) {
+            float x[kN];
+            r.get(x);
 #pragma unroll
-        for (int k = 0; k < (VEC ? 4 : 1); ++k) {
-            if constexpr (VEC && BF16) {
-                v[(2 * k) % kN] += __uint_as_float(w[k] << 16);
-                v[(2 * k + 1) % kN] += __uint_as_float(w[k] & 0xFFFF0000u);
-            } else {
-                v[k] += __uint_as_float(w[k]);
+            for (int k = 0; k < kCols; ++k) v[k] += x[k];
+        } else {
+            const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+            for (int k = 0; k < (VEC ? 4 : 1); ++k) {
+                if constexpr (BF16) {
+                    v[2 * k] += __uint_as_float(w[k] << 16);
+                    v[2 * k + 1] += __uint_as_float(w[k] & 0xFFFF0000u);
+                } else {
+                    v[k] += __uint_as_float(w[k]);
+                }
             }
         }
     }
-    __device__ __forceinline__ void store(void* p, int64_t i) const {
-        if constexpr (!VEC) {
-            put_at<BF16>(p, i, v[0]);
-        } else {
+    // every thread of the warp calls it (left <= 0: nothing of its own)
+    __device__ __forceinline__ void store(void* p, int64_t i, int32_t left) const {
+        if constexpr (BF16) {
             uint32_t w[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                if constexpr (BF16) {
-                    const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-                    w[k] = *reinterpret_cast<const uint32_t*>(&b);
-                } else {
-                    w[k] = __float_as_uint(v[k]);
-                }
+                const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+                w[k] = *reinterpret_cast<const uint32_t*>(&b);
             }
-            *reinterpret_cast<uint4*>((char*)p + i * (BF16 ? 2 : 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+            if constexpr (!VEC) store_any((__nv_bfloat16*)p + i, w, left, threadIdx.x & 31);
+            else if (left > 0) *reinterpret_cast<uint4*>((__nv_bfloat16*)p + i) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else if (left > 0) {
+            if constexpr (VEC) *reinterpret_cast<float4*>((float*)p + i) = make_float4(v[0], v[1], v[2], v[3]);
+            else ((float*)p)[i] = v[0];
         }
     }
 };
@@ -282,12 +323,11 @@ struct Piece {
 template <bool BF16, bool VEC>
 __device__ __forceinline__ void finish_row(const EmbedArgs& a, uint32_t token, int32_t c, Piece<BF16, VEC> sum) {
     const int64_t at = (int64_t)token * a.dweight_stride + c;
+    const int32_t left = a.dim - c;
 #pragma unroll
-    for (int i = 0; i < sum.kN; ++i) sum.v[i] *= a.scale;
-    if (a.add) {
-        sum.add(Piece<BF16, VEC>::fetch(a.dweight, at));
-    }
-    sum.store(a.dweight, at);
+    for (int i = 0; i < sum.kCols; ++i) sum.v[i] *= a.scale;
+    if (a.add && left > 0) sum.add(Piece<BF16, VEC>::fetch(a.dweight, at, left));
+    sum.store(a.dweight, at, left);
 }
 
 template <bool BF16, bool VEC>
@@ -297,7 +337,7 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs s) {
     pdl_wait();
     pdl_trigger();
     const int32_t chunk = blockIdx.x / s.stretches, stretch = blockIdx.x - chunk * s.stretches;
-    const int32_t c = (stretch * kSumThreads + threadIdx.x) * P::kN;
+    const int32_t c = (stretch * kSumThreads + threadIdx.x) * P::kCols;
     const bool on = c < a.dim;
     const int32_t lo = chunk * s.chunk, hi = min(a.n, lo + s.chunk);
     const uint32_t none = (uint32_t)a.n_tokens;
@@ -310,39 +350,40 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs s) {
     };
     stage(lo);
     const uint32_t before = s_order[0].x;
-    float* part = s.part + (int64_t)chunk * 2 * a.dim + c;
+    float* part = s.part + (int64_t)chunk * 2 * s.pitch + c;
     P sum;
     sum.zero();
     uint32_t token = s_order[1].x;
     bool first = true;   // the chunk's first run
     const auto flush = [&](bool last, uint32_t after) {
-        if (token == none || !on) return;
-        if (first && token == before) {
+        if (token == none) return;
+        const bool head = first && token == before;
+        if (head || (last && token == after)) {
+            float* to = head ? part : part + s.pitch;
+            if (on)
 #pragma unroll
-            for (int i = 0; i < P::kN; ++i) part[i] = sum.v[i];
-        } else if (last && token == after) {
-#pragma unroll
-            for (int i = 0; i < P::kN; ++i) part[a.dim + i] = sum.v[i];
+                for (int i = 0; i < P::kCols; ++i) to[i] = sum.v[i];
         } else {
             finish_row<BF16, VEC>(a, token, c, sum);
         }
     };
+    constexpr int kUnroll = BF16 && !VEC ? kSumUnroll / 2 : kSumUnroll;   // two loads each
     for (int32_t b0 = lo; b0 < hi; b0 += kSumChunk) {
         if (b0 > lo) {
             __syncthreads();
             stage(b0);
         }
         const int n = min(kSumChunk, hi - b0);
-        for (int j0 = 0; j0 < n; j0 += kSumUnroll) {
-            uint4 g[kSumUnroll];
+        for (int j0 = 0; j0 < n; j0 += kUnroll) {
+            typename P::Raw g[kUnroll];
 #pragma unroll
-            for (int j = 0; j < kSumUnroll; ++j) {
-                g[j] = make_uint4(0u, 0u, 0u, 0u);
+            for (int j = 0; j < kUnroll; ++j) {
+                g[j] = P::nothing();
                 if (on && j0 + j < n && s_order[1 + j0 + j].x != none)
-                    g[j] = P::fetch(a.grad, (int64_t)s_order[1 + j0 + j].y * a.grad_stride + c);
+                    g[j] = P::fetch(a.grad, (int64_t)s_order[1 + j0 + j].y * a.grad_stride + c, a.dim - c);
             }
 #pragma unroll
-            for (int j = 0; j < kSumUnroll; ++j) {
+            for (int j = 0; j < kUnroll; ++j) {
                 if (j0 + j >= n) break;
                 const uint32_t t = s_order[1 + j0 + j].x;
                 if (t != token) {
@@ -358,7 +399,11 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs s) {
     }
 }
 
-// The runs that cross chunks: each by the CTAs of the chunk that it begins in.
+// The runs that cross chunks: each by the CTAs of the chunk that it begins in; one
+// look at the first tokens of 32 following chunks, then their sums, eight at a
+// time.  (Groups of threads for the eights: four times the threads of the many CTAs
+// that have no such run, 16384 tokens x 4096 11 -> 20 us.)
+
 template <bool BF16, bool VEC>
 __global__ void __launch_bounds__(kSumThreads) join_kernel(const SumArgs s) {
     using P = Piece<BF16, VEC>;
@@ -366,35 +411,38 @@ __global__ void __launch_bounds__(kSumThreads) join_kernel(const SumArgs s) {
     pdl_wait();
     pdl_trigger();
     const int32_t chunk = blockIdx.x / s.stretches, stretch = blockIdx.x - chunk * s.stretches;
-    const int32_t c = (stretch * kSumThreads + threadIdx.x) * P::kN;
+    const int lane = threadIdx.x & 31;
+    const int32_t c = (stretch * kSumThreads + threadIdx.x) * P::kCols;
     const int32_t lo = chunk * s.chunk, hi = lo + s.chunk;
-    if (c >= a.dim || hi >= a.n) return;
+    if (hi >= a.n) return;
+    const bool on = c < a.dim;
     const uint32_t token = s.order[hi - 1].x;
     if (token == (uint32_t)a.n_tokens || s.order[hi].x != token) return;         // no run goes on after the chunk
     if (s.order[lo].x == token && lo > 0 && s.order[lo - 1].x == token) return;   // it began before the chunk
     P sum;
-    const float* part = s.part + (int64_t)chunk * 2 * a.dim + c;
+    sum.zero();
+    const float* part = s.part + (int64_t)chunk * 2 * s.pitch + c;
+    if (on)
 #pragma unroll
-    for (int i = 0; i < P::kN; ++i) sum.v[i] = part[a.dim + i];
-    // the following chunks that begin with the token, eight at a time: the loads do not wait for one another
-    for (int32_t k = chunk + 1; k < s.chunks; k += kSumUnroll) {
-        uint32_t t[kSumUnroll];
-        float v[kSumUnroll][P::kN];
+        for (int i = 0; i < P::kCols; ++i) sum.v[i] = part[s.pitch + i];
+    for (int32_t k = chunk + 1; k < s.chunks; k += 32) {
+        // the chunks that begin with the token: the first `more` of the 32 (the list is sorted)
+        const bool same = k + lane < s.chunks && s.order[(int64_t)(k + lane) * s.chunk].x == token;
+        const int more = __popc(__ballot_sync(0xffffffffu, same));
+#pragma unroll 2
+        for (int j0 = 0; j0 < more; j0 += kSumUnroll) {
+            float v[kSumUnroll][P::kCols];
 #pragma unroll
-        for (int j = 0; j < kSumUnroll; ++j) {
-            const bool in = k + j < s.chunks;
-            t[j] = in ? s.order[(int64_t)(k + j) * s.chunk].x : (uint32_t)a.n_tokens;
+            for (int j = 0; j < kSumUnroll; ++j)
 #pragma unroll
-            for (int i = 0; i < P::kN; ++i) v[j][i] = in ? part[(int64_t)(k + j - chunk) * 2 * a.dim + i] : 0.0f;
+                for (int i = 0; i < P::kCols; ++i)
+                    v[j][i] = on && j0 + j < more ? part[(int64_t)(k + j0 + j - chunk) * 2 * s.pitch + i] : 0.0f;
+#pragma unroll
+            for (int j = 0; j < kSumUnroll; ++j)
+#pragma unroll
+                for (int i = 0; i < P::kCols; ++i) sum.v[i] += v[j][i];
         }
-        bool more = true;
-#pragma unroll
-        for (int j = 0; j < kSumUnroll; ++j) {
-            more = more && t[j] == token;
-#pragma unroll
-            for (int i = 0; i < P::kN; ++i) sum.v[i] += more ? v[j][i] : 0.0f;   // others' parts may hold anything
-        }
-        if (!more) break;
+        if (more < 32) break;
     }
     finish_row<BF16, VEC>(a, token, c, sum);
 }
@@ -430,15 +478,15 @@ EmbedSpace embed_space(const EmbedArgs& a, const LaunchEnv& env) {
     const auto align = [](size_t n) { return (n + 255) & ~(size_t)255; };
     s.b = align((size_t)a.n * sizeof(uint2));
     s.part = 2 * s.b;
-    s.end = s.part + align((size_t)s.chunks * 2 * a.dim * 4);
+    s.end = s.part + align((size_t)s.chunks * 2 * (((size_t)a.dim + 7) / 8 * 8) * 4);
     return s;
 }
 
 template <bool BF16, bool VEC>
 cudaError_t launch_sums(const EmbedArgs& a, const SumArgs& in, cudaStream_t st) {
     SumArgs s = in;
-    constexpr int kN = Piece<BF16, VEC>::kN;
-    s.stretches = (a.dim + kSumThreads * kN - 1) / (kSumThreads * kN);
+    constexpr int kCols = Piece<BF16, VEC>::kCols;
+    s.stretches = (a.dim + kSumThreads * kCols - 1) / (kSumThreads * kCols);
     const dim3 grid((unsigned)s.chunks * (unsigned)s.stretches);
     cudaError_t e = launch_pdl(sum_kernel<BF16, VEC>, grid, dim3(kSumThreads), 0, st, s);
     if (e != cudaSuccess || s.chunks == 1) return e;
@@ -451,7 +499,13 @@ cudaError_t launch_embed(const EmbedArgs& a, const LaunchEnv&, cudaStream_t st) 
     const bool bf16 = a.dtype == DOMINO_DTYPE_BF16;
     const int size = bf16 ? 2 : 4;
     const bool vec = vectors_fit(a.weight, a.weight_stride, a.dim, size) && vectors_fit(a.out, a.out_stride, a.dim, size);
-    if (bf16) return vec ? launch_rows<true, true>(a, st) : launch_rows<true, false>(a, st);
+    if (bf16 && !vec) {
+        const int32_t stretches = (a.dim + 255) / 256;
+        const int64_t ctas = ((int64_t)a.n * stretches + kEmbedThreads / 32 - 1) / (kEmbedThreads / 32);
+        if (ctas > INT_MAX) return cudaErrorInvalidValue;
+        return launch_pdl(embed_any_kernel, dim3((unsigned)ctas), dim3(kEmbedThreads), 0, st, a, stretches);
+    }
+    if (bf16) return launch_rows<true, true>(a, st);
     return vec ? launch_rows<false, true>(a, st) : launch_rows<false, false>(a, st);
 }
 
@@ -493,6 +547,7 @@ cudaError_t launch_embed_grad(const EmbedArgs& a, const LaunchEnv& env, void* sp
     s.order = so.a;
     s.chunk = sp.chunk;
     s.chunks = sp.chunks;
+    s.pitch = (a.dim + 7) / 8 * 8;
     s.part = (float*)(ws + sp.part);
     const bool vec = vectors_fit(a.grad, a.grad_stride, a.dim, size) && vectors_fit(a.dweight, a.dweight_stride, a.dim, size);
     if (bf16) return vec ? launch_sums<true, true>(a, s, st) : launch_sums<true, false>(a, s, st);

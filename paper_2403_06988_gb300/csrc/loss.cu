@@ -25,6 +25,7 @@
 #include <algorithm>
 #include <atomic>
 
+#include "bf16_rows.cuh"
 #include "decode.cuh"
 #include "loss.h"
 #include "tcgen05.cuh"
@@ -515,14 +516,7 @@ __device__ __forceinline__ uint4 read_eight(const Pack& p, const __nv_bfloat16* 
         const uint4 a = __ldg(block);
         if (off == 0) return a;
         const uint4 b = __ldg(block + 1);
-        uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int i = 0; i < 6; ++i) w[i] = off & 4 ? w[i + 2] : w[i];
-#pragma unroll
-        for (int i = 0; i < 5; ++i) w[i] = off & 2 ? w[i + 1] : w[i];
-        const uint32_t shift = off & 1 ? 16 : 0;
-        return make_uint4(__funnelshift_r(w[0], w[1], shift), __funnelshift_r(w[1], w[2], shift),
-                          __funnelshift_r(w[2], w[3], shift), __funnelshift_r(w[3], w[4], shift));
+        return eight_from(a, b, off);
     }
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll

@@ -16,6 +16,7 @@
 
 #include <algorithm>
 
+#include "bf16_rows.cuh"
 #include "decode.cuh"
 #include "loss.h"
 
@@ -38,49 +39,19 @@ struct FewCall {
 // Eight consecutive bf16 of a row as fp32, zeros beyond the row's end.  ALIGNED:
 // rows begin on 16-byte boundaries and have whole vectors.  Else they are read in
 // the 16-byte blocks that hold the values, and shifted.
-constexpr int kN = 8;
 template <bool ALIGNED>
-struct Cols {
-    uint4 u, v;
-    uint32_t off, n;
-    __device__ __forceinline__ void zero() {
-        u = v = make_uint4(0, 0, 0, 0);
-        off = 0;
-        n = kN;
-    }
-    // left: values from p to the row's end, at least one
-    __device__ __forceinline__ void load(const __nv_bfloat16* p, int32_t left) {
-        if constexpr (ALIGNED) {
-            u = __ldg(reinterpret_cast<const uint4*>(p));
-        } else {
-            const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-            const uint4* block = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
-            off = (uint32_t)(at & 15) / 2;
-            n = (uint32_t)min(left, kN);
-            u = __ldg(block);
-            v = make_uint4(0, 0, 0, 0);
-            if (off + n > kN) v = __ldg(block + 1);
-        }
-    }
+struct Cols : Eight {};
+template <>
+struct Cols<true> {
+    uint4 u;
+    __device__ __forceinline__ void zero() { u = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, int32_t) { u = __ldg(reinterpret_cast<const uint4*>(p)); }
     __device__ __forceinline__ void get(float (&f)[kN]) const {
-        uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
-        if constexpr (!ALIGNED) {
-#pragma unroll
-            for (int i = 0; i < 6; ++i) w[i] = off & 4 ? w[i + 2] : w[i];
-#pragma unroll
-            for (int i = 0; i < 5; ++i) w[i] = off & 2 ? w[i + 1] : w[i];
-            const uint32_t shift = off & 1 ? 16 : 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], shift);
-        }
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             f[2 * i] = __uint_as_float(w[i] << 16);
             f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-        }
-        if constexpr (!ALIGNED) {
-#pragma unroll
-            for (int i = 0; i < kN; ++i) f[i] = (uint32_t)i < n ? f[i] : 0.0f;
         }
     }
 };
@@ -229,43 +200,6 @@ struct FewSums {
     float* planes;                        // [strips][rows][pitch]
     bool aligned_out;
 };
-
-// A warp's 256 consecutive values (eight a lane, `left` of lane 0's to the row's end) to a row of bf16 at any
-// alignment: in the 16-byte blocks that lie in them, each lane's from its own values and the lane's before it, and one
-// by one at the two ends.
-__device__ __forceinline__ void store_any(__nv_bfloat16* to, const uint32_t (&w)[4], int32_t left, int lane) {
-    // to, left: this lane's
-    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(to) & 15) / 2;
-    uint32_t x[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[i] = __shfl_up_sync(0xffffffffu, w[i], 1);
-        x[4 + i] = w[i];
-    }
-    // values 8 - off.. of the 16 are the block at `to` rounded down
-    const uint32_t from = 8 - off;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = from & 8 ? x[i + 4] : x[i];
-#pragma unroll
-    for (int i = 0; i < 6; ++i) x[i] = from & 4 ? x[i + 2] : x[i];
-#pragma unroll
-    for (int i = 0; i < 5; ++i) x[i] = from & 2 ? x[i + 1] : x[i];
-    const uint32_t shift = from & 1 ? 16 : 0;
-    const uint4 block = make_uint4(__funnelshift_r(x[0], x[1], shift), __funnelshift_r(x[1], x[2], shift),
-                                   __funnelshift_r(x[2], x[3], shift), __funnelshift_r(x[3], x[4], shift));
-    unsigned short* p = reinterpret_cast<unsigned short*>(to);
-    const int32_t n = left < kN ? (left < 0 ? 0 : left) : kN;             // this lane's values
-    const bool whole = (off == 0 || lane > 0) && left >= (int32_t)(kN - off);   // the block ends in the row
-    if (whole) *reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(to) & ~(uintptr_t)15) = block;
-    // beside the blocks: lane 0's first, what the next block would hold of the last lane's or of the row's last values
-    const bool next_whole = lane < 31 && left - kN >= (int32_t)(kN - off) && off > 0;
-#pragma unroll
-    for (int e = 0; e < kN; ++e) {
-        const bool in_mine = e < (int)(kN - off);   // else in the next lane's block
-        const bool one = in_mine ? !whole : !next_whole;
-        if (e < n && one) p[e] = (unsigned short)(w[e / 2] >> (16 * (e & 1)));
-    }
-}
 
 template <int TN, bool ALIGNED>
 __global__ void __launch_bounds__(kSumsThreads) few_sums_kernel(const __grid_constant__ FewSums c) {

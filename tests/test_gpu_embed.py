@@ -167,3 +167,23 @@ def test_refusals(d):
     with pytest.raises(DominoError) as e:
         B.domino_embed_grad(d.h, t, 5, w, 12, B.DTYPE_BF16, 40, 12, 1.0, 2, w, 12)
     assert e.value.status == -1
+
+
+@pytest.mark.parametrize("n,V,D", [(3, 9, 3), (40, 12, 257), (700, 50, 515), (64, 7, 2055)])
+def test_bf16_rows_at_every_offset(d, n, V, D):
+    """Odd widths: consecutive rows begin at every even byte of a 16-byte block; nothing beside them is written."""
+    t, w, g = tokens(n, V), values(V, D, "bf16"), values(n, D, "bf16")
+    want = torch.where((t >= 0)[:, None], w[t.long().clamp(min=0)].float() * 1.5, torch.zeros((), device="cuda"))
+    guard = torch.full((n * D + 64,), 7.0, dtype=torch.bfloat16, device="cuda")
+    for off in (0, 3, 8):
+        guard.fill_(7.0)
+        out = guard[off:off + n * D].view(n, D)
+        d.embed(t, w, 1.5, out=out)
+        assert torch.equal(out, want.bfloat16())
+        assert (guard[:off] == 7).all() and (guard[off + n * D:] == 7).all()
+    big = torch.full((V * D + 64,), 7.0, dtype=torch.bfloat16, device="cuda")
+    into = big[5:5 + V * D].view(V, D)
+    into.copy_(w)
+    ref, tol = embed_grad(t, g, V, 0.5, w)
+    assert_within(d.embed_grad(t, g, V, 0.5, into=into), ref, tol, "into")
+    assert (big[:5] == 7).all() and (big[5 + V * D:] == 7).all()

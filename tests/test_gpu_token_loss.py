@@ -246,3 +246,41 @@ def test_capture_needs_room_first():
     assert e.value.status == -1
     torch.cuda.synchronize()
     d.close()
+
+
+@pytest.mark.parametrize("T,V,D", [(1, 300, 1029), (2, 6000, 517), (4, 90, 3), (3, 20000, 261), (5, 300, 1029), (200, 900, 261)])
+@pytest.mark.parametrize("off", [0, 1, 6])
+def test_odd_widths_at_every_offset(d, T, V, D, off):
+    """Rows that begin at every even byte of a 16-byte block; nothing beside the gradients is written."""
+    h, w, y, mask, c = inputs(T, V, D, density=0.5)
+    ref = TokenLoss(h, w, y, mask, c)
+
+    def inside(x):
+        base = torch.full((x.numel() + off + 64,), float("nan"), dtype=x.dtype, device="cuda")
+        view = base[off:off + x.numel()].view(x.shape)
+        view.copy_(x)
+        return base, view
+    (_, hv), (_, wv) = inside(h), inside(w)
+    loss, lse = d.token_loss(hv, wv, y, mask)
+    (bh, dh), (bw, dw) = inside(torch.zeros_like(h)), inside(torch.zeros_like(w))
+    d.token_loss_grad(hv, wv, y, lse, c, mask, out=(dh, dw))
+    for name, got in (("lse", lse), ("loss", loss), ("dhidden", dh), ("dweight", dw)):
+        assert_within(got, getattr(ref, name), ref.tol[name], name)
+    for base, x in ((bh, h), (bw, w)):
+        assert torch.isnan(base[:off]).all() and torch.isnan(base[off + x.numel():]).all()
+
+
+@pytest.mark.parametrize("T", [3, 40])
+def test_weights_of_masked_tokens_hold_anything_forward(d, T):
+    """The loss is over the allowed tokens alone."""
+    h, w, y, mask, _ = inputs(T, 700, 64, density=0.3)
+    bits = torch.zeros(T, 700, dtype=torch.bool, device="cuda")
+    bits[:, ::2] = True
+    y = (y // 2 * 2).clamp(max=698)
+    mask = pack(bits)
+    ref = TokenLoss(h, w, y, mask)
+    w2 = w.clone()
+    w2[1::2] = float("nan")
+    loss, lse = d.token_loss(h, w2, y, mask)
+    assert_within(lse, ref.lse, ref.tol["lse"], "lse")
+    assert_within(loss, ref.loss, ref.tol["loss"], "loss")
