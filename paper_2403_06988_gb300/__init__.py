@@ -254,13 +254,22 @@ class Domino:
         return so
 
     # -- losses over the vocabulary, the embedding (no loaded vocabulary needed) -----
+    # These methods call the library themselves: of a small call's time, the host's
+    # is the larger part.
+    def _new(self, shape, dtype, device):
+        return _T.empty(shape, dtype=dtype, device=device) if self.fill_byte is None else self._empty(shape, dtype, device)
+
     def _floats(self, out, i, n, like, what):
         """out[i], or a new fp32 tensor of n values, and its address."""
         x = None if out is None else out[i]
         if x is None:
-            x = self._empty(n, _T.float32, like.device)
+            x = self._new(n, _T.float32, like.device)
             return x, x.data_ptr()
         return x, _words(x, self.device, _T.float32, n, what)
+
+    def _raw(self, stream):
+        """The cudaStream_t of `stream`, or of the handle's device's current one."""
+        return _T._C._cuda_getCurrentRawStream(self.device) if stream is None else B._stream(stream)
 
     def _loss_inputs(self, hidden, weight, targets, mask):
         torch, dev = _torch(), self.device
@@ -280,7 +289,9 @@ class Domino:
         args = self._loss_inputs(hidden, weight, targets, mask)
         loss, pl = self._floats(out, 0, args[6], hidden, "loss")
         lse, pz = self._floats(out, 1, args[6], hidden, "lse")
-        B.domino_token_loss(*args, pl, pz, stream)
+        rc = B.lib().domino_token_loss(*args, pl, pz, self._raw(stream))
+        if rc:
+            B._check("domino_token_loss", rc)
         return loss, lse
 
     def token_loss_grad(self, hidden, weight, targets, lse, grad_loss, mask=None, out=None, stream=None) -> Tuple:
@@ -290,16 +301,18 @@ class Domino:
         dh, dw = out if out is not None else (None, None)
         hs = ws = dim
         if dh is None:
-            dh = self._empty((rows, dim), hidden.dtype, hidden.device)
+            dh = self._new((rows, dim), hidden.dtype, hidden.device)
         else:
             hs = _like(dh, self.device, "dhidden", rows, dim, code)
         if dw is None:
-            dw = self._empty((V, dim), weight.dtype, weight.device)
+            dw = self._new((V, dim), weight.dtype, weight.device)
         else:
             ws = _like(dw, self.device, "dweight", V, dim, code)
-        B.domino_token_loss_grad(*args, _words(lse, self.device, _T.float32, rows, "lse"),
-                                 _words(grad_loss, self.device, _T.float32, rows, "grad_loss"), dh.data_ptr(), hs,
-                                 dw.data_ptr(), ws, stream)
+        rc = B.lib().domino_token_loss_grad(*args, _words(lse, self.device, _T.float32, rows, "lse"),
+                                            _words(grad_loss, self.device, _T.float32, rows, "grad_loss"),
+                                            dh.data_ptr(), hs, dw.data_ptr(), ws, self._raw(stream))
+        if rc:
+            B._check("domino_token_loss_grad", rc)
         return dh, dw
 
     def _distill_inputs(self, logits, teacher, ids, temperature, mask):
@@ -319,7 +332,9 @@ class Domino:
         args = self._distill_inputs(logits, teacher, ids, temperature, mask)
         loss, pl = self._floats(out, 0, args[3], logits, "loss")
         lse, pz = self._floats(out, 1, args[3], logits, "lse")
-        B.domino_distill_loss(*args, pl, pz, stream)
+        rc = B.lib().domino_distill_loss(*args, pl, pz, self._raw(stream))
+        if rc:
+            B._check("domino_distill_loss", rc)
         return loss, lse
 
     def distill_grad(self, logits, teacher, ids, temperature: float, lse, grad_loss, mask=None, out=None, stream=None):
@@ -328,11 +343,14 @@ class Domino:
         rows, V = args[3], args[5]
         step = V
         if out is None:
-            out = self._empty((rows, V), logits.dtype, logits.device)
+            out = self._new((rows, V), logits.dtype, logits.device)
         else:
             step = _like(out, self.device, "out", rows, V, args[2])
-        B.domino_distill_grad(*args, _words(lse, self.device, _T.float32, rows, "lse"),
-                              _words(grad_loss, self.device, _T.float32, rows, "grad_loss"), out.data_ptr(), step, stream)
+        rc = B.lib().domino_distill_grad(*args, _words(lse, self.device, _T.float32, rows, "lse"),
+                                         _words(grad_loss, self.device, _T.float32, rows, "grad_loss"),
+                                         out.data_ptr(), step, self._raw(stream))
+        if rc:
+            B._check("domino_distill_grad", rc)
         return out
 
     def embed(self, tokens, weight, scale: float = 1.0, out=None, stream=None):
@@ -343,10 +361,13 @@ class Domino:
         pt = _words(tokens, dev, torch.int32, n, "tokens")
         step = dim
         if out is None:
-            out = self._empty((n, dim), weight.dtype, weight.device)
+            out = self._new((n, dim), weight.dtype, weight.device)
         else:
             step = _like(out, dev, "out", n, dim, code)
-        B.domino_embed(self.h, pt, n, weight.data_ptr(), ws, code, V, dim, scale, out.data_ptr(), step, stream)
+        rc = B.lib().domino_embed(self.h, pt, n, weight.data_ptr(), ws, code, V, dim, scale, out.data_ptr(), step,
+                                  self._raw(stream))
+        if rc:
+            B._check("domino_embed", rc)
         return out
 
     def embed_grad(self, tokens, grad, n_tokens: int, scale: float = 1.0, into=None, stream=None):
@@ -357,11 +378,13 @@ class Domino:
         pt = _words(tokens, dev, torch.int32, n, "tokens")
         dw, step = into, dim
         if dw is None:
-            dw = self._empty((n_tokens, dim), grad.dtype, grad.device)
+            dw = self._new((n_tokens, dim), grad.dtype, grad.device)
         else:
             step = _like(dw, dev, "into", n_tokens, dim, code)
-        B.domino_embed_grad(self.h, pt, n, grad.data_ptr(), gs, code, n_tokens, dim, scale, 0 if into is None else 1,
-                            dw.data_ptr(), step, stream)
+        rc = B.lib().domino_embed_grad(self.h, pt, n, grad.data_ptr(), gs, code, n_tokens, dim, scale,
+                                       0 if into is None else 1, dw.data_ptr(), step, self._raw(stream))
+        if rc:
+            B._check("domino_embed_grad", rc)
         return dw
 
     def device_error(self, stream=None) -> int:
