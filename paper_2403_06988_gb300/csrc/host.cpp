@@ -178,7 +178,9 @@ int dev_reserve(DevBuf& b, size_t n) { return dev_upload(b, nullptr, n); }
 int grow_scratch(domino_ctx* h, DevBuf& of, size_t n) {
     if (of.n >= n) return DOMINO_OK;
     DevBuf b;
-    if (int rc = dev_reserve(b, std::max(n, 2 * of.n))) return rc;
+    int rc = dev_reserve(b, std::max(n, 2 * of.n));
+    if (rc == DOMINO_E_OOM && n < 2 * of.n) rc = dev_reserve(b, n);
+    if (rc) return rc;
     if (of.p) h->fpart_old.push_back(of);
     of = b;
     return DOMINO_OK;

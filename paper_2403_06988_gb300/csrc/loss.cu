@@ -812,7 +812,7 @@ Operand operand(Pack& pack, const void* p, int64_t stride, int32_t rows, int32_t
 }  // namespace
 
 size_t loss_workspace(const LossArgs& a, const LaunchEnv& env, bool grad) {
-    return a.rows <= kFewRows ? few_workspace(a, env, grad) : loss_space(a, env, grad).end;
+    return few_rows(a) ? few_workspace(a, env, grad) : loss_space(a, env, grad).end;
 }
 
 cudaError_t launch_loss_merge(const LossArgs& a, const float2* part, int32_t parts, const float* target_logit,
@@ -827,7 +827,7 @@ bool loss_fits(const LossArgs& a) {
 }
 
 cudaError_t launch_token_loss(const LossArgs& a, const LaunchEnv& env, void* space, cudaStream_t st) {
-    if (a.rows <= kFewRows) return launch_few_loss(a, env, space, st);
+    if (few_rows(a)) return launch_few_loss(a, env, space, st);
     const LossSpace s = loss_space(a, env, false);
     char* ws = (char*)space;
     Prep prep{};
@@ -852,7 +852,7 @@ cudaError_t launch_token_loss(const LossArgs& a, const LaunchEnv& env, void* spa
 }
 
 cudaError_t launch_token_loss_grad(const LossArgs& a, const LaunchEnv& env, void* space, cudaStream_t st) {
-    if (a.rows <= kFewRows) return launch_few_loss_grad(a, env, space, st);
+    if (few_rows(a)) return launch_few_loss_grad(a, env, space, st);
     const LossSpace s = loss_space(a, env, true);
     char* ws = (char*)space;
     Prep prep{};

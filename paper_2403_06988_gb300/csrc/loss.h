@@ -26,8 +26,8 @@ bool loss_fits(const LossArgs& a);
 size_t loss_workspace(const LossArgs& a, const LaunchEnv& env, bool grad);
 cudaError_t launch_token_loss(const LossArgs& a, const LaunchEnv& env, void* space, cudaStream_t st);
 cudaError_t launch_token_loss_grad(const LossArgs& a, const LaunchEnv& env, void* space, cudaStream_t st);
-// Up to kFewRows rows (loss_few.cu).
-constexpr int kFewRows = 4;
+// Few rows (loss_few.cu): whether these are.
+bool few_rows(const LossArgs& a);
 size_t few_workspace(const LossArgs& a, const LaunchEnv& env, bool grad);
 cudaError_t launch_few_loss(const LossArgs& a, const LaunchEnv& env, void* space, cudaStream_t st);
 cudaError_t launch_few_loss_grad(const LossArgs& a, const LaunchEnv& env, void* space, cudaStream_t st);

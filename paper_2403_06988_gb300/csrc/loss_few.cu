@@ -70,12 +70,13 @@ __device__ __forceinline__ float transpose_sum(float (&acc)[32], int lane) {
     return acc[0];
 }
 
-// TN rows of tokens (those beyond the call's are not read).  SINGLE: blocks of one token, whose loads are unrolled along
-// the row; else blocks of up to 32 / TN, four weight rows together.
-template <int TN, bool SINGLE, bool ALIGNED>
+// TN rows of tokens (those beyond the call's are not read).  ROWS: weight rows read together, 1 (blocks of one token, the
+// loads unrolled along the row), 4, or 8 (rows of up to 256 values).
+template <int TN, int ROWS, bool ALIGNED>
 __global__ void __launch_bounds__(kFewThreads, 2) few_logits_kernel(const __grid_constant__ FewCall c) {
     constexpr int kR = 32 / TN;                              // lane l: row l / kR, token l % kR of the block
-    constexpr int kRows = SINGLE ? 1 : 4, kSteps = (ALIGNED ? kFewLoads : kFewLoads / 2) / kRows;
+    constexpr bool SINGLE = ROWS == 1;
+    constexpr int kRows = ROWS, kLoads = ALIGNED ? kFewLoads : kFewLoads / 2, kSteps = kLoads > kRows ? kLoads / kRows : 1;
     __shared__ float2 s_part[kFewWarps][TN];
     const LossArgs& a = c.a;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -188,7 +189,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) few_logits_kernel(const __grid
     }
 }
 
-constexpr int kSumsThreads = 128;
+constexpr int kSumsThreads = 128;          // at most: a warp per 256 columns
 constexpr int kSumsTokens = 64;           // whose G lies in shared memory at a time
 constexpr int kSumsLoads = 8;
 
@@ -210,7 +211,7 @@ __global__ void __launch_bounds__(kSumsThreads) few_sums_kernel(const __grid_con
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31;
-    const int32_t col = (blockIdx.y * kSumsThreads + threadIdx.x) * kN, left = a.dim - col;
+    const int32_t col = (blockIdx.y * blockDim.x + threadIdx.x) * kN, left = a.dim - col;
     const bool on = left > 0;
     const int32_t lo = blockIdx.x * c.strip, hi = min(a.n_tokens, lo + c.strip);
     // rows without a gradient have no part in dweight, whatever they hold: their G is 0
@@ -234,7 +235,7 @@ __global__ void __launch_bounds__(kSumsThreads) few_sums_kernel(const __grid_con
     constexpr int kLoads = ALIGNED ? kSumsLoads : kSumsLoads / 2;
     for (int32_t v0 = lo; v0 < hi; v0 += kSumsTokens) {
         __syncthreads();
-        for (int k = threadIdx.x; k < kSumsTokens * TN; k += kSumsThreads) {
+        for (int k = threadIdx.x; k < kSumsTokens * TN; k += blockDim.x) {
             const int i = k / kSumsTokens, v = k - i * kSumsTokens;
             s_g[v][i] = i < a.rows && v0 + v < hi ? c.g[(int64_t)i * a.n_tokens + v0 + v] : 0.0f;
         }
@@ -333,7 +334,7 @@ bool vectors(const LossArgs& a) {
 
 struct FewSpace {
     int padded;              // rows, to 1, 2 or 4
-    int32_t block, blocks, ctas, strip, strips, pitch;
+    int32_t block, blocks, ctas, threads, stretches, strip, strips, pitch;
     size_t target_logit, g, planes, end;
 };
 
@@ -357,8 +358,9 @@ FewSpace few_space(const LossArgs& a, const LaunchEnv& env, bool grad) {
         take((size_t)a.rows * s.ctas * sizeof(float2));   // part, at 0
         s.target_logit = take((size_t)a.rows * 4);
     } else {
-        const int stretches = (a.dim + kSumsThreads * kN - 1) / (kSumsThreads * kN);
-        const int want = std::max(1, env.num_sms * 4 / stretches);
+        s.threads = std::min(kSumsThreads, (a.dim + 32 * kN - 1) / (32 * kN) * 32);
+        s.stretches = (a.dim + s.threads * kN - 1) / (s.threads * kN);
+        const int want = std::max(1, env.num_sms * 4 * (kSumsThreads / s.threads) / s.stretches);
         s.pitch = (a.dim + kN - 1) / kN * kN;
         s.strip = std::max(16, (a.n_tokens + want - 1) / want);
         s.strips = (a.n_tokens + s.strip - 1) / s.strip;
@@ -369,15 +371,19 @@ FewSpace few_space(const LossArgs& a, const LaunchEnv& env, bool grad) {
     return s;
 }
 
-template <int TN, bool SINGLE>
+template <int TN, int ROWS>
 cudaError_t launch_logits_v(const FewCall& c, int ctas, bool vec, cudaStream_t st) {
     const dim3 grid((unsigned)ctas), block(kFewThreads);
-    return vec ? launch_pdl(few_logits_kernel<TN, SINGLE, true>, grid, block, 0, st, c)
-               : launch_pdl(few_logits_kernel<TN, SINGLE, false>, grid, block, 0, st, c);
+    return vec ? launch_pdl(few_logits_kernel<TN, ROWS, true>, grid, block, 0, st, c)
+               : launch_pdl(few_logits_kernel<TN, ROWS, false>, grid, block, 0, st, c);
 }
 template <int TN>
 cudaError_t launch_few_t(const FewCall& c, int ctas, bool vec, cudaStream_t st) {
-    return c.block == 1 ? launch_logits_v<TN, true>(c, ctas, vec, st) : launch_logits_v<TN, false>(c, ctas, vec, st);
+    if (c.block == 1) return launch_logits_v<TN, 1>(c, ctas, vec, st);
+    // off 16-byte boundaries eight rows' two blocks each do not fit the registers
+    if (vec && c.block >= 8 && c.a.dim <= 32 * kN)
+        return launch_pdl(few_logits_kernel<TN, 8, true>, dim3((unsigned)ctas), dim3(kFewThreads), 0, st, c);
+    return launch_logits_v<TN, 4>(c, ctas, vec, st);
 }
 cudaError_t launch_few(const FewCall& c, const FewSpace& s, cudaStream_t st) {
     const bool vec = vectors(c.a);
@@ -389,9 +395,9 @@ cudaError_t launch_few(const FewCall& c, const FewSpace& s, cudaStream_t st) {
 }
 
 template <int TN>
-cudaError_t launch_sums_t(const FewSums& c, dim3 grid, bool vec, cudaStream_t st) {
-    return vec ? launch_pdl(few_sums_kernel<TN, true>, grid, dim3(kSumsThreads), 0, st, c)
-               : launch_pdl(few_sums_kernel<TN, false>, grid, dim3(kSumsThreads), 0, st, c);
+cudaError_t launch_sums_t(const FewSums& c, dim3 grid, int threads, bool vec, cudaStream_t st) {
+    return vec ? launch_pdl(few_sums_kernel<TN, true>, grid, dim3((unsigned)threads), 0, st, c)
+               : launch_pdl(few_sums_kernel<TN, false>, grid, dim3((unsigned)threads), 0, st, c);
 }
 
 FewCall few_call(const LossArgs& a, const FewSpace& s) {
@@ -404,6 +410,17 @@ FewCall few_call(const LossArgs& a, const FewSpace& s) {
 }
 
 }  // namespace
+
+// One or two rows, and three or four of a small vocabulary (GB300, us few / tensor cores, loss and gradient: 2 rows, V =
+// 32000, 1024 wide 13.9, 38.5 / 17.6, 52.6, V = 128256, 4096 wide 177, 543 / 188, 584; 3 rows, V = 17972, 1472 wide 12.5,
+// 25.3 / 17.1, 49.7; 4 rows, V = 5000, 2048 wide 11.3, 23.6 / 14.8, 34.0, V = 32000, 1024 wide 18.9, 49.9 / 16.8, 52.7, V =
+// 128256, 512 wide 34.8, 126 / 35.3, 92).  Off 16-byte boundaries the tensor cores' operands are laid out first, which
+// takes longer than the products of a large weight: 4 rows, V = 20001, 333 wide 17.2, 51.2 / 16.0, 42.5, 3 rows, V =
+// 39587, 2757 wide 118, 298 / 140, 308.
+bool few_rows(const LossArgs& a) {
+    if (a.rows <= 2 || a.rows > 4) return a.rows <= 2;
+    return vectors(a) ? a.n_tokens <= 20000 : (int64_t)a.n_tokens * a.dim > ((int64_t)1 << 24);
+}
 
 size_t few_workspace(const LossArgs& a, const LaunchEnv& env, bool grad) { return few_space(a, env, grad).end; }
 
@@ -430,13 +447,12 @@ cudaError_t launch_few_loss_grad(const LossArgs& a, const LaunchEnv& env, void* 
     f.pitch = s.pitch;
     f.aligned_out = rows_aligned(a.dweight, a.dweight_stride, a.dim);
     const bool vec = vectors(a);
-    const int width = kSumsThreads * kN;
-    const dim3 grid((unsigned)s.strips, (unsigned)((a.dim + width - 1) / width));
+    const dim3 grid((unsigned)s.strips, (unsigned)s.stretches);
     cudaError_t e;
     switch (s.padded) {
-        case 1: e = launch_sums_t<1>(f, grid, vec, st); break;
-        case 2: e = launch_sums_t<2>(f, grid, vec, st); break;
-        default: e = launch_sums_t<4>(f, grid, vec, st);
+        case 1: e = launch_sums_t<1>(f, grid, s.threads, vec, st); break;
+        case 2: e = launch_sums_t<2>(f, grid, s.threads, vec, st); break;
+        default: e = launch_sums_t<4>(f, grid, s.threads, vec, st);
     }
     if (e != cudaSuccess) return e;
     return launch_pdl(few_hidden_kernel, dim3((unsigned)((a.dim + 31) / 32), (unsigned)a.rows), dim3(kHiddenThreads), 0, st,

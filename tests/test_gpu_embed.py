@@ -187,3 +187,21 @@ def test_bf16_rows_at_every_offset(d, n, V, D):
     ref, tol = embed_grad(t, g, V, 0.5, w)
     assert_within(d.embed_grad(t, g, V, 0.5, into=into), ref, tol, "into")
     assert (big[:5] == 7).all() and (big[5 + V * D:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("off,stride", [(0, 40), (1, 33), (3, 37)])
+def test_table_rows_apart_are_cleared(d, dtype, off, stride):
+    """accumulate = 0 with rows that do not follow each other: every row is written, nothing between them."""
+    n, V, D = 30, 300, 33
+    t, g = tokens(n, V), values(n, D, dtype)
+    want, tol = embed_grad(t, g, V, 2.0)
+    base = torch.full((V * stride + 16,), 7.0, dtype=TYPES[dtype], device="cuda")
+    dw = base[off:off + V * stride].view(V, stride)[:, :D]
+    code = B.DTYPE_BF16 if dtype == "bf16" else B.DTYPE_F32
+    for count in (n, 0):
+        B.domino_embed_grad(d.h, t, count, g, D, code, V, D, 2.0, 0, dw.data_ptr(), stride)
+        assert_within(dw, want if count else torch.zeros_like(want), tol if count else torch.zeros_like(tol), "table")
+        rest = base.clone()
+        rest[off:off + V * stride].view(V, stride)[:, :D] = 7.0
+        assert (rest == 7.0).all()
