@@ -62,12 +62,22 @@ constexpr int kProductSmem = kRingBytes + kFoldWarps * kOutBuffers * kOutBytes +
 constexpr int kProductThreads = 128 + 32 * kFoldWarps;
 constexpr int kGroupM = 16;                    // row tiles that share a pass over the columns' tiles
 
+// A tensor-core sum is cut, not rounded, at every step of 16 products: what it
+// loses grows with the steps.  Logits of more than kDeepBlocks k blocks are
+// summed in parts, each in an accumulator of its own, which are added in fp32
+// (256 x 128256 x 4096: lse 1.9e-6 off in one part of 64 blocks, 4e-7 in parts of
+// 16; 188 us in one part, 199, 196 and 195 in parts of 16, 22 and 32; 4096 rows
+// 2370, 2410, 2384, 2370).  G is rounded to bf16, a thousand times as much: its
+// logits are summed in one.
+constexpr int kDeepBlocks = 24;
+
 // What becomes of a tile of products.
 enum ProductFold : int {
     kFoldLogSum = 0,   // rows of tokens, columns of the vocabulary: (max, sum of exp) and the target's logit
     kFoldGrad = 1,     // the same tile: G, in bf16
     kFoldHidden = 2,   // G w: added to fp32 planes
     kFoldWeight = 3,   // G^T h: the weight's gradient, in bf16
+    kFoldLogSumDeep = 4,   // kFoldLogSum in parts
 };
 
 struct Product {
@@ -199,10 +209,43 @@ __device__ __forceinline__ void put_rows(const CUtensorMap* map, int32_t x, int3
     }
 }
 
+// 32 logits of a row, those that `word` allows, into the row's (m, sum).
+__device__ __forceinline__ void fold_log_sum(float* v, uint32_t word, float& m, float& sum) {
+    if (!__all_sync(0xffffffffu, word == 0xFFFFFFFFu)) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] = (word & (1u << e)) ? v[e] : -INFINITY;
+    }
+    float top = m;
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) top = fmaxf(fmaxf(top, v[e]), v[e + 1]);
+    const float ref = sum_ref(top);
+    float2 s0 = make_float2(sum * exp_diff(m, ref), 0.0f), s1 = make_float2(0.0f, 0.0f);
+    const float2 nref = make_float2(-ref, -ref);
+#pragma unroll
+    for (int e = 0; e < 32; e += 4) {
+        const float2 d0 = mul2(add2(make_float2(v[e], v[e + 1]), nref), kLog2e);
+        const float2 d1 = mul2(add2(make_float2(v[e + 2], v[e + 3]), nref), kLog2e);
+        s0 = add2(s0, make_float2(ex2(d0.x), ex2(d0.y)));
+        s1 = add2(s1, make_float2(ex2(d1.x), ex2(d1.y)));
+    }
+    s0 = add2(s0, s1);
+    sum = s0.x + s0.y;
+    m = top;
+}
+
+// The value at place `at` of 32 (below 32), if this row has it there.
+__device__ __forceinline__ float pick(const float* v, uint32_t at) {
+    float x = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) x = at == (uint32_t)e ? v[e] : x;
+    return x;
+}
+
 template <int FOLD, bool PAIR, int N>
 __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ Product p) {
     using T = Tile<PAIR, N>;
     constexpr int kStages = T::kStages, kColumns = T::kColumns, kTmemColumns = kAccs * N;
+    constexpr bool kDeep = FOLD == kFoldLogSumDeep, kLogSum = FOLD == kFoldLogSum || kDeep;
     extern __shared__ unsigned char smem[];
     __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_acc_full[kAccs], s_acc_empty[kAccs], s_done;
     __shared__ uint32_t s_tmem, s_failed;
@@ -267,23 +310,30 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             const uint32_t step_a = p.a_mn ? 2048 / 16 : 32 / 16, step_b = p.b_mn ? 2048 / 16 : 32 / 16;
             uint32_t loads = 0, accs = 0;
             bool ok = true;
-            for (int32_t i = first; i < p.items && ok; i += step, ++accs) {
+            for (int32_t i = first; i < p.items && ok; i += step) {
                 const Item t = item_at(p, i);
-                const uint32_t s_acc = accs % kAccs, acc = tmem + s_acc * N;
-                if (!(ok = bar_wait(smem_addr(&s_acc_empty[s_acc]), ((accs / kAccs) & 1u) ^ 1u, failed))) break;
-                tcgen_after();
-                for (int32_t k = t.k0; k < t.k1; ++k, ++loads) {
-                    const uint32_t s = loads % kStages;
-                    if (!(ok = bar_wait(smem_addr(&s_full[s]), (loads / kStages) & 1u, failed))) break;
+                for (int32_t k0 = t.k0, k1; ok; k0 = k1, ++accs) {   // an accumulator each
+                    k1 = kDeep ? min(t.k1, k0 + kDeepBlocks) : t.k1;
+                    const uint32_t s_acc = accs % kAccs, acc = tmem + s_acc * N;
+                    if (!(ok = bar_wait(smem_addr(&s_acc_empty[s_acc]), ((accs / kAccs) & 1u) ^ 1u, failed))) break;
                     tcgen_after();
-                    const uint64_t a = operand_desc(tiles + s * T::kStageBytes, kTileK * 128);
-                    const uint64_t b = operand_desc(tiles + s * T::kStageBytes + T::kBytesA, kTileK * 128);
+                    for (int32_t k = k0; k < k1; ++k, ++loads) {
+                        const uint32_t s = loads % kStages;
+                        if (!(ok = bar_wait(smem_addr(&s_full[s]), (loads / kStages) & 1u, failed))) break;
+                        tcgen_after();
+                        const uint64_t a = operand_desc(tiles + s * T::kStageBytes, kTileK * 128);
+                        const uint64_t b = operand_desc(tiles + s * T::kStageBytes + T::kBytesA, kTileK * 128);
 #pragma unroll
-                    for (int j = 0; j < kTileK / 16; ++j)
-                        mma_bf16<PAIR>(acc, a + (uint64_t)(j * step_a), b + (uint64_t)(j * step_b), desc, k > t.k0 || j > 0);
-                    mma_commit<PAIR>(smem_addr(&s_empty[s]));
+                        for (int j = 0; j < kTileK / 16; ++j)
+                            mma_bf16<PAIR>(acc, a + (uint64_t)(j * step_a), b + (uint64_t)(j * step_b), desc, k > k0 || j > 0);
+                        mma_commit<PAIR>(smem_addr(&s_empty[s]));
+                    }
+                    if (ok) mma_commit<PAIR>(smem_addr(&s_acc_full[s_acc]));
+                    if (k1 >= t.k1) {
+                        ++accs;
+                        break;
+                    }
                 }
-                if (ok) mma_commit<PAIR>(smem_addr(&s_acc_full[s_acc]));
             }
             mma_commit<PAIR>(smem_addr(&s_done));
         }
@@ -296,25 +346,65 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         const uint32_t buffers = tiles + kRingBytes + (warp - 4) * kOutBuffers * kOutBytes;
         const int row_in_tile = rank * kRowsM + quarter * 32 + lane;
-        constexpr bool kTokens = FOLD == kFoldLogSum || FOLD == kFoldGrad;
+        constexpr bool kTokens = kLogSum || FOLD == kFoldGrad;
         uint32_t accs = 0, puts = 0;
         Side<kColumns> next{};
         if (kTokens && first < p.items) next = load_side<FOLD, T>(p, first, row_in_tile, half);
         float scale = 1.0f;
         if constexpr (FOLD == kFoldWeight) scale = *p.scale;
-        for (int32_t i = first; i < p.items; i += step, ++accs) {
+        // waits for the next accumulator; the whole warp goes on or leaves: loads from tensor memory are a warp's
+        const auto filled = [&] {
+            const bool ok = __all_sync(0xffffffffu, bar_wait(smem_addr(&s_acc_full[accs % kAccs]), (accs / kAccs) & 1u, failed));
+            tcgen_after();
+            return ok;
+        };
+        const auto columns = [&] { return tmem + (accs % kAccs) * N + half * kColumns + ((uint32_t)(quarter * 32) << 16); };
+        // gives it back
+        const auto emptied = [&] {
+            tcgen_before();
+            __syncwarp();
+            const uint32_t bar = smem_addr(&s_acc_empty[accs % kAccs]);
+            if (lane == 0) {
+                if constexpr (PAIR) bar_arrive_cluster(in_cta(bar, 0));
+                else bar_arrive(bar);
+            }
+            ++accs;
+        };
+        bool ok = true;
+        for (int32_t i = first; i < p.items; i += step) {
             const Item t = item_at(p, i);
-            const uint32_t s_acc = accs % kAccs;
             const int32_t row = t.m * T::kM + row_in_tile, row0 = row - lane, c0 = t.n * N + half * kColumns;
             const bool on = row < p.m;
             // the next tile's are on their way while this one is folded
             const Side<kColumns> side = next;
             if (kTokens && i + step < p.items) next = load_side<FOLD, T>(p, i + step, row_in_tile, half);
-            // the whole warp goes on or leaves: loads from tensor memory are a warp's
-            if (!__all_sync(0xffffffffu, bar_wait(smem_addr(&s_acc_full[s_acc]), (accs / kAccs) & 1u, failed))) break;
-            tcgen_after();
-            const uint32_t acc = tmem + s_acc * N + half * kColumns + ((uint32_t)(quarter * 32) << 16);
             float m = -INFINITY, sum = 0.0f;
+            if constexpr (kDeep) {
+                float x[kColumns];
+#pragma unroll
+                for (int e = 0; e < kColumns; ++e) x[e] = 0.0f;
+                for (int32_t k = t.k0; k < t.k1; k += kDeepBlocks) {
+                    if (!(ok = filled())) break;
+                    const uint32_t acc = columns();
+#pragma unroll
+                    for (int e = 0; e < kColumns; e += 16) tmem_add16(x + e, acc + e);
+                    emptied();
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int j = 0; j < kColumns / 32; ++j) {
+                    const uint32_t at = (uint32_t)side.target - (uint32_t)(c0 + 32 * j);
+                    if (__any_sync(0xffffffffu, at < 32u)) {
+                        const float y = pick(x + 32 * j, at);
+                        if (at < 32u && on) p.target_logit[row] = y;
+                    }
+                    fold_log_sum(x + 32 * j, side.word[j], m, sum);
+                }
+                if (on) p.part[(int64_t)row * p.part_pitch + t.n * (N / kColumns) + half] = make_float2(m, sum);
+                continue;
+            }
+            if (!(ok = filled())) break;
+            const uint32_t acc = columns();
 #pragma unroll 1
             for (int j = 0; j < kColumns / 32; ++j) {
                 const int32_t c = c0 + 32 * j;
@@ -327,31 +417,10 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 const uint32_t at = (uint32_t)side.target - (uint32_t)c;   // below 32: the target's place
                 if constexpr (FOLD == kFoldLogSum) {
                     if (__any_sync(0xffffffffu, at < 32u)) {
-                        float x = 0.0f;
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) x = at == (uint32_t)e ? v[e] : x;
+                        const float x = pick(v, at);
                         if (at < 32u && on) p.target_logit[row] = x;
                     }
-                    if (!__all_sync(0xffffffffu, word == 0xFFFFFFFFu)) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) v[e] = (word & (1u << e)) ? v[e] : -INFINITY;
-                    }
-                    float top = m;
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2) top = fmaxf(fmaxf(top, v[e]), v[e + 1]);
-                    const float ref = sum_ref(top);
-                    float2 s0 = make_float2(sum * exp_diff(m, ref), 0.0f), s1 = make_float2(0.0f, 0.0f);
-                    const float2 nref = make_float2(-ref, -ref);
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
-                        const float2 d0 = mul2(add2(make_float2(v[e], v[e + 1]), nref), kLog2e);
-                        const float2 d1 = mul2(add2(make_float2(v[e + 2], v[e + 3]), nref), kLog2e);
-                        s0 = add2(s0, make_float2(ex2(d0.x), ex2(d0.y)));
-                        s1 = add2(s1, make_float2(ex2(d1.x), ex2(d1.y)));
-                    }
-                    s0 = add2(s0, s1);
-                    sum = s0.x + s0.y;
-                    m = top;
+                    fold_log_sum(v, word, m, sum);
                 } else if constexpr (FOLD == kFoldGrad) {
                     const float2 nlse = make_float2(-side.lse, -side.lse);
 #pragma unroll
@@ -421,12 +490,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             if constexpr (FOLD == kFoldLogSum) {
                 if (on) p.part[(int64_t)row * p.part_pitch + t.n * (N / kColumns) + half] = make_float2(m, sum);
             }
-            tcgen_before();
-            __syncwarp();
-            if (lane == 0) {
-                if constexpr (PAIR) bar_arrive_cluster(in_cta(smem_addr(&s_acc_empty[s_acc]), 0));
-                else bar_arrive(smem_addr(&s_acc_empty[s_acc]));
-            }
+            emptied();
         }
         if (lane == 0) tma_wait_all();
     }
@@ -716,7 +780,7 @@ cudaError_t launch_product_t(const LaunchEnv& env, const Product& p, cudaStream_
 }
 template <int FOLD>
 cudaError_t launch_product(const LaunchEnv& env, Shape shape, const Product& p, cudaStream_t st) {
-    if constexpr (FOLD == kFoldLogSum || FOLD == kFoldGrad)
+    if constexpr (FOLD != kFoldHidden && FOLD != kFoldWeight)
         if (shape == kNarrow) return launch_product_t<FOLD, false, kNarrowN>(env, p, st);
     return shape == kPair ? launch_product_t<FOLD, true, kWideN>(env, p, st) : launch_product_t<FOLD, false, kWideN>(env, p, st);
 }
@@ -847,7 +911,9 @@ cudaError_t launch_token_loss(const LossArgs& a, const LaunchEnv& env, void* spa
     p.part_pitch = s.part_pitch;
     p.target_logit = (float*)(ws + s.target_logit);
     p.err = a.err;
-    if ((e = launch_product<kFoldLogSum>(env, s.logits, p, st)) != cudaSuccess) return e;
+    e = p.k_blocks > kDeepBlocks ? launch_product<kFoldLogSumDeep>(env, s.logits, p, st)
+                                 : launch_product<kFoldLogSum>(env, s.logits, p, st);
+    if (e != cudaSuccess) return e;
     return launch_loss_merge(a, p.part, s.part_pitch, p.target_logit, st);
 }
 
