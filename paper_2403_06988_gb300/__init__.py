@@ -15,64 +15,21 @@ from . import _binding as B
 from ._binding import DominoError, DTYPE_BF16, DTYPE_F32  # noqa: F401
 
 
-_T = None        # torch, and its types' codes, once a method below has been called
-_CODES = {}
+_CALLS = None
 
 
-def _torch():
-    global _T
-    if _T is None:
-        import torch
-        _CODES.update({torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32})
-        _T = torch
-    return _T
+def _calls():
+    """The extension that the losses and the embedding are called through (csrc/calls.cpp), bound to the loaded library."""
+    global _CALLS
+    if _CALLS is None:
+        import ctypes
 
-
-def _matrix(x, device, what):
-    """(rows, columns, elements from a row to the next, type code) of a matrix of contiguous rows on `device`."""
-    if x.dim() != 2:
-        raise ValueError(f"{what}: a matrix expected, not {tuple(x.shape)}")
-    rows, cols = x.shape
-    step, one = x.stride()
-    if one != 1 and cols > 1:
-        raise ValueError(f"{what} rows must be contiguous")
-    code = _CODES.get(x.dtype)
-    if code is None:
-        raise TypeError(f"{what} must be float32 or bfloat16")
-    if x.get_device() != device:
-        raise ValueError(f"{what} must be on the handle's device")
-    return rows, cols, step if rows > 1 else cols, code
-
-
-def _like(x, device, what, rows, cols, code):
-    """Elements from a row of x to the next; x is a matrix of this shape and type."""
-    got = _matrix(x, device, what)
-    if got[0] != rows or got[1] != cols:
-        raise ValueError(f"{what}: shape {(rows, cols)} expected, not {got[:2]}")
-    if got[3] != code:
-        raise TypeError(f"{what} must be of the inputs' type")
-    return got[2]
-
-
-def _words(x, device, dtype, n, what):
-    """The address of n contiguous values of a 4-byte type."""
-    if x.dtype is not dtype:
-        raise TypeError(f"{what} must be {dtype}")
-    if x.numel() != n or not x.is_contiguous():
-        raise ValueError(f"{what}: {n} contiguous values expected, not {tuple(x.shape)}")
-    if x.get_device() != device:
-        raise ValueError(f"{what} must be on the handle's device")
-    return x.data_ptr()
-
-
-def _mask_words(mask, device, rows, n_tokens):
-    if mask is None:
-        return None
-    if mask.shape != (rows, (n_tokens + 31) >> 5) or mask.element_size() != 4 or not mask.is_contiguous():
-        raise ValueError("mask: one contiguous row of ceil(n_tokens / 32) 32-bit words per row expected")
-    if mask.get_device() != device:
-        raise ValueError("mask must be on the handle's device")
-    return mask.data_ptr()
+        import torch  # noqa: F401  (its libraries, before the extension's)
+        from . import _loss_calls as c
+        c.bind(*(ctypes.cast(getattr(B.lib(), "domino_" + n), ctypes.c_void_p).value
+                 for n in ("token_loss", "token_loss_grad", "distill_loss", "distill_grad", "embed", "embed_grad")))
+        _CALLS = c
+    return _CALLS
 
 
 class Domino:
@@ -254,138 +211,75 @@ class Domino:
         return so
 
     # -- losses over the vocabulary, the embedding (no loaded vocabulary needed) -----
-    # These methods call the library themselves: of a small call's time, the host's
-    # is the larger part.
-    def _new(self, shape, dtype, device):
-        return _T.empty(shape, dtype=dtype, device=device) if self.fill_byte is None else self._empty(shape, dtype, device)
+    def _result(self, name, r):
+        if type(r) is int:
+            B._check(name, r)
+        return r
 
-    def _floats(self, out, i, n, like, what):
-        """out[i], or a new fp32 tensor of n values, and its address."""
-        x = None if out is None else out[i]
-        if x is None:
-            x = self._new(n, _T.float32, like.device)
-            return x, x.data_ptr()
-        return x, _words(x, self.device, _T.float32, n, what)
+    def _fill(self, out, rows, cols, dtype, like):
+        """`out`, or with fill_byte the filled tensor that the call would otherwise make itself."""
+        if out is not None or self.fill_byte is None:
+            return out
+        return self._empty(rows if cols is None else (rows, cols), dtype, like.device)
 
-    def _raw(self, stream):
-        """The cudaStream_t of `stream`, or of the handle's device's current one."""
-        return _T._C._cuda_getCurrentRawStream(self.device) if stream is None else B._stream(stream)
-
-    def _loss_inputs(self, hidden, weight, targets, mask):
-        torch, dev = _torch(), self.device
-        rows, dim, hs, code = _matrix(hidden, dev, "hidden")
-        V, wd, ws, wcode = _matrix(weight, dev, "weight")
-        if wd != dim:
-            raise ValueError(f"weight: {dim} columns expected, not {wd}")
-        if wcode != code:
-            raise TypeError("weight must be of hidden's type")
-        return (self.h, hidden.data_ptr(), hs, weight.data_ptr(), ws, code, rows, dim, V,
-                _mask_words(mask, dev, rows, V), _words(targets, dev, torch.int32, rows, "targets"))
+    def _losses(self, out, like):
+        import torch
+        loss, lse = out if out is not None else (None, None)
+        if self.fill_byte is None:
+            return loss, lse
+        n = like.shape[0]
+        return self._fill(loss, n, None, torch.float32, like), self._fill(lse, n, None, torch.float32, like)
 
     def token_loss(self, hidden, weight, targets, mask=None, out=None, stream=None) -> Tuple:
         """Cross entropy of `targets` under the masked softmax of hidden @ weight.T, the logits never kept: (loss,
         lse), fp32 [rows].  hidden [rows, dim], weight [n_tokens, dim] bf16; targets int32 (below 0: none); mask as
         step_mask's or None.  out: (loss, lse) to write to."""
-        args = self._loss_inputs(hidden, weight, targets, mask)
-        loss, pl = self._floats(out, 0, args[6], hidden, "loss")
-        lse, pz = self._floats(out, 1, args[6], hidden, "lse")
-        rc = B.lib().domino_token_loss(*args, pl, pz, self._raw(stream))
-        if rc:
-            B._check("domino_token_loss", rc)
-        return loss, lse
+        loss, lse = self._losses(out, hidden)
+        return self._result("domino_token_loss", _calls().token_loss(
+            self.h, self.device, hidden, weight, targets, mask, loss, lse, None if stream is None else B._stream(stream)))
 
     def token_loss_grad(self, hidden, weight, targets, lse, grad_loss, mask=None, out=None, stream=None) -> Tuple:
         """(dhidden, dweight) of sum(grad_loss * loss), lse as token_loss returned it; in the inputs' type."""
-        args = self._loss_inputs(hidden, weight, targets, mask)
-        code, rows, dim, V = args[5:9]
         dh, dw = out if out is not None else (None, None)
-        hs = ws = dim
-        if dh is None:
-            dh = self._new((rows, dim), hidden.dtype, hidden.device)
-        else:
-            hs = _like(dh, self.device, "dhidden", rows, dim, code)
-        if dw is None:
-            dw = self._new((V, dim), weight.dtype, weight.device)
-        else:
-            ws = _like(dw, self.device, "dweight", V, dim, code)
-        rc = B.lib().domino_token_loss_grad(*args, _words(lse, self.device, _T.float32, rows, "lse"),
-                                            _words(grad_loss, self.device, _T.float32, rows, "grad_loss"),
-                                            dh.data_ptr(), hs, dw.data_ptr(), ws, self._raw(stream))
-        if rc:
-            B._check("domino_token_loss_grad", rc)
-        return dh, dw
-
-    def _distill_inputs(self, logits, teacher, ids, temperature, mask):
-        torch, dev = _torch(), self.device
-        rows, V, step, code = _matrix(logits, dev, "logits")
-        trows, k, tstep, tcode = _matrix(teacher, dev, "teacher")
-        if trows != rows or tstep != k:
-            raise ValueError(f"teacher: {rows} contiguous rows expected")
-        if ids.shape != teacher.shape:
-            raise ValueError("ids must have the teacher's shape")
-        return (self.h, logits.data_ptr(), code, rows, step, V, _mask_words(mask, dev, rows, V), teacher.data_ptr(),
-                tcode, _words(ids, dev, torch.int32, rows * k, "ids"), k, temperature)
+        if self.fill_byte is not None:
+            dh = self._fill(dh, *hidden.shape, hidden.dtype, hidden)
+            dw = self._fill(dw, *weight.shape, weight.dtype, weight)
+        return self._result("domino_token_loss_grad", _calls().token_loss_grad(
+            self.h, self.device, hidden, weight, targets, lse, grad_loss, mask, dh, dw,
+            None if stream is None else B._stream(stream)))
 
     def distill_loss(self, logits, teacher, ids, temperature: float = 1.0, mask=None, out=None, stream=None) -> Tuple:
         """Divergence of the teacher's top logits (teacher, ids [rows, k]; ids below 0: no entry) from the masked
         softmax of logits / temperature, times temperature^2: (loss, lse), fp32 [rows]."""
-        args = self._distill_inputs(logits, teacher, ids, temperature, mask)
-        loss, pl = self._floats(out, 0, args[3], logits, "loss")
-        lse, pz = self._floats(out, 1, args[3], logits, "lse")
-        rc = B.lib().domino_distill_loss(*args, pl, pz, self._raw(stream))
-        if rc:
-            B._check("domino_distill_loss", rc)
-        return loss, lse
+        loss, lse = self._losses(out, logits)
+        return self._result("domino_distill_loss", _calls().distill_loss(
+            self.h, self.device, logits, teacher, ids, temperature, mask, loss, lse,
+            None if stream is None else B._stream(stream)))
 
     def distill_grad(self, logits, teacher, ids, temperature: float, lse, grad_loss, mask=None, out=None, stream=None):
         """d sum(grad_loss * loss) / d logits, in the logits' type; out may be `logits` itself."""
-        args = self._distill_inputs(logits, teacher, ids, temperature, mask)
-        rows, V = args[3], args[5]
-        step = V
-        if out is None:
-            out = self._new((rows, V), logits.dtype, logits.device)
-        else:
-            step = _like(out, self.device, "out", rows, V, args[2])
-        rc = B.lib().domino_distill_grad(*args, _words(lse, self.device, _T.float32, rows, "lse"),
-                                         _words(grad_loss, self.device, _T.float32, rows, "grad_loss"),
-                                         out.data_ptr(), step, self._raw(stream))
-        if rc:
-            B._check("domino_distill_grad", rc)
-        return out
+        if self.fill_byte is not None:
+            out = self._fill(out, *logits.shape, logits.dtype, logits)
+        return self._result("domino_distill_grad", _calls().distill_grad(
+            self.h, self.device, logits, teacher, ids, temperature, lse, grad_loss, mask, out,
+            None if stream is None else B._stream(stream)))
 
     def embed(self, tokens, weight, scale: float = 1.0, out=None, stream=None):
         """scale * weight[tokens], zeros for tokens below 0: [n, dim] of the weight's type."""
-        torch, dev = _torch(), self.device
-        V, dim, ws, code = _matrix(weight, dev, "weight")
-        n = tokens.numel()
-        pt = _words(tokens, dev, torch.int32, n, "tokens")
-        step = dim
-        if out is None:
-            out = self._new((n, dim), weight.dtype, weight.device)
-        else:
-            step = _like(out, dev, "out", n, dim, code)
-        rc = B.lib().domino_embed(self.h, pt, n, weight.data_ptr(), ws, code, V, dim, scale, out.data_ptr(), step,
-                                  self._raw(stream))
-        if rc:
-            B._check("domino_embed", rc)
-        return out
+        if self.fill_byte is not None:
+            out = self._fill(out, tokens.numel(), weight.shape[-1], weight.dtype, weight)
+        return self._result("domino_embed", _calls().embed(
+            self.h, self.device, tokens, weight, scale, out, None if stream is None else B._stream(stream)))
 
     def embed_grad(self, tokens, grad, n_tokens: int, scale: float = 1.0, into=None, stream=None):
         """Gradient of the table [n_tokens, dim]: scale * the sums of grad's rows by token.  into: a gradient that the
         sums are added to (the loss's, for a table that is its weight too)."""
-        torch, dev = _torch(), self.device
-        n, dim, gs, code = _matrix(grad, dev, "grad")
-        pt = _words(tokens, dev, torch.int32, n, "tokens")
-        dw, step = into, dim
-        if dw is None:
-            dw = self._new((n_tokens, dim), grad.dtype, grad.device)
-        else:
-            step = _like(dw, dev, "into", n_tokens, dim, code)
-        rc = B.lib().domino_embed_grad(self.h, pt, n, grad.data_ptr(), gs, code, n_tokens, dim, scale,
-                                       0 if into is None else 1, dw.data_ptr(), step, self._raw(stream))
-        if rc:
-            B._check("domino_embed_grad", rc)
-        return dw
+        out = into
+        if self.fill_byte is not None:
+            out = self._fill(into, n_tokens, grad.shape[-1], grad.dtype, grad)
+        return self._result("domino_embed_grad", _calls().embed_grad(
+            self.h, self.device, tokens, grad, n_tokens, scale, out, into is not None,
+            None if stream is None else B._stream(stream)))
 
     def device_error(self, stream=None) -> int:
         return B.domino_get_device_error(self.h, stream)

@@ -4,6 +4,9 @@ Eight translation units (host.cpp: C ABI and loaders; kernels.cu, rows.cu, logit
 loss.cu, loss_few.cu, distill.cu and embed.cu: kernels) are compiled in parallel and linked into paper_2403_06988_gb300/libdomino.so.
 Objects go to paper_2403_06988_gb300/_build/.
 
+csrc/calls.cpp becomes the Python extension _loss_calls.so beside it (g++, against the
+installed torch's headers and libraries).
+
 build(debug=True) makes libdomino_debug.so instead (objects in _build_debug/),
 compiled with -DDOMINO_DEBUG: every transition-table lookup checks its state,
 class and entry against the table's bounds and reports a violation in the
@@ -24,6 +27,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libdomino.so")
 LIB_DEBUG = os.path.join(PKG, "libdomino_debug.so")
+CALLS = os.path.join(PKG, "_loss_calls.so")
 SOURCES = ["host.cpp", "kernels.cu", "rows.cu", "logits.cu", "loss.cu", "loss_few.cu", "distill.cu", "embed.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
@@ -50,7 +54,37 @@ def up_to_date(lib: str = LIB) -> bool:
     return all(os.path.getmtime(f) <= t for f in _inputs())
 
 
+def build_calls(force: bool = False) -> str:
+    """The Python extension _loss_calls.so."""
+    import importlib.util
+    import sysconfig
+    src = [os.path.join(CSRC, "calls.cpp"), os.path.join(INCLUDE, "domino.h")]
+    if not force and os.path.exists(CALLS) and all(os.path.getmtime(f) <= os.path.getmtime(CALLS) for f in src):
+        return CALLS
+    torch_dir = importlib.util.find_spec("torch").submodule_search_locations[0]
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc())))
+    lib = os.path.join(torch_dir, "lib")
+    tmp = CALLS + f".tmp{os.getpid()}"
+    cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", src[0], "-o", tmp, "-I", INCLUDE,
+           "-I", os.path.join(torch_dir, "include"), "-I", sysconfig.get_paths()["include"],
+           "-I", os.path.join(cuda, "include"), "-L", lib, f"-Wl,-rpath,{lib}", "-ltorch_python", "-ltorch_cpu",
+           "-lc10_cuda", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed for calls.cpp:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, CALLS)
+    return CALLS
+
+
 def build(force: bool = False, verbose: bool = False, extra_flags=(), debug: bool = False) -> str:
+    with concurrent.futures.ThreadPoolExecutor(1) as calls:   # beside the kernels
+        done = calls.submit(build_calls, force)
+        lib = _build_library(force, verbose, extra_flags, debug)
+        done.result()
+    return lib
+
+
+def _build_library(force, verbose, extra_flags, debug) -> str:
     lib = LIB_DEBUG if debug else LIB
     bdir = BUILD + "_debug" if debug else BUILD
     if not force and up_to_date(lib):

@@ -34,3 +34,20 @@ def test_no_handle(host_handle, name):
     with pytest.raises(B.DominoError) as e:
         getattr(B, name)(None, *CALLS[name], stream=0)
     assert e.value.status == -1
+
+
+def test_python_calls_refuse_without_a_device(host_handle):
+    """The extension that Domino's methods go through loads without a GPU; host tensors and bad arguments are refused."""
+    torch = pytest.importorskip("torch")
+    from paper_2403_06988_gb300 import Domino
+    d = Domino(-1)
+    w, t = torch.zeros(4, 8), torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        d.embed(t, w)
+    with pytest.raises(ValueError):
+        d.token_loss(w, w, t)
+    with pytest.raises(TypeError):
+        d.embed(3, w)
+    with pytest.raises(TypeError):
+        d.embed_grad(t, None, 4)
+    d.close()
