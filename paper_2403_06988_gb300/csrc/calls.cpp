@@ -245,8 +245,8 @@ PyObject* distill_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* embed(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded<7>(n, [&]() -> PyObject* {
         const Call c(a, a[6]);
-        const Matrix w = matrix(a[3], c.device, "weight");
         const at::Tensor& t = tensor(a[2], c.device, "tokens");
+        const Matrix w = matrix(a[3], c.device, "weight");
         words(a[2], c.device, at::kInt, t.numel(), "tokens");
         if (t.numel() > INT32_MAX) throw Refused{PyExc_ValueError, "tokens", "too large"};
         const Matrix out = output(a[5], c.device, "out", t.numel(), w.cols, w);
