@@ -446,7 +446,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                     if (row0 < p.m) put_rows(&p.to, c, row0, false, buffers + (puts++ % kOutBuffers) * kOutBytes, lane, w);
                 } else if constexpr (FOLD == kFoldHidden) {
                     // a split of a short piece may have no products: its accumulator holds an earlier tile's
-                    if (t.k0 < t.k1 || !p.add) {
+                    if (row0 < p.m && (t.k0 < t.k1 || !p.add)) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             uint32_t w[16];
@@ -780,7 +780,7 @@ cudaError_t launch_product_t(const LaunchEnv& env, const Product& p, cudaStream_
 }
 template <int FOLD>
 cudaError_t launch_product(const LaunchEnv& env, Shape shape, const Product& p, cudaStream_t st) {
-    if constexpr (FOLD != kFoldHidden && FOLD != kFoldWeight)
+    if constexpr (FOLD != kFoldHidden)
         if (shape == kNarrow) return launch_product_t<FOLD, false, kNarrowN>(env, p, st);
     return shape == kPair ? launch_product_t<FOLD, true, kWideN>(env, p, st) : launch_product_t<FOLD, false, kWideN>(env, p, st);
 }
@@ -853,7 +853,7 @@ LossSpace loss_space(const LossArgs& a, const LaunchEnv& env, bool grad) {
         s.sums = a.rows > kRowsM ? kPair : kWide;
         // few tiles: their sums are split, each part into a plane of its own
         const int64_t tiles = (int64_t)ceil_div(a.rows, shape_m(s.sums)) * ceil_div(a.dim, kWideN);
-        s.splits = (int)std::max<int64_t>(1, std::min<int64_t>(env.num_sms / (s.sums == kPair ? 2 : 1) / tiles, s.piece / kTileK / 4));
+        s.splits = (int)std::max<int64_t>(1, std::min<int64_t>(env.num_sms / (s.sums == kPair ? 2 : 1) / tiles, s.piece / kTileK / 2));
         s.plane_rows = ceil_div(a.rows, shape_m(s.sums)) * shape_m(s.sums);
         s.planes = take((size_t)s.splits * s.plane_rows * s.pitch * 4);
     }
@@ -962,7 +962,9 @@ cudaError_t launch_token_loss_grad(const LossArgs& a, const LaunchEnv& env, void
         d.add = v0 > 0;
         d.err = a.err;
         if ((e = launch_product<kFoldHidden>(env, s.sums, d, st)) != cudaSuccess) return e;
-        const Shape shape_w = n > kRowsM ? kPair : kWide;
+        // few tiles: the fold of a wide one, not its products, is the longer part (31 x 1760 x 219 8.5 us)
+        const bool few = (int64_t)ceil_div(n, kRowsM) * ceil_div(a.dim, kNarrowN) <= env.num_sms;
+        const Shape shape_w = few ? kNarrow : n > kRowsM ? kPair : kWide;
         Product g2{};   // the piece's rows of the weight's gradient
         if ((e = make_map(&g2.a, ws + s.grad, a.rows, width, width, 64)) != cudaSuccess) return e;
         if ((e = make_map(&g2.b, h.p, a.rows, a.dim, h.stride, 64)) != cudaSuccess) return e;
