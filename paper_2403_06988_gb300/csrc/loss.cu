@@ -39,6 +39,7 @@ namespace {
 constexpr int kRowsM = 128, kTileK = 64, kWideN = 256, kNarrowN = 64;
 constexpr int kAccs = 2;                       // accumulators of N columns: of 256, all of tensor memory
 constexpr int kRingBytes = 196608;             // of operand tiles on their way
+constexpr int kMaxStages = 16;                 // k blocks of them
 constexpr int kFoldWarps = 8;
 template <bool PAIR, int N>
 struct Tile {
@@ -46,9 +47,8 @@ struct Tile {
     static constexpr int kM = kRowsM * kCtas, kN = N;
     static constexpr int kRowsB = N / kCtas;           // a CTA's
     static constexpr int kBytesA = kRowsM * kTileK * 2, kBytesB = kRowsB * kTileK * 2;
-    static constexpr int kStageBytes = kBytesA + kBytesB, kStages = kRingBytes / kStageBytes;
     static constexpr int kColumns = N / (kFoldWarps / 4);   // a fold warp's: 32 rows, half of the columns
-    static_assert(kStages * kStageBytes == kRingBytes && kColumns % 32 == 0);
+    static_assert(kRingBytes % (kBytesA + kBytesB) == 0 && kColumns % 32 == 0);
 };
 // Which tiles a launch takes: 256 x 256 of two CTAs, 128 x 256, 128 x 64.
 enum Shape : int { kPair = 0, kWide = 1, kNarrow = 2 };
@@ -86,6 +86,10 @@ struct Product {
     int32_t m, n;                  // valid rows and columns of the product
     int32_t m_tiles, n_tiles, splits, k_blocks;   // k_blocks: of the whole sum, shared out over the splits
     int32_t a_mn, b_mn;            // operands whose rows of memory run along k (MN-major)
+    // Rows of A that a CTA loads, a multiple of 8.  Fewer than kRowsM where the product has fewer: a product then reads
+    // what lies behind them in shared memory, into rows of the accumulator that nothing uses, and the ring holds more
+    // k blocks (5 rows, V = 7040, 2640 wide: 20.0 us with 8 blocks on their way).
+    int32_t a_rows;
     int32_t items;                 // m_tiles * n_tiles * splits
     // kFoldLogSum, kFoldGrad
     const uint32_t* mask;          // at the first column's word; nullptr: everything allowed
@@ -178,8 +182,9 @@ __device__ __forceinline__ Side<T::kColumns> load_side(const Product& p, int32_t
     s.lse = FOLD == kFoldGrad && on ? p.lse[row] : 0.0f;
     s.coef = FOLD == kFoldGrad && on ? p.coef[row] : 0.0f;
     const uint32_t* mrow = p.mask && on ? p.mask + (int64_t)row * p.mask_words : nullptr;
+    // a row that is none does not slow its warp's others down
 #pragma unroll
-    for (int j = 0; j < T::kColumns / 32; ++j) s.word[j] = on ? allowed_word(mrow, c0 + 32 * j, p.n) : 0u;
+    for (int j = 0; j < T::kColumns / 32; ++j) s.word[j] = on ? allowed_word(mrow, c0 + 32 * j, p.n) : 0xFFFFFFFFu;
     return s;
 }
 
@@ -244,19 +249,21 @@ __device__ __forceinline__ float pick(const float* v, uint32_t at) {
 template <int FOLD, bool PAIR, int N>
 __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ Product p) {
     using T = Tile<PAIR, N>;
-    constexpr int kStages = T::kStages, kColumns = T::kColumns, kTmemColumns = kAccs * N;
+    constexpr int kColumns = T::kColumns, kTmemColumns = kAccs * N;
     constexpr bool kDeep = FOLD == kFoldLogSumDeep, kLogSum = FOLD == kFoldLogSum || kDeep;
     extern __shared__ unsigned char smem[];
-    __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_acc_full[kAccs], s_acc_empty[kAccs], s_done;
+    __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_acc_full[kAccs], s_acc_empty[kAccs], s_done;
     __shared__ uint32_t s_tmem, s_failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t tiles = (smem_addr(smem) + 1023u) & ~1023u;
     const uint32_t rank = PAIR ? cluster_rank() : 0u;
     const int32_t first = blockIdx.x / T::kCtas, step = gridDim.x / T::kCtas;   // items of this CTA or pair
     volatile uint32_t* failed = &s_failed;
+    const uint32_t bytes_a = p.a_rows * kTileK * 2, stage_bytes = bytes_a + T::kBytesB;
+    const uint32_t stages = min((uint32_t)kMaxStages, kRingBytes / stage_bytes);
     if (threadIdx.x == 0) {
         s_failed = 0u;
-        for (int s = 0; s < kStages; ++s) {
+        for (int s = 0; s < kMaxStages; ++s) {
             bar_init(smem_addr(&s_full[s]), 1);
             bar_init(smem_addr(&s_empty[s]), 1);
         }
@@ -279,63 +286,72 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     pdl_trigger();
 
     if (warp == 0) {   // ---- loads: each CTA its part of the tiles; the first CTA's barriers count the bytes of both
-        if (lane == 0) {
-            uint32_t loads = 0;
-            bool ok = true;
-            for (int32_t i = first; i < p.items && ok; i += step) {
-                const Item t = item_at(p, i);
-                const int32_t row_a = t.m * T::kM + rank * kRowsM, row_b = t.n * N + rank * T::kRowsB;
-                for (int32_t k = t.k0; k < t.k1; ++k, ++loads) {
-                    const uint32_t s = loads % kStages, turn = loads / kStages;
-                    if (!(ok = bar_wait(smem_addr(&s_empty[s]), (turn & 1u) ^ 1u, failed))) break;
-                    const uint32_t mine = smem_addr(&s_full[s]), a = tiles + s * T::kStageBytes;
-                    const uint32_t full = PAIR ? in_cta(mine, 0) : mine;
-                    if (rank == 0) bar_expect(mine, T::kStageBytes * T::kCtas);
+        uint32_t s = 0, turn = 0, loads = 0;   // the stage, how often the ring has come round
+        bool ok = true;
+        for (int32_t i = first; i < p.items && ok; i += step) {
+            const Item t = item_at(p, i);
+            const int32_t row_a = t.m * T::kM + rank * kRowsM, row_b = t.n * N + rank * T::kRowsB;
+            for (int32_t k = t.k0; k < t.k1; ++k) {
+                if (!(ok = warp_wait(smem_addr(&s_empty[s]), (turn & 1u) ^ 1u, failed))) break;
+                const uint32_t mine = smem_addr(&s_full[s]), a = tiles + s * stage_bytes;
+                const uint32_t full = PAIR ? in_cta(mine, 0) : mine;
+                if (elect_lane()) {
+                    if (rank == 0) bar_expect(mine, stage_bytes * T::kCtas);
                     load_tile<PAIR>(a, &p.a, p.a_mn, kRowsM, row_a, k * kTileK, full);
-                    load_tile<PAIR>(a + T::kBytesA, &p.b, p.b_mn, T::kRowsB, row_b, k * kTileK, full);
+                    load_tile<PAIR>(a + bytes_a, &p.b, p.b_mn, T::kRowsB, row_b, k * kTileK, full);
+                }
+                ++loads;
+                if (++s == stages) {
+                    s = 0;
+                    ++turn;
                 }
             }
-            // given up: the loads on their way write into this CTA's memory
-            if (!ok && rank == 0)
-                for (uint32_t s = 0; s < (uint32_t)kStages && s < loads; ++s) {
-                    const uint32_t last = loads - 1 - s;   // the stages' last loads
-                    const uint64_t end = timer_ns() + kWaitNs;
-                    while (!bar_try(smem_addr(&s_full[last % kStages]), (last / kStages) & 1u) && timer_ns() < end) {}
-                }
         }
+        // given up: the loads on their way write into this CTA's memory
+        if (!ok && rank == 0 && lane == 0)
+            for (uint32_t j = 1; j <= stages && j <= loads; ++j) {
+                const uint32_t last = loads - j;   // the stages' last loads
+                const uint64_t end = timer_ns() + kWaitNs;
+                while (!bar_try(smem_addr(&s_full[last % stages]), (last / stages) & 1u) && timer_ns() < end) {}
+            }
     } else if (warp == 1) {   // ---- products
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             const uint32_t desc = mma_desc(T::kM, N, p.a_mn, p.b_mn);
             // 16 k further: 32 bytes along a row of a K-major tile, 16 rows of an MN-major one (16-byte units)
             const uint32_t step_a = p.a_mn ? 2048 / 16 : 32 / 16, step_b = p.b_mn ? 2048 / 16 : 32 / 16;
-            uint32_t loads = 0, accs = 0;
+            uint32_t s = 0, turn = 0, accs = 0;
             bool ok = true;
             for (int32_t i = first; i < p.items && ok; i += step) {
                 const Item t = item_at(p, i);
                 for (int32_t k0 = t.k0, k1; ok; k0 = k1, ++accs) {   // an accumulator each
                     k1 = kDeep ? min(t.k1, k0 + kDeepBlocks) : t.k1;
                     const uint32_t s_acc = accs % kAccs, acc = tmem + s_acc * N;
-                    if (!(ok = bar_wait(smem_addr(&s_acc_empty[s_acc]), ((accs / kAccs) & 1u) ^ 1u, failed))) break;
+                    if (!(ok = warp_wait(smem_addr(&s_acc_empty[s_acc]), ((accs / kAccs) & 1u) ^ 1u, failed))) break;
                     tcgen_after();
-                    for (int32_t k = k0; k < k1; ++k, ++loads) {
-                        const uint32_t s = loads % kStages;
-                        if (!(ok = bar_wait(smem_addr(&s_full[s]), (loads / kStages) & 1u, failed))) break;
+                    for (int32_t k = k0; k < k1; ++k) {
+                        if (!(ok = warp_wait(smem_addr(&s_full[s]), turn & 1u, failed))) break;
                         tcgen_after();
-                        const uint64_t a = operand_desc(tiles + s * T::kStageBytes, kTileK * 128);
-                        const uint64_t b = operand_desc(tiles + s * T::kStageBytes + T::kBytesA, kTileK * 128);
+                        const uint64_t a = operand_desc(tiles + s * stage_bytes, kTileK * 128);
+                        const uint64_t b = operand_desc(tiles + s * stage_bytes + bytes_a, kTileK * 128);
+                        if (elect_lane()) {
 #pragma unroll
-                        for (int j = 0; j < kTileK / 16; ++j)
-                            mma_bf16<PAIR>(acc, a + (uint64_t)(j * step_a), b + (uint64_t)(j * step_b), desc, k > k0 || j > 0);
-                        mma_commit<PAIR>(smem_addr(&s_empty[s]));
+                            for (int j = 0; j < kTileK / 16; ++j)
+                                mma_bf16<PAIR>(acc, a + (uint64_t)(j * step_a), b + (uint64_t)(j * step_b), desc, k > k0 || j > 0);
+                            mma_commit<PAIR>(smem_addr(&s_empty[s]));
+                        }
+                        if (++s == stages) {
+                            s = 0;
+                            ++turn;
+                        }
                     }
-                    if (ok) mma_commit<PAIR>(smem_addr(&s_acc_full[s_acc]));
+                    if (ok && elect_lane()) mma_commit<PAIR>(smem_addr(&s_acc_full[s_acc]));
                     if (k1 >= t.k1) {
                         ++accs;
                         break;
                     }
                 }
             }
-            mma_commit<PAIR>(smem_addr(&s_done));
+            if (elect_lane()) mma_commit<PAIR>(smem_addr(&s_done));
         }
         // no product, and no arrival at a barrier of this CTA, may be on its way when the CTA ends
         if (lane == 0) {
@@ -354,7 +370,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         if constexpr (FOLD == kFoldWeight) scale = *p.scale;
         // waits for the next accumulator; the whole warp goes on or leaves: loads from tensor memory are a warp's
         const auto filled = [&] {
-            const bool ok = __all_sync(0xffffffffu, bar_wait(smem_addr(&s_acc_full[accs % kAccs]), (accs / kAccs) & 1u, failed));
+            const bool ok = warp_wait(smem_addr(&s_acc_full[accs % kAccs]), (accs / kAccs) & 1u, failed);
             tcgen_after();
             return ok;
         };
@@ -748,12 +764,16 @@ cudaError_t make_plane_map(CUtensorMap* map, void* base, int64_t rows, int64_t c
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
+// Rows of a K-major A that a CTA loads.
+int rows_loaded(Shape shape, int32_t m) { return shape == kPair ? kRowsM : std::min(kRowsM, (m + 7) / 8 * 8); }
+
 void cut_product(Product& p, Shape shape, int32_t m, int32_t n, int64_t k, int splits) {
     p.m = m;
     p.n = n;
     p.m_tiles = ceil_div(m, shape_m(shape));
     p.n_tiles = ceil_div(n, shape_n(shape));
     p.k_blocks = ceil_div(k, kTileK);
+    p.a_rows = rows_loaded(shape, m);
     p.splits = splits;
     p.items = p.m_tiles * p.n_tiles * splits;
 }
@@ -901,7 +921,7 @@ cudaError_t launch_token_loss(const LossArgs& a, const LaunchEnv& env, void* spa
     if (prep.pack[0].rows || prep.pack[1].rows) e = launch_prep(env, prep, st);
     if (e != cudaSuccess) return e;
     Product p{};
-    if ((e = make_map(&p.a, h.p, a.rows, a.dim, h.stride, kRowsM)) != cudaSuccess) return e;
+    if ((e = make_map(&p.a, h.p, a.rows, a.dim, h.stride, rows_loaded(s.logits, a.rows))) != cudaSuccess) return e;
     if ((e = make_map(&p.b, w.p, a.n_tokens, a.dim, w.stride, shape_box(s.logits))) != cudaSuccess) return e;
     cut_product(p, s.logits, a.rows, a.n_tokens, a.dim, 1);
     p.mask = a.mask;
@@ -939,7 +959,7 @@ cudaError_t launch_token_loss_grad(const LossArgs& a, const LaunchEnv& env, void
         const int32_t n = std::min(s.piece, a.n_tokens - v0), width = ceil_div(n, kWideN) * kWideN;
         const char* wp = (const char*)w.p + (int64_t)v0 * w.stride * 2;
         Product g{};   // G of the piece, [rows][width]
-        if ((e = make_map(&g.a, h.p, a.rows, a.dim, h.stride, kRowsM)) != cudaSuccess) return e;
+        if ((e = make_map(&g.a, h.p, a.rows, a.dim, h.stride, rows_loaded(s.logits, a.rows))) != cudaSuccess) return e;
         if ((e = make_map(&g.b, wp, n, a.dim, w.stride, shape_box(s.logits))) != cudaSuccess) return e;
         cut_product(g, s.logits, a.rows, n, a.dim, 1);
         g.mask = a.mask ? a.mask + v0 / 32 : nullptr;
@@ -952,7 +972,7 @@ cudaError_t launch_token_loss_grad(const LossArgs& a, const LaunchEnv& env, void
         g.err = a.err;
         if ((e = launch_product<kFoldGrad>(env, s.logits, g, st)) != cudaSuccess) return e;
         Product d{};   // its part of the hidden gradient
-        if ((e = make_map(&d.a, ws + s.grad, a.rows, width, width, kRowsM)) != cudaSuccess) return e;
+        if ((e = make_map(&d.a, ws + s.grad, a.rows, width, width, rows_loaded(s.sums, a.rows))) != cudaSuccess) return e;
         if ((e = make_map(&d.b, wp, n, a.dim, w.stride, 64)) != cudaSuccess) return e;
         cut_product(d, s.sums, a.rows, a.dim, n, s.splits);
         d.b_mn = 1;
@@ -970,6 +990,7 @@ cudaError_t launch_token_loss_grad(const LossArgs& a, const LaunchEnv& env, void
         if ((e = make_map(&g2.b, h.p, a.rows, a.dim, h.stride, 64)) != cudaSuccess) return e;
         cut_product(g2, shape_w, n, a.dim, a.rows, 1);
         g2.a_mn = g2.b_mn = 1;
+        g2.a_rows = kRowsM;   // its loads are of 64 rows of m each
         __nv_bfloat16* rows = (__nv_bfloat16*)a.dweight + (int64_t)v0 * a.dweight_stride;
         if (tma_ready(a.dweight, a.dweight_stride)) {
             if ((e = make_out_map(&g2.to, rows, n, a.dim, a.dweight_stride)) != cudaSuccess) return e;

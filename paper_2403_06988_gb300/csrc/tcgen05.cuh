@@ -79,6 +79,23 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
     return true;
 }
 
+// One lane of a converged warp.  Loads, products and commits are issued inside of `if (elect_lane())`, by a warp that
+// runs its loops whole: their addresses and descriptors then stay in uniform registers.  (A loop of one lane's own took
+// 540 cycles to issue a k block's two loads and 650 its four products and commit.)
+__device__ __forceinline__ bool elect_lane() {
+    uint32_t p;
+    asm volatile(
+        "{\n.reg .pred q;\n"
+        "elect.sync _|q, 0xffffffff;\n"
+        "selp.u32 %0, 1, 0, q;\n}\n"
+        : "=r"(p));
+    return p != 0;
+}
+// bar_wait by a whole warp, which goes on or leaves as one.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* failed) {
+    return __all_sync(0xffffffffu, bar_wait(bar, parity, failed));
+}
+
 // A box of the tensor that `map` describes, its corner at (x, y), into shared
 // memory at `dst`; `bar` counts its bytes.  x is a multiple of 16 bytes.
 // PAIR: `bar` may be the other CTA's of a pair (its address in the cluster).
