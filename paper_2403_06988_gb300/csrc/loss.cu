@@ -66,8 +66,8 @@ constexpr int kGroupM = 16;                    // row tiles that share a pass ov
 // loses grows with the steps.  Logits of more than kDeepBlocks k blocks are
 // summed in parts, each in an accumulator of its own, which are added in fp32
 // (256 x 128256 x 4096: lse 1.9e-6 off in one part of 64 blocks, 4e-7 in parts of
-// 16; 188 us in one part, 199, 196 and 195 in parts of 16, 22 and 32; 4096 rows
-// 2370, 2410, 2384, 2370).  G is rounded to bf16, a thousand times as much: its
+// 16, 6e-7 of 24; 184 us in one part, 193, 192 and 192 in parts of 16, 24 and 32; 4096
+// rows 2060, 2120, 2100, 2064).  G is rounded to bf16, a thousand times as much: its
 // logits are summed in one.
 constexpr int kDeepBlocks = 24;
 
@@ -88,7 +88,7 @@ struct Product {
     int32_t a_mn, b_mn;            // operands whose rows of memory run along k (MN-major)
     // Rows of A that a CTA loads, a multiple of 8.  Fewer than kRowsM where the product has fewer: a product then reads
     // what lies behind them in shared memory, into rows of the accumulator that nothing uses, and the ring holds more
-    // k blocks (5 rows, V = 7040, 2640 wide: 20.0 us with 8 blocks on their way).
+    // k blocks (5 rows, V = 32000, 1024 wide: 16.2 us with 4 blocks on their way, 12.7 with 5).
     int32_t a_rows;
     int32_t items;                 // m_tiles * n_tiles * splits
     // kFoldLogSum, kFoldGrad
@@ -487,6 +487,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                         put_words(buffer, lane, w);
                         __syncwarp();
                         const uint32_t chunk = (uint32_t)lane >> 3, byte = (lane & 7) * 2;
+                        uint16_t* to = reinterpret_cast<uint16_t*>(p.out) + (int64_t)row0 * p.ld + c + lane;
+                        const int rows = c + lane < p.n ? min(32, p.m - row0) : 0;
 #pragma unroll
                         for (int r0 = 0; r0 < 32; r0 += 8) {
                             uint16_t x[8];
@@ -496,9 +498,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                                              : "=h"(x[r - r0])
                                              : "r"(buffer + r * 64 + ((chunk ^ ((r >> 1) & 3)) << 4) + byte));
 #pragma unroll
-                            for (int r = r0; r < r0 + 8; ++r)
-                                if (row0 + r < p.m && c + lane < p.n)
-                                    reinterpret_cast<uint16_t*>(p.out + (int64_t)(row0 + r) * p.ld)[c + lane] = x[r - r0];
+                            for (int r = r0; r < r0 + 8; ++r, to += p.ld)
+                                if (r < rows) *to = x[r - r0];
                         }
                     }
                 }
@@ -832,14 +833,14 @@ constexpr int64_t kGradBytes = (int64_t)256 << 20;
 // The tiles of the logits of `rows` rows and `n` tokens.  Pairs of CTAs have
 // tiles of 256 rows: not where that leaves a quarter or more of the last of few
 // tiles empty (GB300, us single / pairs, loss and gradient: 256 rows, V =
-// 128256, 4096 wide 208, 732 / 192, 656; 777 rows, V = 32003, 1024 wide 44, 148 /
-// 53, 151; 1024 rows, V = 65536, 1024 wide 94, 320 / 94, 287; 4096 rows, V =
-// 128256, 4096 wide 2440, 8420 / 2440, 7900).  Rows off 128-byte lines (each of
-// TMA's 128 bytes takes two lines) gain more by reading less: 777 rows, 1000 wide 66,
-// 186 / 58, 168.  Narrow tiles where every SM has at most one: a k block takes
-// them nearly as long as wide ones (us wide / narrow: 300 rows, V = 2000, 256 wide 8.2,
-// 23.4 / 6.6, 21.7; 64 rows, V = 8000, 4096 wide 25.2, 68.7 / 24.9, 59.0; two rounds of
-// them, 64 rows, V = 12000, 512 wide 9.2, 28.0 / 12.0, 30.5).
+// 128256, 4096 wide 214, 641 / 192, 607; 300 rows, V = 32003, 1024 wide 23.1, 90 /
+// 28.3, 93; 777 rows 37.9, 137 / 42.5, 134; 1024 rows, V = 65536 91.7, 277 / 79.1,
+// 260; 2000 rows, V = 32003, 512 wide 60.0, 170 / 53.7, 169).  Rows off 128-byte
+// lines (each of TMA's 128 bytes takes two lines) gain more by reading less: 777
+// rows, 1000 wide 65.9, 167 / 62.0, 157.  Narrow tiles where every SM has at most one:
+// a k block takes them nearly as long as wide ones (us wide / narrow: 300 rows, V =
+// 2000, 256 wide 8.1, 21.1 / 6.3, 19.6; 64 rows, V = 8000, 4096 wide 23.6, 64.1 / 21.7,
+// 54.2; two rounds of them, 64 rows, V = 12000, 512 wide 9.2, 28.0 / 12.0, 30.5).
 Shape logits_shape(const LaunchEnv& env, int32_t rows, int64_t n, bool off_lines) {
     const int tiles = ceil_div(rows, kRowsM);
     if ((int64_t)tiles * ceil_div(n, kNarrowN) <= env.num_sms) return kNarrow;
