@@ -411,15 +411,19 @@ FewCall few_call(const LossArgs& a, const FewSpace& s) {
 
 }  // namespace
 
-// One or two rows, and three or four of a small vocabulary (GB300, us few / tensor cores, loss and gradient: 2 rows, V =
-// 32000, 1024 wide 13.9, 38.5 / 17.6, 52.6, V = 128256, 4096 wide 177, 543 / 188, 584; 3 rows, V = 17972, 1472 wide 12.5,
-// 25.3 / 17.1, 49.7; 4 rows, V = 5000, 2048 wide 11.3, 23.6 / 14.8, 34.0, V = 32000, 1024 wide 18.9, 49.9 / 16.8, 52.7, V =
-// 128256, 512 wide 34.8, 126 / 35.3, 92).  Off 16-byte boundaries the tensor cores' operands are laid out first, which
-// takes longer than the products of a large weight: 4 rows, V = 20001, 333 wide 17.2, 51.2 / 16.0, 42.5, 3 rows, V =
-// 39587, 2757 wide 118, 298 / 140, 308.
+// One or two rows: as fast as the tensor cores over dense masks (GB300, us few / tensor cores, loss and gradient together: 2
+// rows, V = 2000, 256 wide 18.5 / 21.2, V = 32000, 1024 wide 53 / 61, V = 128256, 2048 wide 376 / 352, 4096 wide 726 / 657),
+// and weight rows that no mask allows are not read (V = 128256, 2048 wide, sparse masks 123 / 353).  Three and four rows
+// without a mask only where the launches are what counts (4 rows, V = 2000, 512 wide 20 / 23, V = 5000, 2048 wide 39 / 42, V =
+// 20000, 1024 wide 58 / 44).  With one, sparse masks decide, unless the weight is so large that a dense one would cost twice
+// (V = 20000, 1024 wide 38 / 45, 3 rows, V = 14000, 2048 wide 44 / 62; dense: V = 32000, 1024 wide 84 / 61, V = 20000, 4096
+// wide 225 / 133); off 16-byte boundaries the tensor cores' operands are laid out first, which takes longer than the products
+// of a large weight (4 rows, V = 39587, 1001 wide 86 / 143, V = 128256, 2049 wide 690 / 904; V = 20001, 333 wide 56 / 46).
 bool few_rows(const LossArgs& a) {
     if (a.rows <= 2 || a.rows > 4) return a.rows <= 2;
-    return vectors(a) ? a.n_tokens <= 20000 : (int64_t)a.n_tokens * a.dim > ((int64_t)1 << 24);
+    const int64_t values = (int64_t)a.n_tokens * a.dim;
+    if (!a.mask) return vectors(a) && values <= (10 << 20);
+    return vectors(a) ? values <= (28 << 20) : values > (1 << 24);
 }
 
 size_t few_workspace(const LossArgs& a, const LaunchEnv& env, bool grad) { return few_space(a, env, grad).end; }

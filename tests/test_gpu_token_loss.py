@@ -64,6 +64,12 @@ def test_loss_and_gradient(d, T, V, D, density):
     check(d, *inputs(T, V, D, density=density), f"{T} x {V} x {D}")
 
 
+@pytest.mark.parametrize("T,V,D", [(2, 33001, 517), (3, 9000, 1904), (3, 33001, 517), (4, 5000, 2048), (4, 33001, 517)])
+@pytest.mark.parametrize("density", [None, 0.02, 0.7])
+def test_few_rows_of_a_large_weight(d, T, V, D, density):
+    check(d, *inputs(T, V, D, density=density), f"{T} x {V} x {D}")
+
+
 def test_several_pieces_of_the_vocabulary(d):
     """G of 2100 x 65600 tokens passes what is kept at a time; the last piece is short."""
     check(d, *inputs(2100, 65600, 64, density=0.3), "pieces")
