@@ -388,7 +388,9 @@ int domino_mask_logits_noalloc(const void* logits_dev, int32_t dtype, int32_t ba
  * vocabulary or automaton: n_tokens (V) is an argument, 1 <= V <= 2^24, and masks
  * are [rows][ceil(V/32)] words as written by domino_step_mask; NULL allows
  * every token.  Bits at or beyond V are ignored.  rows = 0 is allowed (a weight's
- * gradient is then zero).  Scratch is the handle's and grows on demand: the
+ * gradient is then zero); domino_token_loss, its gradient and
+ * domino_embed_grad take at most 2^31 - 2^20 - 1 rows (above:
+ * DOMINO_E_UNSUPPORTED).  Scratch is the handle's and grows on demand: the
  * first call at larger sizes must not run under a stream capture
  * (DOMINO_E_INVALID_ARG; the calls that need no scratch are marked).  All sums
  * are held in fp32 and every result is the same on every run.  A target, teacher

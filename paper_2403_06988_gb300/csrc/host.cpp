@@ -1985,7 +1985,7 @@ int token_loss_args(LossArgs& a, domino_ctx* h, const void* hidden, int64_t hidd
     a.mask = mask;
     a.targets = targets;
     a.err = (uint32_t*)h->d_err.p;
-    return rows == 0 || loss_fits(a) ? DOMINO_OK : DOMINO_E_UNSUPPORTED;
+    return rows == 0 || (rows <= kMaxRows && loss_fits(a)) ? DOMINO_OK : DOMINO_E_UNSUPPORTED;
 }
 
 int distill_args(DistillArgs& a, domino_ctx* h, const void* logits, int32_t dtype, int32_t rows, int64_t stride,
@@ -2137,6 +2137,7 @@ int domino_embed_grad(domino_t h, const int32_t* tokens_dev, int32_t n, const vo
         (accumulate != 0 && accumulate != 1) || grad_stride < dim || dweight_stride < dim || !dweight_dev ||
         (n > 0 && (!tokens_dev || !grad_dev)))
         return DOMINO_E_INVALID_ARG;
+    if (n > kMaxRows) return DOMINO_E_UNSUPPORTED;
     EmbedArgs a{};
     a.tokens = tokens_dev;
     a.n = n;

@@ -5,6 +5,10 @@
 
 namespace domino {
 
+// Rows of tokens, and tokens of a list: the kernels count them in 32 bits, in steps of a tile, a chunk (2^19 at most) or a
+// CTA's threads beyond the last.
+constexpr int32_t kMaxRows = INT32_MAX - (1 << 20);
+
 // Cross entropy under the masked softmax of hidden . weight^T.
 struct LossArgs {
     const void* hidden;        // bf16 [rows][hidden_stride]
@@ -21,7 +25,7 @@ struct LossArgs {
     int64_t dhidden_stride, dweight_stride;
     uint32_t* err;
 };
-// rows, dim and n_tokens at least 1; tma_ready() operands need no copy.
+// rows, dim and n_tokens at least 1, at most kMaxRows rows; tma_ready() operands need no copy.
 bool loss_fits(const LossArgs& a);
 size_t loss_workspace(const LossArgs& a, const LaunchEnv& env, bool grad);
 cudaError_t launch_token_loss(const LossArgs& a, const LaunchEnv& env, void* space, cudaStream_t st);
