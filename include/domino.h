@@ -395,7 +395,9 @@ int domino_mask_logits_noalloc(const void* logits_dev, int32_t dtype, int32_t ba
  * (DOMINO_E_INVALID_ARG; the calls that need no scratch are marked).  All sums
  * are held in fp32 and every result is the same on every run.  A target, teacher
  * id or token at or beyond V sets DOMINO_DEVERR_BAD_TOKEN and counts as below
- * 0.  Inputs and outputs do not overlap unless said otherwise. */
+ * 0.  Inputs and outputs do not overlap unless said otherwise.  Pointers are
+ * multiples of their values' size, 2 bytes for bf16 and 4 for everything else
+ * (DOMINO_E_INVALID_ARG); rows need no more than that. */
 
 /* Cross entropy of target tokens under the masked softmax of hidden . weight^T,
  * without keeping the logits:
@@ -436,7 +438,7 @@ int domino_token_loss_grad(domino_t h, const void* hidden_dev, int64_t hidden_st
  * softmax(logits / temperature) over the allowed tokens:
  *   lse[t]  = log sum exp(logits / temperature),
  *   loss[t] = temperature^2 sum_i p_i (ln p_i - ln q[id_i]); 0 without entries.
- * logits_dev [rows][row_stride_elems] of dtype (fp32 or bf16), any alignment.
+ * logits_dev [rows][row_stride_elems] of dtype (fp32 or bf16).
  * 1 <= k <= 1024, temperature > 0 and finite, its inverse too.  lse_dev may be
  * NULL.  Logits of masked tokens are not used.  Needs no scratch. */
 int domino_distill_loss(domino_t h, const void* logits_dev, int32_t dtype, int32_t rows, int64_t row_stride_elems,

@@ -1951,6 +1951,13 @@ constexpr int32_t kMaxTokens = 1 << 24, kMaxDim = 1 << 20;
 
 bool is_dtype(int32_t t) { return t == DOMINO_DTYPE_F32 || t == DOMINO_DTYPE_BF16; }
 
+// Values of `size` bytes may be read or written one by one from p on.
+bool on_values(const void* p, size_t size) { return reinterpret_cast<uintptr_t>(p) % size == 0; }
+bool on_words(const void* a, const void* b = nullptr, const void* c = nullptr, const void* d = nullptr) {
+    return on_values(a, 4) && on_values(b, 4) && on_values(c, 4) && on_values(d, 4);
+}
+size_t type_size(int32_t dtype) { return dtype == DOMINO_DTYPE_BF16 ? 2 : 4; }
+
 int device_handle(domino_ctx* h) {
     if (!h) return DOMINO_E_INVALID_ARG;
     return is_host_only(h) ? DOMINO_E_NO_DEVICE : DOMINO_OK;
@@ -1971,7 +1978,8 @@ int token_loss_args(LossArgs& a, domino_ctx* h, const void* hidden, int64_t hidd
                     const uint32_t* mask, const int32_t* targets) {
     if (int rc = device_handle(h)) return rc;
     if (!is_dtype(dtype) || rows < 0 || dim < 1 || dim > kMaxDim || n_tokens < 1 || n_tokens > kMaxTokens ||
-        hidden_stride < dim || weight_stride < dim || !weight || (rows > 0 && (!hidden || !targets)))
+        hidden_stride < dim || weight_stride < dim || !weight || (rows > 0 && (!hidden || !targets)) ||
+        !on_values(hidden, type_size(dtype)) || !on_values(weight, type_size(dtype)) || !on_words(mask, targets))
         return DOMINO_E_INVALID_ARG;
     if (dtype != DOMINO_DTYPE_BF16) return DOMINO_E_UNSUPPORTED;
     a = LossArgs{};
@@ -1995,7 +2003,8 @@ int distill_args(DistillArgs& a, domino_ctx* h, const void* logits, int32_t dtyp
     if (!is_dtype(dtype) || !is_dtype(teacher_dtype) || rows < 0 || rows > INT32_MAX / 8 || n_tokens < 1 ||
         n_tokens > kMaxTokens || stride < n_tokens || k < 1 || k > kDistillMaxK || !(temperature > 0.0f) ||
         !std::isfinite(temperature) || !std::isfinite(1.0f / temperature) ||
-        (rows > 0 && (!logits || !teacher || !ids)))
+        (rows > 0 && (!logits || !teacher || !ids)) || !on_values(logits, type_size(dtype)) ||
+        !on_values(teacher, type_size(teacher_dtype)) || !on_words(mask, ids))
         return DOMINO_E_INVALID_ARG;
     a = DistillArgs{};
     a.logits = logits;
@@ -2025,7 +2034,7 @@ int domino_token_loss(domino_t h, const void* hidden_dev, int64_t hidden_stride,
                                  mask_dev, targets_dev))
         return rc;
     if (rows == 0) return DOMINO_OK;
-    if (!loss_dev) return DOMINO_E_INVALID_ARG;
+    if (!loss_dev || !on_words(loss_dev, lse_dev)) return DOMINO_E_INVALID_ARG;
     a.loss = loss_dev;
     a.lse = lse_dev;
     DeviceGuard g(h->device);
@@ -2047,7 +2056,8 @@ int domino_token_loss_grad(domino_t h, const void* hidden_dev, int64_t hidden_st
                                  mask_dev, targets_dev))
         return rc;
     if (dhidden_stride < dim || dweight_stride < dim || !dweight_dev ||
-        (rows > 0 && (!lse_dev || !grad_loss_dev || !dhidden_dev)))
+        (rows > 0 && (!lse_dev || !grad_loss_dev || !dhidden_dev)) || !on_values(dhidden_dev, 2) ||
+        !on_values(dweight_dev, 2) || !on_words(lse_dev, grad_loss_dev))
         return DOMINO_E_INVALID_ARG;
     DeviceGuard g(h->device);
     cudaStream_t st = (cudaStream_t)stream;
@@ -2075,7 +2085,7 @@ int domino_distill_loss(domino_t h, const void* logits_dev, int32_t dtype, int32
                               teacher_dtype, ids_dev, k, temperature))
         return rc;
     if (rows == 0) return DOMINO_OK;
-    if (!loss_dev) return DOMINO_E_INVALID_ARG;
+    if (!loss_dev || !on_words(loss_dev, lse_dev)) return DOMINO_E_INVALID_ARG;
     a.loss = loss_dev;
     a.lse = lse_dev;
     DeviceGuard g(h->device);
@@ -2094,7 +2104,9 @@ int domino_distill_grad(domino_t h, const void* logits_dev, int32_t dtype, int32
     if (dlogits_stride < n_tokens || (logits_dev && dlogits_dev == logits_dev && dlogits_stride != row_stride_elems))
         return DOMINO_E_INVALID_ARG;
     if (rows == 0) return DOMINO_OK;
-    if (!lse_dev || !grad_loss_dev || !dlogits_dev) return DOMINO_E_INVALID_ARG;
+    if (!lse_dev || !grad_loss_dev || !dlogits_dev || !on_words(lse_dev, grad_loss_dev) ||
+        !on_values(dlogits_dev, type_size(dtype)))
+        return DOMINO_E_INVALID_ARG;
     a.lse = const_cast<float*>(lse_dev);
     a.grad_loss = grad_loss_dev;
     a.dlogits = dlogits_dev;
@@ -2109,7 +2121,8 @@ int domino_embed(domino_t h, const int32_t* tokens_dev, int32_t n, const void* w
     DOMINO_API_RANGE();
     if (int rc = device_handle(h)) return rc;
     if (!is_dtype(dtype) || n < 0 || n_tokens < 1 || n_tokens > kMaxTokens || dim < 1 || dim > kMaxDim ||
-        weight_stride < dim || out_stride < dim || (n > 0 && (!tokens_dev || !weight_dev || !out_dev)))
+        weight_stride < dim || out_stride < dim || (n > 0 && (!tokens_dev || !weight_dev || !out_dev)) ||
+        !on_words(tokens_dev) || !on_values(weight_dev, type_size(dtype)) || !on_values(out_dev, type_size(dtype)))
         return DOMINO_E_INVALID_ARG;
     if (n == 0) return DOMINO_OK;
     EmbedArgs a{};
@@ -2135,7 +2148,8 @@ int domino_embed_grad(domino_t h, const int32_t* tokens_dev, int32_t n, const vo
     if (int rc = device_handle(h)) return rc;
     if (!is_dtype(dtype) || n < 0 || n_tokens < 1 || n_tokens > kMaxTokens || dim < 1 || dim > kMaxDim ||
         (accumulate != 0 && accumulate != 1) || grad_stride < dim || dweight_stride < dim || !dweight_dev ||
-        (n > 0 && (!tokens_dev || !grad_dev)))
+        (n > 0 && (!tokens_dev || !grad_dev)) || !on_words(tokens_dev) || !on_values(grad_dev, type_size(dtype)) ||
+        !on_values(dweight_dev, type_size(dtype)))
         return DOMINO_E_INVALID_ARG;
     if (n > kMaxRows) return DOMINO_E_UNSUPPORTED;
     EmbedArgs a{};
