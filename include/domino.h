@@ -433,8 +433,8 @@ int domino_token_loss_grad(domino_t h, const void* hidden_dev, int64_t hidden_st
 /* Distillation from a teacher's top logits.  Row t's list holds k entries
  * (teacher_dev [rows][k] logits or log-probabilities of teacher_dtype, ids_dev
  * [rows][k]); entries with an id below 0 are none, and so are those whose token
- * the mask excludes or whose student logit is -inf; of equal ids the first
- * counts.  With p = softmax(teacher / temperature) over the entries and q =
+ * the mask excludes or whose teacher or student logit is -inf; of equal ids
+ * among the others the first counts.  With p = softmax(teacher / temperature) over the entries and q =
  * softmax(logits / temperature) over the allowed tokens:
  *   lse[t]  = log sum exp(logits / temperature),
  *   loss[t] = temperature^2 sum_i p_i (ln p_i - ln q[id_i]); 0 without entries.

@@ -3,8 +3,8 @@
 //
 //   q     = softmax of x[v] / tau over the tokens that the mask allows
 //   p     = softmax of t[i] / tau over the row's entries: those whose id is a
-//           token that the mask allows and whose student logit is not -inf; of
-//           equal ids the first
+//           token that the mask allows and whose logits, the teacher's and the
+//           student's, are not -inf; of equal ids the first
 //   loss  = tau^2 sum_i p_i (ln p_i - ln q_{id_i})         0 without entries
 //   dx[v] = g tau (q_v - sum_{i: id_i = v} p_i)            0 without entries
 //
@@ -159,11 +159,11 @@ __device__ void read_entries(Entries& e, const DistillCall& c, int32_t row, cons
         if (id >= a.n_tokens && report) atomicOr(a.err, DOMINO_DEVERR_BAD_TOKEN);
         if (id < 0 || id >= a.n_tokens || !allowed_bits(mrow, id, 1)) continue;
         const float x = load_at<BF16>(xrow, id);
-        if (x == -INFINITY) continue;
-        e.id[j] = id;
-        e.x[j] = x;
         t[j] = a.teacher_dtype == DOMINO_DTYPE_BF16 ? load_at<true>(a.teacher, (int64_t)row * a.k + i)
                                                     : load_at<false>(a.teacher, (int64_t)row * a.k + i);
+        if (x == -INFINITY || t[j] == -INFINITY) continue;
+        e.id[j] = id;
+        e.x[j] = x;
         // the first entry of an id: its place in a table of ids
         uint32_t h = ((uint32_t)id * 2654435761u >> 16) & (slots - 1);
         while (true) {
