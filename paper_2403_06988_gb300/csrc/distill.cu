@@ -103,6 +103,11 @@ __device__ __forceinline__ uint32_t allowed_bits(const uint32_t* mrow, int32_t t
     return bits & all;
 }
 
+// x / tau, rounded to fp32 wherever it is used: lse holds the largest one's rounding, and a difference from lse that kept the
+// product's other bits (one fma) would be off by up to half a unit in lse's last place, above zero too: exp of it passes all
+// bounds where that unit is large (logits that ban a token, 1e9 and more).
+__device__ __forceinline__ float scaled(float x, const DistillCall& c) { return __fmul_rn(x, c.inv_tau); }
+
 __device__ __forceinline__ float2 merge(float2 a, float2 b, float k) {
     const float m = fmaxf(a.x, b.x), ref = sum_ref(m);
     return make_float2(m, a.y * ex2((a.x - ref) * k) + b.y * ex2((b.x - ref) * k));
@@ -327,14 +332,14 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillCtas) distill_kernel(
             cluster.sync();
             if (slice) return;
         }
-        if (tid == 0) sh.lse = isnan(acc.y) ? acc.y : log_sum_exp(acc.x * c.inv_tau, acc.y);
+        if (tid == 0) sh.lse = isnan(acc.y) ? acc.y : log_sum_exp(scaled(acc.x, c), acc.y);
         __syncthreads();
         const float lse = sh.lse;
         read_entries<BF16>(e, c, row, xrow, mrow, sh, true);
         float sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < kDistillEntries; ++j)
-            if (e.id[j] >= 0 && e.p[j] != 0.0f) sum += e.p[j] * (e.logp[j] - (e.x[j] * c.inv_tau - lse));
+            if (e.id[j] >= 0 && e.p[j] != 0.0f) sum += e.p[j] * (e.logp[j] - (scaled(e.x[j], c) - lse));
         sum = cta_reduce<false>(sum, sh.red);
         if (tid == 0) {
             if (a.lse) a.lse[row] = lse;
@@ -347,9 +352,9 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillCtas) distill_kernel(
         // the entries' logits have been read by every CTA of the row before any is written over
         if (c.slices > 1) cg::this_cluster().sync();
         const float g = e.any ? __ldg(a.grad_loss + row) * a.temperature : 0.0f;
-        const auto grad = [&](float x) { return g * ex2(fmaf(x, c.inv_tau, -lse) * kLog2e); };
+        const auto q = [&](float x) { return ex2((scaled(x, c) - lse) * kLog2e); };
         const auto grad1 = [&](int32_t t) {
-            store_at<BF16>(drow, t, g != 0.0f && allowed_bits(mrow, t, 1) ? grad(load_at<BF16>(xrow, t)) : 0.0f);
+            store_at<BF16>(drow, t, g != 0.0f && allowed_bits(mrow, t, 1) ? g * q(load_at<BF16>(xrow, t)) : 0.0f);
         };
         // a gradient whose rows lie otherwise against 16-byte boundaries than the logits' is written one by one
         const bool same = ((reinterpret_cast<uintptr_t>(xrow) ^ reinterpret_cast<uintptr_t>(drow)) & 15) == 0;
@@ -358,6 +363,7 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillCtas) distill_kernel(
         for (int32_t t = tail + tid; t < t1; t += kDistillThreads) grad1(t);
         constexpr int32_t kStep = kDistillThreads * kDistillUnroll;
         const bool any = g != 0.0f;
+        const float2 nlse = make_float2(-lse, -lse);
         for (int32_t i = tid; same && i < vectors; i += kStep) {
             Batch<BF16> now;
             now.template load<false>(xrow, mrow, cut.head, vectors, i, any);
@@ -372,10 +378,10 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillCtas) distill_kernel(
                     x.set(now.u[j]);
 #pragma unroll
                     for (int b = 0; b < kN; b += 2) {
-                        const float2 d = scale2(fma2(make_float2(x.v[b], x.v[b + 1]), c.inv_tau, -lse), kLog2e);
-                        const float2 q = scale2(make_float2(ex2(d.x), ex2(d.y)), g);
-                        x.v[b] = q.x;
-                        x.v[b + 1] = q.y;
+                        const float2 d = scale2(add2(scale2(make_float2(x.v[b], x.v[b + 1]), c.inv_tau), nlse), kLog2e);
+                        const float2 y = scale2(make_float2(ex2(d.x), ex2(d.y)), g);
+                        x.v[b] = y.x;
+                        x.v[b + 1] = y.y;
                     }
                     if (!full) {
 #pragma unroll
@@ -391,7 +397,7 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillCtas) distill_kernel(
 #pragma unroll
         for (int j = 0; j < kDistillEntries; ++j)
             if (e.id[j] >= t0 && e.id[j] < t1 && g != 0.0f)
-                store_at<BF16>(drow, e.id[j], g * (ex2(fmaf(e.x[j], c.inv_tau, -lse) * kLog2e) - e.p[j]));
+                store_at<BF16>(drow, e.id[j], g * (q(e.x[j]) - e.p[j]));
     }
 }
 
