@@ -439,8 +439,8 @@ int domino_token_loss_grad(domino_t h, const void* hidden_dev, int64_t hidden_st
  *   lse[t]  = log sum exp(logits / temperature),
  *   loss[t] = temperature^2 sum_i p_i (ln p_i - ln q[id_i]); 0 without entries.
  * logits_dev [rows][row_stride_elems] of dtype (fp32 or bf16).
- * 1 <= k <= 1024, temperature > 0 and finite, its inverse too.  lse_dev may be
- * NULL.  Logits of masked tokens are not used.  Needs no scratch. */
+ * 1 <= k <= 1024; temperature > 0 and its square a normal fp32 number (1.1e-19
+ * to 1.8e19).  lse_dev may be NULL.  Logits of masked tokens are not used.  Needs no scratch. */
 int domino_distill_loss(domino_t h, const void* logits_dev, int32_t dtype, int32_t rows, int64_t row_stride_elems,
                         int32_t n_tokens, const uint32_t* mask_dev, const void* teacher_dev, int32_t teacher_dtype,
                         const int32_t* ids_dev, int32_t k, float temperature, float* loss_dev, float* lse_dev,

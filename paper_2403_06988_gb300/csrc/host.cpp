@@ -2002,7 +2002,7 @@ int distill_args(DistillArgs& a, domino_ctx* h, const void* logits, int32_t dtyp
     if (int rc = device_handle(h)) return rc;
     if (!is_dtype(dtype) || !is_dtype(teacher_dtype) || rows < 0 || rows > INT32_MAX / 8 || n_tokens < 1 ||
         n_tokens > kMaxTokens || stride < n_tokens || k < 1 || k > kDistillMaxK || !(temperature > 0.0f) ||
-        !std::isfinite(temperature) || !std::isfinite(1.0f / temperature) ||
+        !std::isnormal(temperature * temperature) ||   // log2(e) / temperature is then a number too
         (rows > 0 && (!logits || !teacher || !ids)) || !on_values(logits, type_size(dtype)) ||
         !on_values(teacher, type_size(teacher_dtype)) || !on_words(mask, ids))
         return DOMINO_E_INVALID_ARG;
