@@ -32,7 +32,8 @@
  *    the caller, and their kernels must not overlap on the GPU either (issue
  *    them on one stream, or order the streams with events): the handle's
  *    scratch (the fused decode's partials, opportunistic masking's row list,
- *    the host-buffer step's staging) is shared by its calls.
+ *    the host-buffer step's staging, that of the losses and of the embedding's
+ *    gradient) is shared by its calls.
  *    Different handles are independent.
  */
 #ifndef DOMINO_H
@@ -392,7 +393,12 @@ int domino_mask_logits_noalloc(const void* logits_dev, int32_t dtype, int32_t ba
  * domino_embed_grad take at most 2^31 - 2^20 - 1 rows (above:
  * DOMINO_E_UNSUPPORTED).  Scratch is the handle's and grows on demand: the
  * first call at larger sizes must not run under a stream capture
- * (DOMINO_E_INVALID_ARG; the calls that need no scratch are marked).  All sums
+ * (DOMINO_E_INVALID_ARG; the calls that need no scratch are marked), and waits
+ * for the stream where it gives the smaller scratch back.  Scratch that a
+ * recorded graph uses stays until the handle is destroyed.  A token loss takes
+ * 8 bytes for every row and 128 tokens (32 where the product is small), its
+ * gradient up to 256 MB and some copies of the hidden rows, both a copy of
+ * operands whose rows are not on 16-byte boundaries.  All sums
  * are held in fp32 and every result is the same on every run.  A target, teacher
  * id or token at or beyond V sets DOMINO_DEVERR_BAD_TOKEN and counts as below
  * 0.  Inputs and outputs do not overlap unless said otherwise.  Pointers are

@@ -60,7 +60,8 @@ struct domino_ctx {
     DevBuf d_dense, d_sparse, d_accept, d_self, d_tok_cls;
     DevBuf d_err, d_fpart;
     DevBuf d_space;                  // scratch of the losses and the embedding's gradient
-    std::vector<DevBuf> fpart_old;   // outgrown ones (of d_fpart and d_space): recorded graphs may still name them
+    bool space_recorded = false;     // a call under a capture has used d_space
+    std::vector<DevBuf> outgrown;    // of d_fpart and d_space: recorded graphs may still name them
     bool arena_ready = false;
     // prefix tree of the class strings (domino_get_prefix_tree)
     std::vector<uint4> t_node;
@@ -146,7 +147,7 @@ int64_t dev_bytes(const domino_ctx* h) {
                            &h->d_xrange, &h->d_exits, &h->d_trec};
     int64_t n = 0;
     for (auto* b : all) n += (int64_t)b->n;
-    for (const DevBuf& b : h->fpart_old) n += (int64_t)b.n;
+    for (const DevBuf& b : h->outgrown) n += (int64_t)b.n;
     return n;
 }
 
@@ -171,23 +172,44 @@ int dev_upload(DevBuf& b, const void* src, size_t n) {
 
 int dev_reserve(DevBuf& b, size_t n) { return dev_upload(b, nullptr, n); }
 
-// A scratch buffer of n bytes or more.  An outgrown buffer is kept until the
-// handle is destroyed: a graph that a caller recorded at a smaller batch goes on
-// using it.  Sizes at least double, so the outgrown ones take no more than the
-// buffer itself.
-int grow_scratch(domino_ctx* h, DevBuf& of, size_t n) {
-    if (of.n >= n) return DOMINO_OK;
+// The fused decode's partials, n bytes or more.  An outgrown buffer is kept
+// until the handle is destroyed: a graph that a caller recorded at a smaller
+// batch goes on using it.  Sizes at least double, so the outgrown ones take
+// no more than the buffer itself.
+int grow_fpart(domino_ctx* h, size_t n) {
+    if (h->d_fpart.n >= n) return DOMINO_OK;
     DevBuf b;
-    int rc = dev_reserve(b, std::max(n, 2 * of.n));
-    if (rc == DOMINO_E_OOM && n < 2 * of.n) rc = dev_reserve(b, n);
-    if (rc) return rc;
-    if (of.p) h->fpart_old.push_back(of);
-    of = b;
+    if (int rc = dev_reserve(b, std::max(n, 2 * h->d_fpart.n))) return rc;
+    if (h->d_fpart.p) h->outgrown.push_back(h->d_fpart);
+    h->d_fpart = b;
     return DOMINO_OK;
 }
 
-// The fused decode's partials.
-int grow_fpart(domino_ctx* h, size_t n) { return grow_scratch(h, h->d_fpart, n); }
+// The losses' scratch, n bytes or more, for a call on `st`.  It may hold a copy
+// of a weight: an outgrown buffer is freed, once the work on it has ended, and
+// the new one is a quarter larger at least (or n, where that is too much).  A
+// buffer that a recorded graph uses is kept until the handle is destroyed, and
+// its successor twice as large where memory allows.  Without memory the scratch
+// stays as it is.
+int grow_space(domino_ctx* h, size_t n, cudaStream_t st) {
+    const DevBuf old = h->d_space;
+    const bool keep = h->space_recorded;
+    if (keep) h->outgrown.reserve(h->outgrown.size() + 1);   // may throw: nothing is changed yet
+    if (old.p && cudaStreamSynchronize(st) != cudaSuccess) return cuda_status(cudaGetLastError());
+    if (keep) h->d_space = DevBuf{};
+    else dev_free(h->d_space);
+    int rc = dev_reserve(h->d_space, std::max(n, old.n + (keep ? old.n : old.n / 4)));
+    if (rc == DOMINO_E_OOM) rc = dev_reserve(h->d_space, n);
+    if (rc == DOMINO_OK) {
+        if (keep) h->outgrown.push_back(old);
+        h->space_recorded = false;
+    } else if (keep) {
+        h->d_space = old;
+    } else if (old.n) {
+        dev_reserve(h->d_space, old.n);
+    }
+    return rc;
+}
 
 bool is_host_only(const domino_ctx* h) { return h->device < 0; }
 
@@ -1089,7 +1111,7 @@ int domino_destroy(domino_t h) {
                          &h->d_rstart, &h->d_loop_of, &h->d_loopbits, &h->d_keeps, &h->d_xrange, &h->d_exits,
                          &h->d_trec};
         for (auto* b : all) dev_free(*b);
-        for (DevBuf& b : h->fpart_old) dev_free(b);
+        for (DevBuf& b : h->outgrown) dev_free(b);
         for (cudaEvent_t& e : h->ev_chunk)
             if (e) cudaEventDestroy(e);
         for (cudaEvent_t& e : h->ev_t)
@@ -1966,11 +1988,15 @@ int device_handle(domino_ctx* h) {
 // The handle's scratch, n bytes or more: allocating is not allowed while the
 // stream is captured.
 int loss_scratch(domino_ctx* h, size_t n, cudaStream_t st) {
-    if (h->d_space.n >= n) return DOMINO_OK;
     cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
     if (cudaStreamIsCapturing(st, &cs) != cudaSuccess) return cuda_status(cudaGetLastError());
-    if (cs != cudaStreamCaptureStatusNone) return DOMINO_E_INVALID_ARG;
-    return grow_scratch(h, h->d_space, n);
+    const bool recording = cs != cudaStreamCaptureStatusNone;
+    if (h->d_space.n < n) {
+        if (recording) return DOMINO_E_INVALID_ARG;
+        if (int rc = grow_space(h, n, st)) return rc;
+    }
+    if (recording) h->space_recorded = true;
+    return DOMINO_OK;
 }
 
 int token_loss_args(LossArgs& a, domino_ctx* h, const void* hidden, int64_t hidden_stride, const void* weight,
