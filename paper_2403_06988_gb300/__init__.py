@@ -9,6 +9,7 @@ handle created without a GPU raise DominoError(E_NO_DEVICE).
 """
 from __future__ import annotations
 
+import os
 from typing import Optional, Tuple
 
 from . import _binding as B
@@ -25,6 +26,10 @@ def _calls():
         import ctypes
 
         import torch  # noqa: F401  (its libraries, before the extension's)
+        from . import build
+        if not os.path.exists(build.CALLS) or build.calls_built_for_another():
+            raise ImportError("_loss_calls.so is not built for this torch; run __graft_entry__.build() or "
+                              "python -m paper_2403_06988_gb300.build")
         from . import _loss_calls as c
         c.bind(*(ctypes.cast(getattr(B.lib(), "domino_" + n), ctypes.c_void_p).value
                  for n in ("token_loss", "token_loss_grad", "distill_loss", "distill_grad", "embed", "embed_grad")))

@@ -5,7 +5,8 @@ loss.cu, loss_few.cu, distill.cu and embed.cu: kernels) are compiled in parallel
 Objects go to paper_2403_06988_gb300/_build/.
 
 csrc/calls.cpp becomes the Python extension _loss_calls.so beside it (g++, against the
-installed torch's headers and libraries).
+installed torch's headers and libraries; built again for another torch or Python).  Without
+a CUDA build of torch the library is built alone.
 
 build(debug=True) makes libdomino_debug.so instead (objects in _build_debug/),
 compiled with -DDOMINO_DEBUG: every transition-table lookup checks its state,
@@ -16,9 +17,12 @@ binding loads it when DOMINO_DEBUG_LIB=1 is set in the environment.
 from __future__ import annotations
 
 import concurrent.futures
+import importlib.util
 import os
 import shutil
 import subprocess
+import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -54,25 +58,64 @@ def up_to_date(lib: str = LIB) -> bool:
     return all(os.path.getmtime(f) <= t for f in _inputs())
 
 
-def build_calls(force: bool = False) -> str:
-    """The Python extension _loss_calls.so."""
-    import importlib.util
-    import sysconfig
+def _torch():
+    """The folder of the installed torch if it is a CUDA build (not imported), else None."""
+    spec = importlib.util.find_spec("torch")
+    folder = spec and spec.submodule_search_locations and spec.submodule_search_locations[0]
+    return folder if folder and os.path.exists(os.path.join(folder, "lib", "libc10_cuda.so")) else None
+
+
+def _torch_version(folder) -> str:
+    with open(os.path.join(folder, "version.py")) as f:
+        return f.read()
+
+
+def _calls_for(folder) -> str:
+    """What the extension is built for: it unpacks this torch's objects in this Python."""
+    return "\n".join((sysconfig.get_config_var("SOABI") or "", folder, _torch_version(folder)))
+
+
+def calls_built_for_another() -> bool:
+    """Whether _loss_calls.so is known to be built for another torch or Python than the installed one."""
+    folder, stamp = _torch(), CALLS + ".for"
+    if not folder:
+        return True
+    if not os.path.exists(stamp):
+        return False
+    with open(stamp) as f:
+        return f.read() != _calls_for(folder)
+
+
+def calls_up_to_date() -> bool:
+    """Whether _loss_calls.so is there, built from its source for the installed torch."""
     src = [os.path.join(CSRC, "calls.cpp"), os.path.join(INCLUDE, "domino.h")]
-    if not force and os.path.exists(CALLS) and all(os.path.getmtime(f) <= os.path.getmtime(CALLS) for f in src):
+    return (os.path.exists(CALLS) and os.path.exists(CALLS + ".for") and not calls_built_for_another() and
+            all(os.path.getmtime(f) <= os.path.getmtime(CALLS) for f in src))
+
+
+def build_calls(force: bool = False):
+    """The Python extension _loss_calls.so (None without a CUDA build of torch)."""
+    folder = _torch()
+    if not folder:
+        print("no CUDA build of torch is installed: libdomino.so is built without the Python calls of the losses and the "
+              "embedding", file=sys.stderr)
+        return None
+    if not force and calls_up_to_date():
         return CALLS
-    torch_dir = importlib.util.find_spec("torch").submodule_search_locations[0]
     cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc())))
-    lib = os.path.join(torch_dir, "lib")
+    lib = os.path.join(folder, "lib")
     tmp = CALLS + f".tmp{os.getpid()}"
-    cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", src[0], "-o", tmp, "-I", INCLUDE,
-           "-I", os.path.join(torch_dir, "include"), "-I", sysconfig.get_paths()["include"],
+    cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", os.path.join(CSRC, "calls.cpp"), "-o", tmp,
+           "-I", INCLUDE, "-I", os.path.join(folder, "include"), "-I", sysconfig.get_paths()["include"],
            "-I", os.path.join(cuda, "include"), "-L", lib, f"-Wl,-rpath,{lib}", "-ltorch_python", "-ltorch_cpu",
            "-lc10_cuda", "-lc10"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"g++ failed for calls.cpp:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, CALLS)
+    with open(tmp, "w") as f:
+        f.write(_calls_for(folder))
+    os.replace(tmp, CALLS + ".for")
     return CALLS
 
 
@@ -119,5 +162,4 @@ def _build_library(force, verbose, extra_flags, debug) -> str:
 
 
 if __name__ == "__main__":
-    import sys
     print(build(force="--force" in sys.argv, verbose="-v" in sys.argv))
