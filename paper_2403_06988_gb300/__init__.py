@@ -216,6 +216,8 @@ class Domino:
         return so
 
     # -- losses over the vocabulary, the embedding (no loaded vocabulary needed) -----
+    # Their gradients are calls of their own; autograd does not see them.  Tensors that require a gradient are refused in grad
+    # mode (RuntimeError): pass detach(), or call under torch.no_grad().
     def _result(self, name, r):
         if type(r) is int:
             B._check(name, r)

@@ -10,6 +10,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/core/grad_mode.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -45,6 +46,10 @@ struct Matrix {
 const at::Tensor& tensor(PyObject* o, int device, const char* what) {
     if (!THPVariable_Check(o)) throw Refused{PyExc_TypeError, what, "a tensor expected"};
     const at::Tensor& t = THPVariable_Unpack(o);
+    // autograd does not see these calls: what they return would be a constant to it
+    if (t.requires_grad() && at::GradMode::is_enabled())
+        throw Refused{PyExc_RuntimeError, what,
+                      "requires a gradient, which these calls do not record; pass detach(), or call under torch.no_grad()"};
     if (!t.is_cuda() || t.get_device() != device) throw Refused{PyExc_ValueError, what, "not on the handle's device"};
     return t;
 }
