@@ -137,6 +137,18 @@ PyObject* pair(const at::Tensor& a, const at::Tensor& b) {
     return r;
 }
 
+// torch.OutOfMemoryError, which every torch allocation raises.
+PyObject* out_of_memory() {
+    static PyObject* const type = [] {
+        PyObject* torch = PyImport_ImportModule("torch");
+        PyObject* t = torch ? PyObject_GetAttrString(torch, "OutOfMemoryError") : nullptr;
+        Py_XDECREF(torch);
+        if (!t) PyErr_Clear();
+        return t ? t : PyExc_RuntimeError;
+    }();
+    return type;
+}
+
 // Runs f, whose exceptions become Python's.
 template <int N, typename F>
 PyObject* guarded(Py_ssize_t n, F f) {
@@ -148,7 +160,9 @@ PyObject* guarded(Py_ssize_t n, F f) {
         return f();
     } catch (const Refused& r) {
         PyErr_Format(r.type, "%s: %s", r.what, r.why);
-    } catch (const std::exception& e) {   // torch's, out of memory for one
+    } catch (const c10::OutOfMemoryError& e) {
+        PyErr_SetString(out_of_memory(), e.what_without_backtrace());
+    } catch (const std::exception& e) {   // torch's
         PyErr_SetString(PyExc_RuntimeError, e.what());
     }
     return nullptr;
