@@ -82,10 +82,24 @@ class Domino:
     def info(self) -> dict:
         return B.domino_get_info(self.h)
 
-    def _empty(self, shape, dtype, device):
+    def _empty(self, shape, dtype, device, stream=None, zero=False):
+        """An output of a call on `stream`.  Where that is not torch's current one, it is made on it (not from a block that
+        the current stream has given back and may still be using), and stays in use until what the current stream does
+        with it has ended."""
         import torch
+        if stream is not None:
+            now, to = torch.cuda.current_stream(device), B._stream(stream)
+            if to != now.cuda_stream:
+                to = 0 if to == 1 else to     # cudaStreamLegacy: the default stream's other name
+                with torch.cuda.stream(torch.cuda.ExternalStream(to, device)):
+                    t = self._empty(shape, dtype, device, None, zero)
+                if t.numel():
+                    t.record_stream(now)
+                return t
         t = torch.empty(shape, dtype=dtype, device=device)
-        if self.fill_byte is not None and t.numel():
+        if zero:
+            t.zero_()
+        elif self.fill_byte is not None and t.numel():
             t.view(torch.uint8).fill_(self.fill_byte)
         return t
 
@@ -98,9 +112,9 @@ class Domino:
         if mask is None or (want_next and nxt is None):
             V, W = B.sizes(self.h)
             if mask is None:
-                mask = self._empty((b, W), torch.int32, states.device)
+                mask = self._empty((b, W), torch.int32, states.device, stream)
             if want_next and nxt is None:
-                nxt = self._empty((b, V), torch.int32, states.device)
+                nxt = self._empty((b, V), torch.int32, states.device, stream)
         B.domino_step_mask(self.h, states, stacks, b, mask, nxt, stream)
         return mask, nxt
 
@@ -120,11 +134,11 @@ class Domino:
         if mask is None or want_logprobs:
             V, W = B.sizes(self.h)
             if mask is None:
-                mask = self._empty((b, W), torch.int32, dev)
+                mask = self._empty((b, W), torch.int32, dev, stream)
             if want_logprobs:
-                lp = self._empty((b, V), torch.float32, dev)
-        argmax = self._empty(b, torch.int32, dev)
-        lse = self._empty(b, torch.float32, dev)
+                lp = self._empty((b, V), torch.float32, dev, stream)
+        argmax = self._empty(b, torch.int32, dev, stream)
+        lse = self._empty(b, torch.float32, dev, stream)
         B.domino_step_decode(self.h, states, stacks, b, logits.data_ptr(), dtype, logits.stride(0), mask, argmax, lse,
                              lp, states if advance else None, stacks if advance else None, stream)
         return mask, argmax, lse, lp
@@ -133,8 +147,8 @@ class Domino:
         import torch
         info = self.info()
         dev = f"cuda:{self.device}"
-        nxt = self._empty((info["n_states"], info["n_tokens"]), torch.int32, dev) if want_next else None
-        mask = self._empty((info["n_states"], info["n_words"]), torch.int32, dev) if want_mask else None
+        nxt = self._empty((info["n_states"], info["n_tokens"]), torch.int32, dev, stream) if want_next else None
+        mask = self._empty((info["n_states"], info["n_words"]), torch.int32, dev, stream) if want_mask else None
         B.domino_precompute_table(self.h, nxt, mask, stream)
         return nxt, mask
 
@@ -151,11 +165,11 @@ class Domino:
             raise ValueError("logits rows must be contiguous")
         argmax, lse, lp = out if out is not None else (None, None, None)
         if argmax is None:
-            argmax = self._empty(b, torch.int32, logits.device)
+            argmax = self._empty(b, torch.int32, logits.device, stream)
         if want_lse and lse is None:
-            lse = self._empty(b, torch.float32, logits.device)
+            lse = self._empty(b, torch.float32, logits.device, stream)
         if want_logprobs and lp is None:
-            lp = self._empty((b, n_tokens), torch.float32, logits.device)
+            lp = self._empty((b, n_tokens), torch.float32, logits.device, stream)
         B.domino_mask_logits(self.h, logits.data_ptr(), dtype, b, logits.stride(0), mask, argmax,
                              lse if want_lse else None, lp if want_logprobs else None, stream)
         return argmax, (lse if want_lse else None), (lp if want_logprobs else None)
@@ -174,7 +188,7 @@ class Domino:
         dtype = DTYPE_BF16 if logits.dtype == torch.bfloat16 else DTYPE_F32
         if logits.stride(1) != 1:
             raise ValueError("logits rows must be contiguous")
-        tokens = self._empty(b, torch.int32, logits.device)
+        tokens = self._empty(b, torch.int32, logits.device, stream)
         B.domino_mask_sample(self.h, logits, dtype, b, logits.stride(0), mask, temperature, seed, offset, tokens,
                              stream)
         return tokens
@@ -187,9 +201,9 @@ class Domino:
         if logits.stride(1) != 1:
             raise ValueError("logits rows must be contiguous")
         W = B.sizes(self.h)[1]
-        scratch = self._empty((b, W), torch.int32, logits.device)
-        tokens = self._empty(b, torch.int32, logits.device)
-        n_fb = torch.zeros(1, dtype=torch.int32, device=logits.device)
+        scratch = self._empty((b, W), torch.int32, logits.device, stream)
+        tokens = self._empty(b, torch.int32, logits.device, stream)
+        n_fb = self._empty(1, torch.int32, logits.device, stream, zero=True)
         B.domino_opportunistic_step(self.h, logits, dtype, b, logits.stride(0), states, stacks, scratch, tokens, n_fb,
                                     stream)
         return tokens, n_fb
@@ -202,9 +216,9 @@ class Domino:
         dtype = DTYPE_BF16 if logits.dtype == torch.bfloat16 else DTYPE_F32
         if logits.stride(1) != 1:
             raise ValueError("logits rows must be contiguous")
-        argmax = self._empty(b, torch.int32, logits.device)
-        lse = self._empty(b, torch.float32, logits.device) if want_lse else None
-        lp = self._empty((b, B.sizes(self.h)[0]), torch.float32, logits.device) if want_logprobs else None
+        argmax = self._empty(b, torch.int32, logits.device, stream)
+        lse = self._empty(b, torch.float32, logits.device, stream) if want_lse else None
+        lp = self._empty((b, B.sizes(self.h)[0]), torch.float32, logits.device, stream) if want_logprobs else None
         B.domino_mask_logits_table(self.h, logits, dtype, b, logits.stride(0), table_mask, states, argmax, lse, lp,
                                    stream)
         return argmax, lse, lp
@@ -223,25 +237,25 @@ class Domino:
             B._check(name, r)
         return r
 
-    def _fill(self, out, rows, cols, dtype, like):
+    def _fill(self, out, rows, cols, dtype, like, stream):
         """`out`, or with fill_byte the filled tensor that the call would otherwise make itself."""
         if out is not None or self.fill_byte is None:
             return out
-        return self._empty(rows if cols is None else (rows, cols), dtype, like.device)
+        return self._empty(rows if cols is None else (rows, cols), dtype, like.device, stream)
 
-    def _losses(self, out, like):
+    def _losses(self, out, like, stream):
         import torch
         loss, lse = out if out is not None else (None, None)
         if self.fill_byte is None:
             return loss, lse
         n = like.shape[0]
-        return self._fill(loss, n, None, torch.float32, like), self._fill(lse, n, None, torch.float32, like)
+        return tuple(self._fill(o, n, None, torch.float32, like, stream) for o in (loss, lse))
 
     def token_loss(self, hidden, weight, targets, mask=None, out=None, stream=None) -> Tuple:
         """Cross entropy of `targets` under the masked softmax of hidden @ weight.T, the logits never kept: (loss,
         lse), fp32 [rows].  hidden [rows, dim], weight [n_tokens, dim] bf16; targets int32 (below 0: none); mask as
         step_mask's or None.  out: (loss, lse) to write to."""
-        loss, lse = self._losses(out, hidden)
+        loss, lse = self._losses(out, hidden, stream)
         return self._result("domino_token_loss", _calls().token_loss(
             self.h, self.device, hidden, weight, targets, mask, loss, lse, None if stream is None else B._stream(stream)))
 
@@ -249,8 +263,8 @@ class Domino:
         """(dhidden, dweight) of sum(grad_loss * loss), lse as token_loss returned it; in the inputs' type."""
         dh, dw = out if out is not None else (None, None)
         if self.fill_byte is not None:
-            dh = self._fill(dh, *hidden.shape, hidden.dtype, hidden)
-            dw = self._fill(dw, *weight.shape, weight.dtype, weight)
+            dh = self._fill(dh, *hidden.shape, hidden.dtype, hidden, stream)
+            dw = self._fill(dw, *weight.shape, weight.dtype, weight, stream)
         return self._result("domino_token_loss_grad", _calls().token_loss_grad(
             self.h, self.device, hidden, weight, targets, lse, grad_loss, mask, dh, dw,
             None if stream is None else B._stream(stream)))
@@ -258,7 +272,7 @@ class Domino:
     def distill_loss(self, logits, teacher, ids, temperature: float = 1.0, mask=None, out=None, stream=None) -> Tuple:
         """Divergence of the teacher's top logits (teacher, ids [rows, k]; ids below 0: no entry) from the masked
         softmax of logits / temperature, times temperature^2: (loss, lse), fp32 [rows]."""
-        loss, lse = self._losses(out, logits)
+        loss, lse = self._losses(out, logits, stream)
         return self._result("domino_distill_loss", _calls().distill_loss(
             self.h, self.device, logits, teacher, ids, temperature, mask, loss, lse,
             None if stream is None else B._stream(stream)))
@@ -266,7 +280,7 @@ class Domino:
     def distill_grad(self, logits, teacher, ids, temperature: float, lse, grad_loss, mask=None, out=None, stream=None):
         """d sum(grad_loss * loss) / d logits, in the logits' type; out may be `logits` itself."""
         if self.fill_byte is not None:
-            out = self._fill(out, *logits.shape, logits.dtype, logits)
+            out = self._fill(out, *logits.shape, logits.dtype, logits, stream)
         return self._result("domino_distill_grad", _calls().distill_grad(
             self.h, self.device, logits, teacher, ids, temperature, lse, grad_loss, mask, out,
             None if stream is None else B._stream(stream)))
@@ -274,7 +288,7 @@ class Domino:
     def embed(self, tokens, weight, scale: float = 1.0, out=None, stream=None):
         """scale * weight[tokens], zeros for tokens below 0: [n, dim] of the weight's type."""
         if self.fill_byte is not None:
-            out = self._fill(out, tokens.numel(), weight.shape[-1], weight.dtype, weight)
+            out = self._fill(out, tokens.numel(), weight.shape[-1], weight.dtype, weight, stream)
         return self._result("domino_embed", _calls().embed(
             self.h, self.device, tokens, weight, scale, out, None if stream is None else B._stream(stream)))
 
@@ -283,7 +297,7 @@ class Domino:
         sums are added to (the loss's, for a table that is its weight too)."""
         out = into
         if self.fill_byte is not None:
-            out = self._fill(into, n_tokens, grad.shape[-1], grad.dtype, grad)
+            out = self._fill(into, n_tokens, grad.shape[-1], grad.dtype, grad, stream)
         return self._result("domino_embed_grad", _calls().embed_grad(
             self.h, self.device, tokens, grad, n_tokens, scale, out, into is not None,
             None if stream is None else B._stream(stream)))

@@ -15,6 +15,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <optional>
 
 #include "domino.h"
 
@@ -34,6 +35,68 @@ struct Refused {
     PyObject* type;
     const char* what;
     const char* why;
+};
+
+int64_t integer(PyObject* o, const char* what) {
+    const int64_t v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) {
+        PyErr_Clear();
+        throw Refused{PyExc_TypeError, what, "an integer expected"};
+    }
+    return v;
+}
+int32_t integer32(PyObject* o, const char* what) {
+    const int64_t v = integer(o, what);
+    if (v != (int32_t)v) throw Refused{PyExc_ValueError, what, "too large"};
+    return (int32_t)v;
+}
+float number(PyObject* o, const char* what) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) {
+        PyErr_Clear();
+        throw Refused{PyExc_TypeError, what, "a number expected"};
+    }
+    return (float)v;
+}
+
+// While it lives, torch's current stream of the device is the call's: outputs come from that stream's memory, not from
+// blocks that the current one has given back and may still be using.  They stay in use (made()) until what the current
+// stream does with them has ended.
+class OnStream {
+  public:
+    OnStream(void* stream, int device) {
+        if (device < 0) return;
+        const c10::cuda::CUDAStream now = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device);
+        if ((void*)now.stream() == stream) return;
+        current_ = now;
+        // cudaStreamLegacy is the default stream's other name
+        cudaStream_t to = (cudaStream_t)stream == cudaStreamLegacy ? nullptr : (cudaStream_t)stream;
+        c10::cuda::setCurrentCUDAStream(c10::cuda::getStreamFromExternal(to, (c10::DeviceIndex)device));
+    }
+    OnStream(const OnStream&) = delete;
+    ~OnStream() {
+        if (current_) c10::cuda::setCurrentCUDAStream(*current_);
+    }
+    at::Tensor made(at::Tensor t) const {
+        if (current_) t.record_stream(current_->unwrap());
+        return t;
+    }
+
+  private:
+    std::optional<c10::cuda::CUDAStream> current_;
+};
+
+struct Call {
+    domino_t h;
+    int device;
+    void* stream;
+    OnStream on;
+    Call(PyObject* const* args, PyObject* st)
+        : h((domino_t)(uintptr_t)(args[0] == Py_None ? 0 : integer(args[0], "handle"))),
+          device(integer32(args[1], "device")),
+          stream(st == Py_None ? (device < 0 ? nullptr : (void*)c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream())
+                               : (void*)(uintptr_t)integer(st, "stream")),
+          on(stream, device) {}
 };
 
 struct Matrix {
@@ -68,9 +131,9 @@ Matrix matrix(PyObject* o, int device, const char* what) {
 }
 
 // The matrix given, or a new one.
-Matrix output(PyObject* o, int device, const char* what, int64_t rows, int64_t cols, const Matrix& like) {
-    if (o == Py_None) return Matrix{at::empty({rows, cols}, like.t.options()), rows, cols, cols, like.dtype};
-    Matrix m = matrix(o, device, what);
+Matrix output(PyObject* o, const Call& c, const char* what, int64_t rows, int64_t cols, const Matrix& like) {
+    if (o == Py_None) return Matrix{c.on.made(at::empty({rows, cols}, like.t.options())), rows, cols, cols, like.dtype};
+    Matrix m = matrix(o, c.device, what);
     if (m.rows != rows || m.cols != cols) throw Refused{PyExc_ValueError, what, "another shape expected"};
     if (m.dtype != like.dtype) throw Refused{PyExc_TypeError, what, "must be of the inputs' type"};
     return m;
@@ -84,8 +147,8 @@ const at::Tensor& words(PyObject* o, int device, at::ScalarType type, int64_t n,
     if (t.numel() != n || !t.is_contiguous()) throw Refused{PyExc_ValueError, what, "another number of contiguous values expected"};
     return t;
 }
-at::Tensor floats(PyObject* o, int device, int64_t n, const char* what, const Matrix& like) {
-    return o == Py_None ? at::empty({n}, like.t.options().dtype(at::kFloat)) : words(o, device, at::kFloat, n, what);
+at::Tensor floats(PyObject* o, const Call& c, int64_t n, const char* what, const Matrix& like) {
+    return o == Py_None ? c.on.made(at::empty({n}, like.t.options().dtype(at::kFloat))) : words(o, c.device, at::kFloat, n, what);
 }
 
 const uint32_t* mask_words(PyObject* o, int device, int64_t rows, int64_t n_tokens) {
@@ -95,39 +158,6 @@ const uint32_t* mask_words(PyObject* o, int device, int64_t rows, int64_t n_toke
         throw Refused{PyExc_ValueError, "mask", "one contiguous row of ceil(n_tokens / 32) 32-bit words per row expected"};
     return (const uint32_t*)t.data_ptr();
 }
-
-int64_t integer(PyObject* o, const char* what) {
-    const int64_t v = PyLong_AsLongLong(o);
-    if (v == -1 && PyErr_Occurred()) {
-        PyErr_Clear();
-        throw Refused{PyExc_TypeError, what, "an integer expected"};
-    }
-    return v;
-}
-int32_t integer32(PyObject* o, const char* what) {
-    const int64_t v = integer(o, what);
-    if (v != (int32_t)v) throw Refused{PyExc_ValueError, what, "too large"};
-    return (int32_t)v;
-}
-float number(PyObject* o, const char* what) {
-    const double v = PyFloat_AsDouble(o);
-    if (v == -1.0 && PyErr_Occurred()) {
-        PyErr_Clear();
-        throw Refused{PyExc_TypeError, what, "a number expected"};
-    }
-    return (float)v;
-}
-
-struct Call {
-    domino_t h;
-    int device;
-    void* stream;
-    Call(PyObject* const* args, PyObject* st)
-        : h((domino_t)(uintptr_t)(args[0] == Py_None ? 0 : integer(args[0], "handle"))), device(integer32(args[1], "device")) {
-        stream = st == Py_None ? (device < 0 ? nullptr : (void*)c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream())
-                               : (void*)(uintptr_t)integer(st, "stream");
-    }
-};
 
 PyObject* pair(const at::Tensor& a, const at::Tensor& b) {
     PyObject* r = PyTuple_New(2);
@@ -186,8 +216,8 @@ PyObject* token_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded<9>(n, [&]() -> PyObject* {
         const Call c(a, a[8]);
         const LossInputs in(a[2], a[3], a[4], a[5], c.device);
-        const at::Tensor loss = floats(a[6], c.device, in.hidden.rows, "loss", in.hidden);
-        const at::Tensor lse = floats(a[7], c.device, in.hidden.rows, "lse", in.hidden);
+        const at::Tensor loss = floats(a[6], c, in.hidden.rows, "loss", in.hidden);
+        const at::Tensor lse = floats(a[7], c, in.hidden.rows, "lse", in.hidden);
         const int s = g_token_loss(c.h, in.hidden.p(), in.hidden.step, in.weight.p(), in.weight.step, in.hidden.dtype,
                                    (int32_t)in.hidden.rows, (int32_t)in.hidden.cols, (int32_t)in.weight.rows, in.mask, in.targets,
                                    (float*)loss.data_ptr(), (float*)lse.data_ptr(), c.stream);
@@ -202,8 +232,8 @@ PyObject* token_loss_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const LossInputs in(a[2], a[3], a[4], a[7], c.device);
         const at::Tensor &lse = words(a[5], c.device, at::kFloat, in.hidden.rows, "lse"),
                          &g = words(a[6], c.device, at::kFloat, in.hidden.rows, "grad_loss");
-        const Matrix dh = output(a[8], c.device, "dhidden", in.hidden.rows, in.hidden.cols, in.hidden);
-        const Matrix dw = output(a[9], c.device, "dweight", in.weight.rows, in.weight.cols, in.hidden);
+        const Matrix dh = output(a[8], c, "dhidden", in.hidden.rows, in.hidden.cols, in.hidden);
+        const Matrix dw = output(a[9], c, "dweight", in.weight.rows, in.weight.cols, in.hidden);
         const int s = g_token_loss_grad(c.h, in.hidden.p(), in.hidden.step, in.weight.p(), in.weight.step, in.hidden.dtype,
                                         (int32_t)in.hidden.rows, (int32_t)in.hidden.cols, (int32_t)in.weight.rows, in.mask,
                                         in.targets, (const float*)lse.data_ptr(), (const float*)g.data_ptr(), dh.p(), dh.step,
@@ -234,8 +264,8 @@ PyObject* distill_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded<10>(n, [&]() -> PyObject* {
         const Call c(a, a[9]);
         const DistillInputs in(a[2], a[3], a[4], a[5], a[6], c.device);
-        const at::Tensor loss = floats(a[7], c.device, in.logits.rows, "loss", in.logits);
-        const at::Tensor lse = floats(a[8], c.device, in.logits.rows, "lse", in.logits);
+        const at::Tensor loss = floats(a[7], c, in.logits.rows, "loss", in.logits);
+        const at::Tensor lse = floats(a[8], c, in.logits.rows, "lse", in.logits);
         const int s = g_distill_loss(c.h, in.logits.p(), in.logits.dtype, (int32_t)in.logits.rows, in.logits.step,
                                      (int32_t)in.logits.cols, in.mask, in.teacher.p(), in.teacher.dtype, in.ids,
                                      (int32_t)in.teacher.cols, in.temperature, (float*)loss.data_ptr(), (float*)lse.data_ptr(),
@@ -251,7 +281,7 @@ PyObject* distill_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const DistillInputs in(a[2], a[3], a[4], a[5], a[8], c.device);
         const at::Tensor &lse = words(a[6], c.device, at::kFloat, in.logits.rows, "lse"),
                          &g = words(a[7], c.device, at::kFloat, in.logits.rows, "grad_loss");
-        const Matrix out = output(a[9], c.device, "out", in.logits.rows, in.logits.cols, in.logits);
+        const Matrix out = output(a[9], c, "out", in.logits.rows, in.logits.cols, in.logits);
         const int s = g_distill_grad(c.h, in.logits.p(), in.logits.dtype, (int32_t)in.logits.rows, in.logits.step,
                                      (int32_t)in.logits.cols, in.mask, in.teacher.p(), in.teacher.dtype, in.ids,
                                      (int32_t)in.teacher.cols, in.temperature, (const float*)lse.data_ptr(),
@@ -268,7 +298,7 @@ PyObject* embed(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const Matrix w = matrix(a[3], c.device, "weight");
         words(a[2], c.device, at::kInt, t.numel(), "tokens");
         if (t.numel() > INT32_MAX) throw Refused{PyExc_ValueError, "tokens", "too large"};
-        const Matrix out = output(a[5], c.device, "out", t.numel(), w.cols, w);
+        const Matrix out = output(a[5], c, "out", t.numel(), w.cols, w);
         const int s = g_embed(c.h, (const int32_t*)t.data_ptr(), (int32_t)t.numel(), w.p(), w.step, w.dtype, (int32_t)w.rows,
                               (int32_t)w.cols, number(a[4], "scale"), out.p(), out.step, c.stream);
         return s ? PyLong_FromLong(s) : THPVariable_Wrap(out.t);
@@ -283,7 +313,7 @@ PyObject* embed_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor& t = words(a[2], c.device, at::kInt, g.rows, "tokens");
         const int32_t V = integer32(a[4], "n_tokens");
         if (V < 1) throw Refused{PyExc_ValueError, "n_tokens", "at least 1 expected"};
-        const Matrix dw = output(a[6], c.device, "into", V, g.cols, g);
+        const Matrix dw = output(a[6], c, "into", V, g.cols, g);
         const int s = g_embed_grad(c.h, (const int32_t*)t.data_ptr(), (int32_t)g.rows, g.p(), g.step, g.dtype, V,
                                    (int32_t)g.cols, number(a[5], "scale"), a[7] == Py_True ? 1 : 0, dw.p(), dw.step, c.stream);
         return s ? PyLong_FromLong(s) : THPVariable_Wrap(dw.t);
