@@ -154,7 +154,9 @@ at::Tensor floats(PyObject* o, const Call& c, int64_t n, const char* what, const
 const uint32_t* mask_words(PyObject* o, int device, int64_t rows, int64_t n_tokens) {
     if (o == Py_None) return nullptr;
     const at::Tensor& t = tensor(o, device, "mask");
-    if (t.dim() != 2 || t.size(0) != rows || t.size(1) != (n_tokens + 31) / 32 || t.element_size() != 4 || !t.is_contiguous())
+    if (t.scalar_type() != at::kInt && t.scalar_type() != at::kUInt32)
+        throw Refused{PyExc_TypeError, "mask", "must be int32 or uint32"};
+    if (t.dim() != 2 || t.size(0) != rows || t.size(1) != (n_tokens + 31) / 32 || !t.is_contiguous())
         throw Refused{PyExc_ValueError, "mask", "one contiguous row of ceil(n_tokens / 32) 32-bit words per row expected"};
     return (const uint32_t*)t.data_ptr();
 }
