@@ -428,8 +428,10 @@ int domino_token_loss(domino_t h, const void* hidden_dev, int64_t hidden_stride,
  *   dhidden = G weight, dweight = G^T hidden, in bf16, both written whole.
  * Rows without a target, or whose mask excludes it, have no gradient, whatever
  * their hidden values or grad_loss.  The logits are computed again, in pieces of the
- * vocabulary; G is rounded to bf16 before the two products, relative to the
- * largest |grad_loss|. */
+ * vocabulary.  G is rounded to bf16 before the two products, relative to the
+ * largest |grad_loss|: the gradients are about 2.2e-3 off in norm, 1.7e-3 of it
+ * their own rounding to bf16.  Calls of one or two rows, and some of three and
+ * four, keep G in fp32. */
 int domino_token_loss_grad(domino_t h, const void* hidden_dev, int64_t hidden_stride, const void* weight_dev,
                            int64_t weight_stride, int32_t dtype, int32_t rows, int32_t dim, int32_t n_tokens,
                            const uint32_t* mask_dev, const int32_t* targets_dev, const float* lse_dev,

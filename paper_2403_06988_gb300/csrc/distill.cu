@@ -103,9 +103,10 @@ __device__ __forceinline__ uint32_t allowed_bits(const uint32_t* mrow, int32_t t
     return bits & all;
 }
 
-// x / tau, rounded to fp32 wherever it is used: lse holds the largest one's rounding, and a difference from lse that kept the
-// product's other bits (one fma) would be off by up to half a unit in lse's last place, above zero too: exp of it passes all
-// bounds where that unit is large (logits that ban a token, 1e9 and more).
+// x / tau as a product with the inverse (a rounding more than a division), rounded to fp32 wherever it is used: lse holds the
+// largest one's rounding, and a difference from lse that kept the product's other bits (one fma) would be off by up to half a
+// unit in lse's last place, above zero too: exp of it passes all bounds where that unit is large (logits that ban a token, 1e9
+// and more).
 __device__ __forceinline__ float scaled(float x, const DistillCall& c) { return __fmul_rn(x, c.inv_tau); }
 
 __device__ __forceinline__ float2 merge(float2 a, float2 b, float k) {

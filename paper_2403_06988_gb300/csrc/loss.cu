@@ -68,7 +68,10 @@ constexpr int kGroupM = 16;                    // row tiles that share a pass ov
 // (256 x 128256 x 4096: lse 1.9e-6 off in one part of 64 blocks, 4e-7 in parts of
 // 16, 6e-7 of 24; 184 us in one part, 193, 192 and 192 in parts of 16, 24 and 32; 4096
 // rows 2060, 2120, 2100, 2064).  G is rounded to bf16, a thousand times as much: its
-// logits are summed in one.
+// logits are summed in one, and so is a split's part of G w, over up to a whole
+// piece of the vocabulary (4096 x 128256 x 4096 against 64 bits: dhidden 2.20e-3 off,
+// dweight 2.18e-3, 1.66e-3 of each the results' own rounding; their lengths along the
+// right ones are 1.7e-5 too short and 2.7e-5 too long: the cuts do not add up).
 constexpr int kDeepBlocks = 24;
 
 // What becomes of a tile of products.
@@ -626,9 +629,11 @@ __device__ __forceinline__ float row_coef(const Prep& p, int32_t t, uint32_t* re
 }
 
 // Coefficients over the largest finite one's magnitude: what G is rounded from.
-// G is kept in bf16, so a coefficient that all rows share (a mean's 1 / rows)
-// would otherwise be off by one rounding, the same in every entry; the scale is
-// given back in fp32.
+// G is kept in bf16, as the tensor cores take it: the gradients are 2.2e-3 off where
+// their own rounding alone makes 1.66e-3, and a second part of G for the bits that go
+// would be two products more.  A coefficient that all rows share (a mean's 1 / rows)
+// would be off by one rounding, the same in every entry, if it were in G; the scale
+// is given back in fp32.
 __device__ void make_coefs(const Prep& p) {
     __shared__ float s_top[kPackThreads / 32];
     float top = 0.0f;
@@ -668,7 +673,8 @@ __global__ void __launch_bounds__(kPackThreads) prep_kernel(const __grid_constan
 }
 
 // dhidden = scale * the sum of the planes.  PARTS threads share a vector's planes
-// (a chain of up to 76 loads would take longer than the rest of a small call).
+// (of one column tile as many as SMs: a chain of 152 loads, 19 with eight threads,
+// would take longer than the rest of a small call).
 template <int PARTS>
 __global__ void __launch_bounds__(kPackThreads)
     dhidden_kernel(const float* planes, int32_t splits, int64_t plane, int32_t rows, int32_t cols, int32_t pitch,
