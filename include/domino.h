@@ -33,7 +33,7 @@
  *    them on one stream, or order the streams with events): the handle's
  *    scratch (the fused decode's partials, opportunistic masking's row list,
  *    the host-buffer step's staging, that of the losses and of the embedding's
- *    gradient) is shared by its calls.
+ *    and the norm's gradient) is shared by its calls.
  *    Different handles are independent.
  */
 #ifndef DOMINO_H
@@ -479,6 +479,104 @@ int domino_embed(domino_t h, const int32_t* tokens_dev, int32_t n, const void* w
 int domino_embed_grad(domino_t h, const int32_t* tokens_dev, int32_t n, const void* grad_dev, int64_t grad_stride,
                       int32_t dtype, int32_t n_tokens, int32_t dim, float scale, int32_t accumulate,
                       void* dweight_dev, int64_t dweight_stride, void* stream);
+
+/* ---- Norm, 8-bit operands, decode under penalties ---------------------------------
+ *
+ * Not steps of the paper: what stands between a model's last block and the masked
+ * decode.  As with the losses above, a handle with a device but no loaded vocabulary
+ * is needed, rows = 0 is allowed, at most 2^31 - 2^20 - 1 rows, 1 <= dim <= 2^20,
+ * 1 <= n_tokens <= 2^24, pointers are multiples of their values' size, strides are in
+ * elements, results are the same on every run and values are finite.
+ *
+ * Codes are e4m3 (8 bits: 4 of exponent, 3 of mantissa, largest 448) with a float
+ * scale for each block of 128 values along a row (the last block of a row may be
+ * shorter), for one row or for 128 rows together:
+ *   a = the largest |v| of the block, at least 2^-100;  scale = a / 448;
+ *   code = e4m3(v (448 / a)), ties to even;  v is about code * scale.
+ * Rows of codes begin on 16-byte boundaries (pointer and stride are multiples of 16,
+ * DOMINO_E_INVALID_ARG else); bytes of a row at or beyond dim are neither read nor
+ * written. */
+
+/* Root-mean-square norm of x + residual:
+ *   sum = x + residual, rounded to the stream's type,
+ *   rstd = 1 / sqrt(mean(sum^2) + eps),  y = sum rstd weight.
+ * x_dev, residual_dev (NULL: none), sum_dev (required with a residual, NULL else), y_dev
+ * [rows][stride], weight_dev [dim], all of dtype (fp32 or bf16); rstd_dev float [rows] or
+ * NULL.  sum_dev may be residual_dev or x_dev, with the same stride.  eps >= 0 and
+ * finite; a row of zeros with eps = 0 has no norm (NaN).  Needs no scratch. */
+int domino_norm(domino_t h, const void* x_dev, int64_t x_stride, const void* residual_dev, int64_t residual_stride,
+                const void* weight_dev, int32_t dtype, int32_t rows, int32_t dim, float eps, void* y_dev,
+                int64_t y_stride, void* sum_dev, int64_t sum_stride, float* rstd_dev, void* stream);
+
+/* The same with y in codes, rounded once from fp32: codes_dev [rows][codes_stride],
+ * scales_dev [rows][ceil(dim / 128)]. */
+int domino_norm8(domino_t h, const void* x_dev, int64_t x_stride, const void* residual_dev, int64_t residual_stride,
+                 const void* weight_dev, int32_t dtype, int32_t rows, int32_t dim, float eps, uint8_t* codes_dev,
+                 int64_t codes_stride, float* scales_dev, void* sum_dev, int64_t sum_stride, void* stream);
+
+/* Gradient of domino_norm: with h = sum_dev and rstd_dev as written by it (h = x where
+ * there was no residual), dy the gradient of y and dsum that of the sum's other uses
+ * (NULL: none),
+ *   g = weight dy,  dx = rstd (g - h rstd^2 mean(g h)) + dsum   (of x and of the residual),
+ *   dweight = the sum over the rows of dy h rstd,
+ * all of dtype, rounded once.  dx_dev may be dsum_dev or dy_dev, with the same
+ * stride.  Takes scratch: up to 16 times as many fp32 rows of dim as the GPU has SMs. */
+int domino_norm_grad(domino_t h, const void* sum_dev, int64_t sum_stride, const void* weight_dev, const float* rstd_dev,
+                     const void* dy_dev, int64_t dy_stride, const void* dsum_dev, int64_t dsum_stride, int32_t dtype,
+                     int32_t rows, int32_t dim, void* dx_dev, int64_t dx_stride, void* dweight_dev, void* stream);
+
+/* A matrix [rows][stride] of dtype in codes.  block_rows = 1: scales_dev [rows][ceil(dim / 128)]
+ * (hidden states); 128: scales_dev [ceil(rows / 128)][ceil(dim / 128)], one for 128 x 128
+ * values (a weight).  Needs no scratch. */
+int domino_quantize8(domino_t h, const void* x_dev, int64_t x_stride, int32_t dtype, int32_t rows, int32_t dim,
+                     int32_t block_rows, uint8_t* codes_dev, int64_t codes_stride, float* scales_dev, void* stream);
+
+/* Logits of hidden states and a weight in codes:
+ *   logits[t][v] = sum over blocks b of hidden_scales[t][b] weight_scales[v / 128][b]
+ *                  (sum over the block's k of hidden[t][k] weight[v][k]).
+ * hidden_dev [rows][hidden_stride] with scales [rows][ceil(dim / 128)]; weight_dev
+ * [n_tokens][weight_stride] with scales [ceil(n_tokens / 128)][ceil(dim / 128)]; logits_dev
+ * [rows][logits_stride] of dtype (fp32 or bf16).  Sums are fp32, rounded once to dtype.
+ * Logits whose rows are on 16-byte boundaries are written faster.  Needs no scratch. */
+int domino_logits8(domino_t h, const uint8_t* hidden_dev, int64_t hidden_stride, const float* hidden_scales_dev,
+                   const uint8_t* weight_dev, int64_t weight_stride, const float* weight_scales_dev, int32_t rows,
+                   int32_t dim, int32_t n_tokens, int32_t dtype, void* logits_dev, int64_t logits_stride, void* stream);
+
+/* Penalties for what a row has said, and biases: device memory.  history_dev may be NULL where history_len is 0, the
+ * biases where n_bias is 0, and every other pointer. */
+typedef struct {
+    const int32_t* history_dev;        /* [batch][history_len]: prompt, then generated tokens; below 0: no token */
+    const int32_t* lengths_dev;        /* [batch]: of each row's history; NULL: history_len */
+    const int32_t* prompt_lengths_dev; /* [batch]: positions of it that are the prompt's; NULL: 0 */
+    const float* repetition_dev;       /* [batch], above 0; NULL: 1 */
+    const float* presence_dev;         /* [batch]; NULL: 0 */
+    const float* frequency_dev;        /* [batch]; NULL: 0 */
+    const int32_t* bias_ids_dev;       /* [batch][n_bias]; below 0: none; of equal ids the first counts */
+    const float* bias_values_dev;      /* [batch][n_bias], finite or -inf */
+    int32_t history_len;               /* >= 0 */
+    int32_t n_bias;                    /* 0 .. 1024 */
+} domino_penalties;
+
+/* domino_mask_logits of penalised logits.  With n the number of times that token v
+ * occurs in the row's history and c the number beyond the prompt's positions, in fp32
+ * with every step rounded:
+ *   x = logits[v];  n > 0: x = x > 0 ? x / repetition : x repetition;
+ *   c > 0: x = x - frequency c, then x - presence;  x = x + bias of v.
+ * logits_dev, mask_dev (NULL: every token allowed), argmax_dev, lse_dev and logprobs_dev
+ * (of the penalised logits) as there; the logits themselves are not changed.
+ * A history token or bias id at or beyond n_tokens sets DOMINO_DEVERR_BAD_TOKEN and
+ * counts as below 0; so does a length outside [0, history_len], which counts as the
+ * nearer end.  Needs no scratch. */
+int domino_mask_logits_penalized(domino_t h, const void* logits_dev, int32_t dtype, int32_t batch,
+                                 int64_t row_stride_elems, int32_t n_tokens, const domino_penalties* penalties,
+                                 const uint32_t* mask_dev, int32_t* argmax_dev, float* lse_dev, float* logprobs_dev,
+                                 void* stream);
+
+/* domino_mask_sample of penalised logits: the draw that it makes from them. */
+int domino_mask_sample_penalized(domino_t h, const void* logits_dev, int32_t dtype, int32_t batch,
+                                 int64_t row_stride_elems, int32_t n_tokens, const domino_penalties* penalties,
+                                 const uint32_t* mask_dev, float temperature, uint64_t seed, uint64_t offset,
+                                 int32_t* tokens_dev, void* stream);
 
 /* Synchronises `stream`, returns the sticky device error word (DOMINO_DEVERR_*
  * bits, 0 = none) in *code and clears it. */

@@ -20,7 +20,8 @@ _CALLS = None
 
 
 def _calls():
-    """The extension that the losses and the embedding are called through (csrc/calls.cpp), bound to the loaded library."""
+    """The extension that the losses, the embedding, the norm, 8-bit operands and the decode under penalties are called
+    through (csrc/calls.cpp), bound to the loaded library."""
     global _CALLS
     if _CALLS is None:
         import ctypes
@@ -32,7 +33,8 @@ def _calls():
                               "python -m paper_2403_06988_gb300.build")
         from . import _loss_calls as c
         c.bind(*(ctypes.cast(getattr(B.lib(), "domino_" + n), ctypes.c_void_p).value
-                 for n in ("token_loss", "token_loss_grad", "distill_loss", "distill_grad", "embed", "embed_grad")))
+                 for n in ("token_loss", "token_loss_grad", "distill_loss", "distill_grad", "embed", "embed_grad", "norm",
+                           "norm8", "norm_grad", "quantize8", "logits8", "mask_logits_penalized", "mask_sample_penalized")))
         _CALLS = c
     return _CALLS
 
@@ -301,6 +303,107 @@ class Domino:
         return self._result("domino_embed_grad", _calls().embed_grad(
             self.h, self.device, tokens, grad, n_tokens, scale, out, into is not None,
             None if stream is None else B._stream(stream)))
+
+    # -- norm, 8-bit operands, decode under penalties (no loaded vocabulary needed; as above, autograd does not see them) ---
+    def _fill_codes(self, out, rows, cols, like, stream):
+        """_fill of codes: rows on 16-byte boundaries."""
+        import torch
+        if out is not None or self.fill_byte is None:
+            return out
+        return self._empty((rows, -(-cols // 16) * 16), torch.float8_e4m3fn, like.device, stream)[:, :cols]
+
+    def norm(self, x, weight, residual=None, eps: float = 1e-6, out=None, stream=None) -> Tuple:
+        """Root-mean-square norm of x + residual: (y, sum, rstd).  x, residual [rows, dim], weight [dim], y and sum of one
+        type, bf16 or fp32; rstd fp32 [rows].  Without a residual sum is x itself.  out: (y, sum, rstd) to write to; its
+        sum may be x or residual."""
+        import torch
+        y, h, rstd = out if out is not None else (None, None, None)
+        if self.fill_byte is not None:
+            y = self._fill(y, *x.shape, x.dtype, x, stream)
+            h = self._fill(h, *x.shape, x.dtype, x, stream) if residual is not None else h
+            rstd = self._fill(rstd, x.shape[0], None, torch.float32, x, stream)
+        return self._result("domino_norm", _calls().norm(
+            self.h, self.device, x, weight, residual, eps, y, h, rstd, None if stream is None else B._stream(stream)))
+
+    def norm8(self, x, weight, residual=None, eps: float = 1e-6, out=None, stream=None) -> Tuple:
+        """norm with y as logits8 takes it: (codes, scales, sum).  codes float8_e4m3fn [rows, dim], its rows on 16-byte
+        boundaries; scales fp32 [rows, ceil(dim / 128)]."""
+        import torch
+        q, sc, h = out if out is not None else (None, None, None)
+        if self.fill_byte is not None:
+            q = self._fill_codes(q, *x.shape, x, stream)
+            sc = self._fill(sc, x.shape[0], -(-x.shape[1] // 128), torch.float32, x, stream)
+            h = self._fill(h, *x.shape, x.dtype, x, stream) if residual is not None else h
+        return self._result("domino_norm8", _calls().norm8(
+            self.h, self.device, x, weight, residual, eps, q, sc, h, None if stream is None else B._stream(stream)))
+
+    def norm_grad(self, sum, weight, rstd, dy, dsum=None, out=None, stream=None) -> Tuple:
+        """(dx, dweight): dx the gradient of x and of the residual alike, from dy and the gradient dsum of the sum's other
+        uses; sum and rstd as norm returned them.  out: (dx, dweight) to write to; its dx may be dy or dsum."""
+        dx, dw = out if out is not None else (None, None)
+        if self.fill_byte is not None:
+            dx = self._fill(dx, *sum.shape, sum.dtype, sum, stream)
+            dw = self._fill(dw, sum.shape[1], None, sum.dtype, sum, stream)
+        return self._result("domino_norm_grad", _calls().norm_grad(
+            self.h, self.device, sum, weight, rstd, dy, dsum, dx, dw, None if stream is None else B._stream(stream)))
+
+    def quantize8(self, x, block: int = 1, out=None, stream=None) -> Tuple:
+        """(codes, scales) of a matrix: a scale for each 1 x 128 values (block 1, hidden states) or 128 x 128 (block 128, a
+        weight); see norm8."""
+        import torch
+        q, sc = out if out is not None else (None, None)
+        if self.fill_byte is not None:
+            q = self._fill_codes(q, *x.shape, x, stream)
+            sc = self._fill(sc, x.shape[0] if block == 1 else -(-x.shape[0] // 128), -(-x.shape[1] // 128), torch.float32, x, stream)
+        return self._result("domino_quantize8", _calls().quantize8(
+            self.h, self.device, x, block, q, sc, None if stream is None else B._stream(stream)))
+
+    def logits8(self, codes, scales, weight_codes, weight_scales, dtype=None, out=None, stream=None):
+        """hidden @ weight.T of codes: [rows, n_tokens] in dtype (fp32 unless bf16 is asked for), rows on 16-byte boundaries.
+        codes, scales: the hidden states', by norm8 or quantize8; weight_codes, weight_scales: by quantize8(weight, 128)."""
+        import torch
+        if dtype is None:
+            dtype = torch.float32 if out is None else out.dtype
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError("dtype must be float32 or bfloat16")
+        if out is None and self.fill_byte is not None:
+            n, per = weight_codes.shape[0], 16 // dtype.itemsize
+            out = self._empty((codes.shape[0], -(-n // per) * per), dtype, codes.device, stream)[:, :n]
+        return self._result("domino_logits8", _calls().logits8(
+            self.h, self.device, codes, scales, weight_codes, weight_scales, dtype == torch.bfloat16, out,
+            None if stream is None else B._stream(stream)))
+
+    def mask_logits_penalized(self, logits, history=None, lengths=None, prompt_lengths=None, repetition=None, presence=None,
+                              frequency=None, bias_ids=None, bias_values=None, mask=None, want_lse: bool = True,
+                              want_logprobs: bool = False, out=None, stream=None) -> Tuple:
+        """mask_logits of logits under penalties for what each row has said, and biases: (argmax, lse or None, logprobs or
+        None).  history int32 [rows, n], the prompt's prompt_lengths tokens and then the generated ones, lengths of it in
+        use (below 0: no token): a token in it has its logit divided by repetition (multiplied where it is not above 0); of
+        those beyond the prompt one that occurs c times loses frequency * c + presence.  bias_values are added to the
+        logits of bias_ids [rows, k] (below 0: none).  lengths, prompt_lengths int32 and the penalties fp32 [rows]; what is
+        None penalises nothing.  mask as step_mask's or None.  The logits are not changed."""
+        import torch
+        argmax, lse, lp = out if out is not None else (None, None, None)
+        if self.fill_byte is not None:
+            n = logits.shape[0]
+            argmax = self._fill(argmax, n, None, torch.int32, logits, stream)
+            lse = self._fill(lse, n, None, torch.float32, logits, stream) if want_lse else None
+            lp = self._fill(lp, *logits.shape, torch.float32, logits, stream) if want_logprobs else None
+        return self._result("domino_mask_logits_penalized", _calls().mask_logits_penalized(
+            self.h, self.device, logits, history, lengths, prompt_lengths, repetition, presence, frequency, bias_ids, bias_values,
+            mask, argmax, None if not want_lse else True if lse is None else lse,
+            None if not want_logprobs else True if lp is None else lp, None if stream is None else B._stream(stream)))
+
+    def mask_sample_penalized(self, logits, temperature: float, seed: int, offset: int, history=None, lengths=None,
+                              prompt_lengths=None, repetition=None, presence=None, frequency=None, bias_ids=None,
+                              bias_values=None, mask=None, out=None, stream=None):
+        """mask_sample of logits under mask_logits_penalized's penalties and biases."""
+        import torch
+        if self.fill_byte is not None:
+            out = self._fill(out, logits.shape[0], None, torch.int32, logits, stream)
+        return self._result("domino_mask_sample_penalized", _calls().mask_sample_penalized(
+            self.h, self.device, logits, history, lengths, prompt_lengths, repetition, presence, frequency, bias_ids, bias_values,
+            mask, temperature, seed, offset, out, None if stream is None else B._stream(stream)))
 
     def device_error(self, stream=None) -> int:
         return B.domino_get_device_error(self.h, stream)

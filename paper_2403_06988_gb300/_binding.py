@@ -50,6 +50,12 @@ class Info(ctypes.Structure):
                                                               ("tree_units", ctypes.c_int32)]
 
 
+class Penalties(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in (
+        "history_dev", "lengths_dev", "prompt_lengths_dev", "repetition_dev", "presence_dev", "frequency_dev", "bias_ids_dev",
+        "bias_values_dev")] + [("history_len", ctypes.c_int32), ("n_bias", ctypes.c_int32)]
+
+
 _lib = None
 P = ctypes.c_void_p
 I32 = ctypes.c_int32
@@ -84,6 +90,13 @@ _SIGS = {
     "domino_distill_grad": [P, P, I32, I32, I64, I32, P, P, I32, P, I32, ctypes.c_float, P, P, P, I64, P],
     "domino_embed": [P, P, I32, P, I64, I32, I32, I32, ctypes.c_float, P, I64, P],
     "domino_embed_grad": [P, P, I32, P, I64, I32, I32, I32, ctypes.c_float, I32, P, I64, P],
+    "domino_norm": [P, P, I64, P, I64, P, I32, I32, I32, ctypes.c_float, P, I64, P, I64, P, P],
+    "domino_norm8": [P, P, I64, P, I64, P, I32, I32, I32, ctypes.c_float, P, I64, P, P, I64, P],
+    "domino_norm_grad": [P, P, I64, P, P, P, I64, P, I64, I32, I32, I32, P, I64, P, P],
+    "domino_quantize8": [P, P, I64, I32, I32, I32, I32, P, I64, P, P],
+    "domino_logits8": [P, P, I64, P, P, I64, P, I32, I32, I32, I32, P, I64, P],
+    "domino_mask_logits_penalized": [P, P, I32, I32, I64, I32, P, P, P, P, P, P],
+    "domino_mask_sample_penalized": [P, P, I32, I32, I64, I32, P, P, ctypes.c_float, ctypes.c_uint64, ctypes.c_uint64, P, P],
 }
 
 
@@ -381,6 +394,83 @@ def domino_embed_grad(h: int, tokens_dev, n: int, grad_dev, grad_stride: int, dt
                                  scale, accumulate, _address(dweight_dev), dweight_stride, _stream(stream))
     if rc:
         _check("domino_embed_grad", rc)
+
+
+def domino_norm(h: int, x_dev, x_stride: int, residual_dev, residual_stride: int, weight_dev, dtype: int, rows: int,
+                dim: int, eps: float, y_dev, y_stride: int, sum_dev=None, sum_stride: int = 0, rstd_dev=None, stream=None) -> None:
+    rc = lib().domino_norm(h, _address(x_dev), x_stride, _address(residual_dev), residual_stride, _address(weight_dev), dtype,
+                           rows, dim, eps, _address(y_dev), y_stride, _address(sum_dev), sum_stride, _address(rstd_dev),
+                           _stream(stream))
+    if rc:
+        _check("domino_norm", rc)
+
+
+def domino_norm8(h: int, x_dev, x_stride: int, residual_dev, residual_stride: int, weight_dev, dtype: int, rows: int,
+                 dim: int, eps: float, codes_dev, codes_stride: int, scales_dev, sum_dev=None, sum_stride: int = 0,
+                 stream=None) -> None:
+    rc = lib().domino_norm8(h, _address(x_dev), x_stride, _address(residual_dev), residual_stride, _address(weight_dev), dtype,
+                            rows, dim, eps, _address(codes_dev), codes_stride, _address(scales_dev), _address(sum_dev),
+                            sum_stride, _stream(stream))
+    if rc:
+        _check("domino_norm8", rc)
+
+
+def domino_norm_grad(h: int, sum_dev, sum_stride: int, weight_dev, rstd_dev, dy_dev, dy_stride: int, dsum_dev,
+                     dsum_stride: int, dtype: int, rows: int, dim: int, dx_dev, dx_stride: int, dweight_dev,
+                     stream=None) -> None:
+    rc = lib().domino_norm_grad(h, _address(sum_dev), sum_stride, _address(weight_dev), _address(rstd_dev), _address(dy_dev),
+                                dy_stride, _address(dsum_dev), dsum_stride, dtype, rows, dim, _address(dx_dev), dx_stride,
+                                _address(dweight_dev), _stream(stream))
+    if rc:
+        _check("domino_norm_grad", rc)
+
+
+def domino_quantize8(h: int, x_dev, x_stride: int, dtype: int, rows: int, dim: int, block_rows: int, codes_dev,
+                     codes_stride: int, scales_dev, stream=None) -> None:
+    rc = lib().domino_quantize8(h, _address(x_dev), x_stride, dtype, rows, dim, block_rows, _address(codes_dev), codes_stride,
+                                _address(scales_dev), _stream(stream))
+    if rc:
+        _check("domino_quantize8", rc)
+
+
+def domino_logits8(h: int, hidden_dev, hidden_stride: int, hidden_scales_dev, weight_dev, weight_stride: int,
+                   weight_scales_dev, rows: int, dim: int, n_tokens: int, dtype: int, logits_dev, logits_stride: int,
+                   stream=None) -> None:
+    rc = lib().domino_logits8(h, _address(hidden_dev), hidden_stride, _address(hidden_scales_dev), _address(weight_dev),
+                              weight_stride, _address(weight_scales_dev), rows, dim, n_tokens, dtype, _address(logits_dev),
+                              logits_stride, _stream(stream))
+    if rc:
+        _check("domino_logits8", rc)
+
+
+def penalties(history_dev=None, history_len: int = 0, lengths_dev=None, prompt_lengths_dev=None, repetition_dev=None,
+              presence_dev=None, frequency_dev=None, bias_ids_dev=None, bias_values_dev=None, n_bias: int = 0) -> Penalties:
+    return Penalties(_address(history_dev), _address(lengths_dev), _address(prompt_lengths_dev), _address(repetition_dev),
+                     _address(presence_dev), _address(frequency_dev), _address(bias_ids_dev), _address(bias_values_dev),
+                     history_len, n_bias)
+
+
+def _penalties(p):
+    return None if p is None else ctypes.addressof(p)
+
+
+def domino_mask_logits_penalized(h: int, logits_dev, dtype: int, batch: int, row_stride_elems: int, n_tokens: int, penalties,
+                                 mask_dev, argmax_dev, lse_dev=None, logprobs_dev=None, stream=None) -> None:
+    rc = lib().domino_mask_logits_penalized(h, _address(logits_dev), dtype, batch, row_stride_elems, n_tokens,
+                                            _penalties(penalties), _address(mask_dev), _address(argmax_dev), _address(lse_dev),
+                                            _address(logprobs_dev), _stream(stream))
+    if rc:
+        _check("domino_mask_logits_penalized", rc)
+
+
+def domino_mask_sample_penalized(h: int, logits_dev, dtype: int, batch: int, row_stride_elems: int, n_tokens: int, penalties,
+                                 mask_dev, temperature: float, seed: int, offset: int, tokens_dev, stream=None) -> None:
+    rc = lib().domino_mask_sample_penalized(h, _address(logits_dev), dtype, batch, row_stride_elems, n_tokens,
+                                            _penalties(penalties), _address(mask_dev), temperature,
+                                            seed & 0xFFFFFFFFFFFFFFFF, offset & 0xFFFFFFFFFFFFFFFF, _address(tokens_dev),
+                                            _stream(stream))
+    if rc:
+        _check("domino_mask_sample_penalized", rc)
 
 
 def domino_get_device_error(h: int, stream=None) -> int:

@@ -1,7 +1,8 @@
 """Builds libdomino.so in-tree with nvcc for sm_103a (GB300).
 
-Eight translation units (host.cpp: C ABI and loaders; kernels.cu, rows.cu, logits.cu,
-loss.cu, loss_few.cu, distill.cu and embed.cu: kernels) are compiled in parallel and linked into paper_2403_06988_gb300/libdomino.so.
+Twelve translation units (host.cpp: C ABI and loaders; kernels.cu, rows.cu, logits.cu,
+loss.cu, loss_few.cu, distill.cu, embed.cu, norm.cu, quantize8.cu, logits8.cu and penalized.cu:
+kernels) are compiled in parallel and linked into paper_2403_06988_gb300/libdomino.so.
 Objects go to paper_2403_06988_gb300/_build/.
 
 csrc/calls.cpp becomes the Python extension _loss_calls.so beside it (g++, against the
@@ -32,7 +33,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libdomino.so")
 LIB_DEBUG = os.path.join(PKG, "libdomino_debug.so")
 CALLS = os.path.join(PKG, "_loss_calls.so")
-SOURCES = ["host.cpp", "kernels.cu", "rows.cu", "logits.cu", "loss.cu", "loss_few.cu", "distill.cu", "embed.cu"]
+SOURCES = ["host.cpp", "kernels.cu", "rows.cu", "logits.cu", "loss.cu", "loss_few.cu", "distill.cu", "embed.cu",
+           "norm.cu", "quantize8.cu", "logits8.cu", "penalized.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -45,9 +47,9 @@ def nvcc() -> str:
 
 def _inputs():
     files = [os.path.join(CSRC, f) for f in SOURCES]
-    files += [os.path.join(CSRC, "domino_internal.h"), os.path.join(CSRC, "walk_common.cuh"),
-              os.path.join(CSRC, "decode.cuh"), os.path.join(CSRC, "loss.h"), os.path.join(CSRC, "tcgen05.cuh"), os.path.join(CSRC, "bf16_rows.cuh"),
-              os.path.join(INCLUDE, "domino.h")]
+    files += [os.path.join(CSRC, f) for f in ("domino_internal.h", "walk_common.cuh", "decode.cuh", "loss.h", "norm.h", "tcgen05.cuh",
+                                              "tensor_map.h", "bf16_rows.cuh", "values8.cuh")]
+    files.append(os.path.join(INCLUDE, "domino.h"))
     return files
 
 

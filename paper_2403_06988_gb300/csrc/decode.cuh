@@ -1,6 +1,7 @@
 // decode.cuh -- the masked decode of one row by one CTA (or a cluster of CTAs
 // that share out the row's tokens), used by the mask step that decodes its row
-// at once (rows.cu) and by the decode of given masks (logits.cu): masked
+// at once (rows.cu), by the decode of given masks (logits.cu) and by that of
+// penalised logits (penalized.cu): masked
 // maximum, lowest-index argmax and sum of exponentials, or a Gumbel-max draw,
 // over bf16 or fp32 logits at any alignment, and the log-probabilities.
 //
@@ -147,6 +148,19 @@ __device__ __forceinline__ float ln_rn(float x) {
     const float r = __fmul_rn(__fadd_rn(z, z), p);
     const float ef = __int2float_rn(e);
     return __fmaf_rn(ef, 0x1.62e43p-1f, __fmaf_rn(ef, -0x1.05c61p-29f, r));
+}
+
+// Gumbel variate of token t of row r: g_t = -ln(-ln(u_t)), u_t = (2k + 1) / 2^24,
+// k = (word t % 4 of Philox on (t / 4, r, offset)) >> 9.  `blk` / `rnd` cache
+// the last Philox block.
+__device__ __forceinline__ float gumbel(const SampleArgs& a, int r, int t, int& blk, uint4& rnd) {
+    if ((t >> 2) != blk) {
+        blk = t >> 2;
+        rnd = philox10(make_uint4((uint32_t)blk, (uint32_t)r, a.off0, a.off1), a.key0, a.key1);
+    }
+    const uint32_t w = (t & 2) ? ((t & 1) ? rnd.w : rnd.z) : ((t & 1) ? rnd.y : rnd.x);
+    const float u = __fmul_rn(__uint2float_rn(2u * (w >> 9) + 1u), 0x1p-24f);
+    return -ln_rn(-ln_rn(u));
 }
 
 // Every Gumbel variate is below this: u <= 1 - 2^-24 gives -ln(u) >= 5.96e-8

@@ -19,6 +19,7 @@
 #include "domino.h"
 #include "domino_internal.h"
 #include "loss.h"
+#include "norm.h"
 
 using namespace domino;
 
@@ -2197,6 +2198,223 @@ int domino_embed_grad(domino_t h, const int32_t* tokens_dev, int32_t n, const vo
     return cuda_status(launch_embed_grad(a, h->env, h->d_space.p, st));
 } catch (...) {   // std::bad_alloc
     return DOMINO_E_OOM;
+}
+
+// ---- norm, 8-bit operands, decode under penalties -----------------------------------
+namespace {
+
+int norm_args(NormArgs& a, domino_ctx* h, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
+              const void* weight, int32_t dtype, int32_t rows, int32_t dim, float eps, void* sum, int64_t sum_stride) {
+    if (int rc = device_handle(h)) return rc;
+    const size_t size = type_size(dtype);
+    if (!is_dtype(dtype) || rows < 0 || dim < 1 || dim > kMaxDim || x_stride < dim || !weight || (rows > 0 && !x) ||
+        !(eps >= 0.0f) || !std::isfinite(eps) || !on_values(x, size) || !on_values(weight, size) ||
+        (residual && (residual_stride < dim || !on_values(residual, size))) || (rows > 0 && !residual != !sum) ||
+        (sum && (sum_stride < dim || !on_values(sum, size) || (sum == x && sum_stride != x_stride) ||
+                 (sum == residual && sum_stride != residual_stride))))
+        return DOMINO_E_INVALID_ARG;
+    if (rows > kMaxRows) return DOMINO_E_UNSUPPORTED;
+    a = NormArgs{};
+    a.x = x;
+    a.x_stride = x_stride;
+    a.residual = residual;
+    a.residual_stride = residual_stride;
+    a.weight = weight;
+    a.sum = sum;
+    a.sum_stride = sum_stride;
+    a.rows = rows;
+    a.dim = dim;
+    a.dtype = dtype;
+    a.eps = eps;
+    return DOMINO_OK;
+}
+
+// Rows of codes begin on 16-byte boundaries.
+bool code_rows(const void* p, int64_t stride, int32_t dim) { return stride >= dim && stride % 16 == 0 && on_values(p, 16); }
+
+int penalized_args(PenalizedArgs& a, domino_ctx* h, const void* logits, int32_t dtype, int32_t batch, int64_t stride,
+                   int32_t n_tokens, const domino_penalties* p, const uint32_t* mask) {
+    if (int rc = device_handle(h)) return rc;
+    if (!is_dtype(dtype) || batch < 0 || n_tokens < 1 || n_tokens > kMaxTokens || stride < n_tokens || !p ||
+        (batch > 0 && !logits) || p->history_len < 0 || p->n_bias < 0 || p->n_bias > kMaxBias ||
+        (batch > 0 && ((p->n_bias > 0 && (!p->bias_ids_dev || !p->bias_values_dev)) || (p->history_len > 0 && !p->history_dev))) ||
+        !on_values(logits, type_size(dtype)) ||
+        !on_words(mask, p->history_dev, p->lengths_dev, p->prompt_lengths_dev) ||
+        !on_words(p->repetition_dev, p->presence_dev, p->frequency_dev) || !on_words(p->bias_ids_dev, p->bias_values_dev))
+        return DOMINO_E_INVALID_ARG;
+    if (batch > INT32_MAX / 8) return DOMINO_E_UNSUPPORTED;   // up to eight CTAs a row
+    a = PenalizedArgs{};
+    a.logits = logits;
+    a.stride = stride;
+    a.batch = batch;
+    a.n_tokens = n_tokens;
+    a.dtype = dtype;
+    a.p = *p;
+    a.mask = mask;
+    a.err = (uint32_t*)h->d_err.p;
+    return DOMINO_OK;
+}
+
+}  // namespace
+
+int domino_norm(domino_t h, const void* x_dev, int64_t x_stride, const void* residual_dev, int64_t residual_stride,
+                const void* weight_dev, int32_t dtype, int32_t rows, int32_t dim, float eps, void* y_dev,
+                int64_t y_stride, void* sum_dev, int64_t sum_stride, float* rstd_dev, void* stream) {
+    DOMINO_API_RANGE();
+    NormArgs a;
+    if (int rc = norm_args(a, h, x_dev, x_stride, residual_dev, residual_stride, weight_dev, dtype, rows, dim, eps, sum_dev, sum_stride))
+        return rc;
+    if (y_stride < dim || (rows > 0 && !y_dev) || !on_values(y_dev, type_size(dtype)) || !on_words(rstd_dev)) return DOMINO_E_INVALID_ARG;
+    if (rows == 0) return DOMINO_OK;
+    a.y = y_dev;
+    a.y_stride = y_stride;
+    a.rstd = rstd_dev;
+    DeviceGuard g(h->device);
+    return cuda_status(launch_norm(a, h->env, (cudaStream_t)stream));
+}
+
+int domino_norm8(domino_t h, const void* x_dev, int64_t x_stride, const void* residual_dev, int64_t residual_stride,
+                 const void* weight_dev, int32_t dtype, int32_t rows, int32_t dim, float eps, uint8_t* codes_dev,
+                 int64_t codes_stride, float* scales_dev, void* sum_dev, int64_t sum_stride, void* stream) {
+    DOMINO_API_RANGE();
+    NormArgs a;
+    if (int rc = norm_args(a, h, x_dev, x_stride, residual_dev, residual_stride, weight_dev, dtype, rows, dim, eps, sum_dev, sum_stride))
+        return rc;
+    if (!code_rows(codes_dev, codes_stride, dim) || (rows > 0 && (!codes_dev || !scales_dev)) || !on_words(scales_dev))
+        return DOMINO_E_INVALID_ARG;
+    if (rows == 0) return DOMINO_OK;
+    a.codes = codes_dev;
+    a.codes_stride = codes_stride;
+    a.scales = scales_dev;
+    DeviceGuard g(h->device);
+    return cuda_status(launch_norm(a, h->env, (cudaStream_t)stream));
+}
+
+int domino_norm_grad(domino_t h, const void* sum_dev, int64_t sum_stride, const void* weight_dev, const float* rstd_dev,
+                     const void* dy_dev, int64_t dy_stride, const void* dsum_dev, int64_t dsum_stride, int32_t dtype,
+                     int32_t rows, int32_t dim, void* dx_dev, int64_t dx_stride, void* dweight_dev, void* stream) try {
+    DOMINO_API_RANGE();
+    if (int rc = device_handle(h)) return rc;
+    const size_t size = type_size(dtype);
+    if (!is_dtype(dtype) || rows < 0 || dim < 1 || dim > kMaxDim || sum_stride < dim || dy_stride < dim || dx_stride < dim ||
+        (dsum_dev && dsum_stride < dim) || !weight_dev || !dweight_dev ||
+        (rows > 0 && (!sum_dev || !rstd_dev || !dy_dev || !dx_dev)) || !on_values(sum_dev, size) || !on_values(weight_dev, size) ||
+        !on_values(dy_dev, size) || !on_values(dsum_dev, size) || !on_values(dx_dev, size) || !on_values(dweight_dev, size) ||
+        !on_words(rstd_dev) || (dx_dev && dx_dev == dy_dev && dx_stride != dy_stride) ||
+        (dx_dev && dx_dev == dsum_dev && dx_stride != dsum_stride))
+        return DOMINO_E_INVALID_ARG;
+    if (rows > kMaxRows) return DOMINO_E_UNSUPPORTED;
+    DeviceGuard g(h->device);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (rows == 0) return cuda_status(cudaMemsetAsync(dweight_dev, 0, (size_t)dim * size, st));
+    NormGradArgs a{};
+    a.h = sum_dev;
+    a.weight = weight_dev;
+    a.rstd = rstd_dev;
+    a.dy = dy_dev;
+    a.dsum = dsum_dev;
+    a.dx = dx_dev;
+    a.dweight = dweight_dev;
+    a.h_stride = sum_stride;
+    a.dy_stride = dy_stride;
+    a.dsum_stride = dsum_stride;
+    a.dx_stride = dx_stride;
+    a.rows = rows;
+    a.dim = dim;
+    a.dtype = dtype;
+    if (int rc = loss_scratch(h, norm_grad_workspace(a, h->env), st)) return rc;
+    return cuda_status(launch_norm_grad(a, h->env, h->d_space.p, st));
+} catch (...) {   // std::bad_alloc
+    return DOMINO_E_OOM;
+}
+
+int domino_quantize8(domino_t h, const void* x_dev, int64_t x_stride, int32_t dtype, int32_t rows, int32_t dim,
+                     int32_t block_rows, uint8_t* codes_dev, int64_t codes_stride, float* scales_dev, void* stream) {
+    DOMINO_API_RANGE();
+    if (int rc = device_handle(h)) return rc;
+    if (!is_dtype(dtype) || rows < 0 || dim < 1 || dim > kMaxDim || x_stride < dim || (block_rows != 1 && block_rows != 128) ||
+        (rows > 0 && (!x_dev || !codes_dev || !scales_dev)) || !on_values(x_dev, type_size(dtype)) ||
+        !code_rows(codes_dev, codes_stride, dim) || !on_words(scales_dev))
+        return DOMINO_E_INVALID_ARG;
+    // a CTA a tile, in one dimension of the grid
+    if (rows > kMaxRows || (int64_t)((rows + 63) / 64) * ((dim + 127) / 128) > INT32_MAX) return DOMINO_E_UNSUPPORTED;
+    if (rows == 0) return DOMINO_OK;
+    Quantize8Args a{};
+    a.x = x_dev;
+    a.stride = x_stride;
+    a.rows = rows;
+    a.dim = dim;
+    a.dtype = dtype;
+    a.block = block_rows;
+    a.codes = codes_dev;
+    a.codes_stride = codes_stride;
+    a.scales = scales_dev;
+    DeviceGuard g(h->device);
+    return cuda_status(launch_quantize8(a, h->env, (cudaStream_t)stream));
+}
+
+int domino_logits8(domino_t h, const uint8_t* hidden_dev, int64_t hidden_stride, const float* hidden_scales_dev,
+                   const uint8_t* weight_dev, int64_t weight_stride, const float* weight_scales_dev, int32_t rows,
+                   int32_t dim, int32_t n_tokens, int32_t dtype, void* logits_dev, int64_t logits_stride, void* stream) {
+    DOMINO_API_RANGE();
+    if (int rc = device_handle(h)) return rc;
+    if (!is_dtype(dtype) || rows < 0 || dim < 1 || dim > kMaxDim || n_tokens < 1 || n_tokens > kMaxTokens ||
+        !code_rows(hidden_dev, hidden_stride, dim) || !code_rows(weight_dev, weight_stride, dim) || !weight_dev ||
+        !weight_scales_dev || (rows > 0 && (!hidden_dev || !hidden_scales_dev || !logits_dev)) || logits_stride < n_tokens ||
+        !on_values(logits_dev, type_size(dtype)) || !on_words(hidden_scales_dev, weight_scales_dev))
+        return DOMINO_E_INVALID_ARG;
+    if (rows == 0) return DOMINO_OK;
+    Logits8Args a{};
+    a.hidden = hidden_dev;
+    a.hidden_stride = hidden_stride;
+    a.hidden_scales = hidden_scales_dev;
+    a.weight = weight_dev;
+    a.weight_stride = weight_stride;
+    a.weight_scales = weight_scales_dev;
+    a.rows = rows;
+    a.dim = dim;
+    a.n_tokens = n_tokens;
+    a.dtype = dtype;
+    a.logits = logits_dev;
+    a.logits_stride = rows == 1 ? ((int64_t)n_tokens + 7) / 8 * 8 : logits_stride;   // one row has no next one
+    a.err = (uint32_t*)h->d_err.p;
+    if (rows > kMaxRows || !logits8_fits(a)) return DOMINO_E_UNSUPPORTED;
+    DeviceGuard g(h->device);
+    return cuda_status(launch_logits8(a, h->env, (cudaStream_t)stream));
+}
+
+int domino_mask_logits_penalized(domino_t h, const void* logits_dev, int32_t dtype, int32_t batch,
+                                 int64_t row_stride_elems, int32_t n_tokens, const domino_penalties* penalties,
+                                 const uint32_t* mask_dev, int32_t* argmax_dev, float* lse_dev, float* logprobs_dev,
+                                 void* stream) {
+    DOMINO_API_RANGE();
+    PenalizedArgs a;
+    if (int rc = penalized_args(a, h, logits_dev, dtype, batch, row_stride_elems, n_tokens, penalties, mask_dev)) return rc;
+    if (batch == 0) return DOMINO_OK;
+    if (!argmax_dev || !on_words(argmax_dev, lse_dev, logprobs_dev)) return DOMINO_E_INVALID_ARG;
+    a.argmax = argmax_dev;
+    a.lse = lse_dev;
+    a.logprobs = logprobs_dev;
+    DeviceGuard g(h->device);
+    return cuda_status(launch_penalized(a, h->env, (cudaStream_t)stream));
+}
+
+int domino_mask_sample_penalized(domino_t h, const void* logits_dev, int32_t dtype, int32_t batch,
+                                 int64_t row_stride_elems, int32_t n_tokens, const domino_penalties* penalties,
+                                 const uint32_t* mask_dev, float temperature, uint64_t seed, uint64_t offset,
+                                 int32_t* tokens_dev, void* stream) {
+    DOMINO_API_RANGE();
+    PenalizedArgs a;
+    if (int rc = penalized_args(a, h, logits_dev, dtype, batch, row_stride_elems, n_tokens, penalties, mask_dev)) return rc;
+    if (!(temperature > 0.0f) || !std::isfinite(temperature)) return DOMINO_E_INVALID_ARG;
+    if (batch == 0) return DOMINO_OK;
+    if (!tokens_dev || !on_words(tokens_dev)) return DOMINO_E_INVALID_ARG;
+    const SampleArgs sample{(uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)offset, (uint32_t)(offset >> 32),
+                            1.0f / temperature};   // one correctly rounded fp32 division
+    a.argmax = tokens_dev;
+    a.sample = &sample;
+    DeviceGuard g(h->device);
+    return cuda_status(launch_penalized(a, h->env, (cudaStream_t)stream));
 }
 
 int domino_get_device_error(domino_t h, int32_t* code, void* stream) {

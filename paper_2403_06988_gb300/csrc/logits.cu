@@ -156,19 +156,6 @@ __global__ void __launch_bounds__(kDecodeThreads, 2)
                          __ldg(a.lse + r), a.logprobs + (size_t)r * a.V, threadIdx.x);
 }
 
-// Gumbel variate of token t of row r: g_t = -ln(-ln(u_t)), u_t = (2k + 1) / 2^24,
-// k = (word t % 4 of Philox on (t / 4, r, offset)) >> 9.  `blk` / `rnd` cache
-// the last Philox block.
-__device__ __forceinline__ float gumbel(const SampleArgs& a, int r, int t, int& blk, uint4& rnd) {
-    if ((t >> 2) != blk) {
-        blk = t >> 2;
-        rnd = philox10(make_uint4((uint32_t)blk, (uint32_t)r, a.off0, a.off1), a.key0, a.key1);
-    }
-    const uint32_t w = (t & 2) ? ((t & 1) ? rnd.w : rnd.z) : ((t & 1) ? rnd.y : rnd.x);
-    const float u = __fmul_rn(__uint2float_rn(2u * (w >> 9) + 1u), 0x1p-24f);
-    return -ln_rn(-ln_rn(u));
-}
-
 // ---- the greedy / log-sum-exp pass over bf16 rows: a compacted gather -----
 // One CTA per row, its warps (up to 16) on consecutive segments of the row's
 // mask words, each segment cut into spans of 32 x kGatherSpan words (lane l

@@ -29,6 +29,7 @@
 #include "decode.cuh"
 #include "loss.h"
 #include "tcgen05.cuh"
+#include "tensor_map.h"
 
 namespace domino {
 namespace {
@@ -191,17 +192,7 @@ __device__ __forceinline__ Side<T::kColumns> load_side(const Product& p, int32_t
     return s;
 }
 
-// 16 words (64 bytes) of each lane's row to a buffer.
-__device__ __forceinline__ void put_words(uint32_t buffer, int lane, const uint32_t* w) {
-    const uint32_t row = buffer + lane * 64;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(row + ((i ^ ((lane >> 1) & 3)) << 4)), "r"(w[4 * i]),
-                     "r"(w[4 * i + 1]), "r"(w[4 * i + 2]), "r"(w[4 * i + 3])
-                     : "memory");
-}
-
-// They, to one of the warp's buffers, and from there to (x, y).
+// 16 words (64 bytes) of each lane's row to one of the warp's buffers, and from there to (x, y).
 // A buffer was read by its copy before it is written again.
 __device__ __forceinline__ void put_rows(const CUtensorMap* map, int32_t x, int32_t y, bool add, uint32_t buffer, int lane,
                                          const uint32_t* w) {
@@ -726,37 +717,6 @@ __global__ void __launch_bounds__(kPackThreads)
 }
 
 // ---- host --------------------------------------------------------------------
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiled encode_tiled() {
-    static const EncodeTiled f = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess) {
-            cudaGetLastError();
-            p = nullptr;
-        }
-        return reinterpret_cast<EncodeTiled>(p);
-    }();
-    return f;
-}
-
-// A [rows][cols] matrix, rows `pitch` elements apart: bf16, read in boxes of 64
-// columns (128 bytes, swizzled) and `box_rows` rows, zeros outside; or written
-// in boxes of 32 rows of 64 bytes.
-cudaError_t encode_map(CUtensorMap* map, CUtensorMapDataType type, int size, const void* base, int64_t rows, int64_t cols,
-                       int64_t pitch, int box_cols, int box_rows, CUtensorMapSwizzle swizzle) {
-    const EncodeTiled encode = encode_tiled();
-    if (!encode) return cudaErrorNotSupported;
-    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch * size};
-    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, steps[2] = {1, 1};
-    const CUresult r = encode(map, type, 2, const_cast<void*>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
-}
 cudaError_t make_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t pitch, int box_rows) {
     return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, rows, cols, pitch, 64, box_rows,
                       CU_TENSOR_MAP_SWIZZLE_128B);

@@ -1,0 +1,412 @@
+// norm.cu -- the root-mean-square norm of a stream with the residual's addition, its
+// output in the stream's type or in e4m3 codes with a scale for each 128 values, and
+// its gradient (sm_103a).
+//
+//   h    = x + residual, rounded to the stream's type
+//   rstd = (mean(h^2) + eps)^(-1/2)
+//   y    = h rstd w
+//   with g = w dy, c = rstd^2 mean(g h):
+//   dx   = rstd (g - c h) + dsum              (of x and of the residual alike)
+//   dw   = sum over the rows of dy h rstd
+//
+// All of it is bound by HBM: a row is read once, kept in registers between its sum of
+// squares and its use, and written once.  Sums are fp32; y, the codes, dx and dw are
+// rounded once each.
+#include <algorithm>
+
+#include "norm.h"
+#include "values8.cuh"
+
+namespace domino {
+namespace {
+
+constexpr int kRowThreads8 = 512;         // of a row, at most
+constexpr int kCtaThreads = 128;          // of a CTA, at least: short rows share one
+constexpr int kMaxVectors = 4;            // of a thread, in registers
+constexpr int32_t kLongRow = kRowThreads8 * kMaxVectors * kN;   // longer rows are read twice
+constexpr int64_t kFarOut = (int64_t)64 << 20;                  // outputs of half of the L2 or more are written past it
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+    return v;
+}
+
+// The sum over a row's threads (blockDim.x, a multiple of 32), the same in each; every thread of the CTA calls it.
+// `part` is used again only after another barrier.
+__device__ __forceinline__ float row_sum(float v, float (*part)[kRowThreads8 / 32]) {
+    v = warp_sum(v);
+    const int warps = blockDim.x >> 5;
+    if (warps == 1) return v;
+    if ((threadIdx.x & 31) == 0) part[threadIdx.y][threadIdx.x >> 5] = v;
+    __syncthreads();
+    float s = 0.0f;
+    for (int w = 0; w < warps; ++w) s += part[threadIdx.y][w];
+    return s;
+}
+
+template <bool BF16>
+__device__ __forceinline__ char* at_row(const void* p, int64_t row, int64_t stride) {
+    return (char*)p + row * stride * (BF16 ? 2 : 4);
+}
+
+// Eight values of h: x, or the rounded sum.
+template <bool BF16, bool ALIGNED>
+__device__ __forceinline__ void load_sum(const char* x, const char* r, int32_t c, int32_t dim, float (&h)[kN]) {
+    load8<BF16, ALIGNED>(x, c, dim, h);
+    if (r) {
+        float f[kN];
+        load8<BF16, ALIGNED>(r, c, dim, f);
+#pragma unroll
+        for (int e = 0; e < kN; ++e) {
+            h[e] += f[e];
+            if constexpr (BF16) h[e] = __bfloat162float(__float2bfloat16_rn(h[e]));
+        }
+    }
+}
+
+// Eight values of y out: h rstd w, as values or as codes.
+template <bool BF16, bool ALIGNED, bool CODES>
+__device__ __forceinline__ void put_norm(const NormArgs& a, int32_t row, int32_t c, const float (&h)[kN], float rstd, bool far,
+                                         int lane) {
+    float y[kN];
+    load8<BF16, ALIGNED>(a.weight, c, a.dim, y);
+#pragma unroll
+    for (int e = 0; e < kN; ++e) y[e] = h[e] * rstd * y[e];
+    if constexpr (CODES) {
+        const float top = fmaxf(block_largest(largest(y)), kLeast8);
+        if ((lane & (kBlockLanes - 1)) == 0 && c < a.dim)
+            a.scales[(int64_t)row * ((a.dim + kBlock8 - 1) / kBlock8) + c / kBlock8] = top / kMost8;
+        store_codes(a.codes + (int64_t)row * a.codes_stride, c, a.dim, y, kMost8 / top, far);
+    } else {
+        store8<BF16, ALIGNED>(at_row<BF16>(a.y, row, a.y_stride), c, a.dim, y, far, lane);
+    }
+}
+
+// blockDim.y rows a CTA, of blockDim.x threads with VECTORS times eight values each.
+template <bool BF16, bool ALIGNED, bool CODES, int VECTORS>
+__global__ void __launch_bounds__(kRowThreads8) norm_kernel(const __grid_constant__ NormArgs a, const bool far) {
+    __shared__ float s_part[kCtaThreads / 32][kRowThreads8 / 32];
+    const int lane = threadIdx.x & 31;
+    const int32_t row = blockIdx.x * blockDim.y + threadIdx.y;
+    const bool on = row < a.rows;
+    pdl_wait();
+    pdl_trigger();
+    float h[VECTORS][kN], s = 0.0f;
+    const char* x = at_row<BF16>(a.x, row, a.x_stride);
+    const char* r = a.residual ? at_row<BF16>(a.residual, row, a.residual_stride) : nullptr;
+#pragma unroll
+    for (int j = 0; j < VECTORS; ++j)
+        load_sum<BF16, ALIGNED>(x, r, (threadIdx.x + j * blockDim.x) * kN, on ? a.dim : 0, h[j]);
+#pragma unroll
+    for (int j = 0; j < VECTORS; ++j)
+#pragma unroll
+        for (int e = 0; e < kN; ++e) s += h[j][e] * h[j][e];
+    const float rstd = __frsqrt_rn(row_sum(s, s_part) / (float)a.dim + a.eps);
+    if (!on) return;   // whole warps
+    if (!CODES && a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+#pragma unroll
+    for (int j = 0; j < VECTORS; ++j) {
+        const int32_t c = (threadIdx.x + j * blockDim.x) * kN;
+        if (a.sum) store8<BF16, ALIGNED>(at_row<BF16>(a.sum, row, a.sum_stride), c, a.dim, h[j], far, lane);
+        put_norm<BF16, ALIGNED, CODES>(a, row, c, h[j], rstd, far, lane);
+    }
+}
+
+// Rows of more than kLongRow values: a CTA each, the sum read again.
+template <bool BF16, bool ALIGNED, bool CODES>
+__global__ void __launch_bounds__(kRowThreads8) norm_long_kernel(const __grid_constant__ NormArgs a, const bool far) {
+    __shared__ float s_part[1][kRowThreads8 / 32];
+    const int lane = threadIdx.x & 31;
+    const int32_t row = blockIdx.x, steps = (a.dim + kRowThreads8 * kN - 1) / (kRowThreads8 * kN);
+    pdl_wait();
+    pdl_trigger();
+    const char* x = at_row<BF16>(a.x, row, a.x_stride);
+    const char* r = a.residual ? at_row<BF16>(a.residual, row, a.residual_stride) : nullptr;
+    char* sum = a.sum ? at_row<BF16>(a.sum, row, a.sum_stride) : nullptr;
+    float s = 0.0f;
+    for (int32_t j = 0; j < steps; ++j) {
+        const int32_t c = (threadIdx.x + j * kRowThreads8) * kN;
+        float h[kN];
+        load_sum<BF16, ALIGNED>(x, r, c, a.dim, h);
+        if (sum) store8<BF16, ALIGNED>(sum, c, a.dim, h, false, lane);
+#pragma unroll
+        for (int e = 0; e < kN; ++e) s += h[e] * h[e];
+    }
+    const float rstd = __frsqrt_rn(row_sum(s, s_part) / (float)a.dim + a.eps);   // its barrier: the sum is written
+    if (!CODES && a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+    for (int32_t j = 0; j < steps; ++j) {
+        const int32_t c = (threadIdx.x + j * kRowThreads8) * kN;
+        float h[kN];
+        load8<BF16, ALIGNED>(sum ? sum : x, c, a.dim, h);
+        put_norm<BF16, ALIGNED, CODES>(a, row, c, h, rstd, far, lane);
+    }
+}
+
+// ---- gradient ------------------------------------------------------------------
+constexpr int kGradThreads = 256;         // of a row, at most
+constexpr int kGradVectors = 4;
+constexpr int32_t kGradLongRow = kGradThreads * kGradVectors * kN;
+
+// A CTA's rows (blockDim.y strips of them, threads as in norm_kernel) one after the other; the strip's part of dw stays
+// in registers and goes to parts[strip][pitch].
+template <bool BF16, bool ALIGNED, int VECTORS>
+__global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const __grid_constant__ NormGradArgs a, float* parts,
+                                                                 const int32_t strips, const int32_t pitch, const bool far) {
+    __shared__ float s_part[2][kCtaThreads / 32][kRowThreads8 / 32];
+    const int lane = threadIdx.x & 31;
+    const int32_t strip = blockIdx.x * blockDim.y + threadIdx.y;
+    pdl_wait();
+    pdl_trigger();
+    const int32_t row0 = strip < strips ? (int32_t)((int64_t)a.rows * strip / strips) : 0;
+    const int32_t row1 = strip < strips ? (int32_t)((int64_t)a.rows * (strip + 1) / strips) : 0;
+    const int32_t most = (a.rows + strips - 1) / strips;   // the CTA's strips differ by a row: all take part in the barriers
+    float w[VECTORS][kN], dw[VECTORS][kN];
+#pragma unroll
+    for (int j = 0; j < VECTORS; ++j) {
+        load8<BF16, ALIGNED>(a.weight, (threadIdx.x + j * blockDim.x) * kN, a.dim, w[j]);
+#pragma unroll
+        for (int e = 0; e < kN; ++e) dw[j][e] = 0.0f;
+    }
+    for (int32_t i = 0; i < most; ++i) {
+        const int32_t row = row0 + i;
+        const bool on = row < row1;
+        const int32_t dim = on ? a.dim : 0;
+        const char* ph = at_row<BF16>(a.h, row, a.h_stride);
+        const char* pd = at_row<BF16>(a.dy, row, a.dy_stride);
+        float h[VECTORS][kN], g[VECTORS][kN], ds[VECTORS][kN], s = 0.0f;
+        const float rstd = on ? a.rstd[row] : 0.0f;
+#pragma unroll
+        for (int j = 0; j < VECTORS; ++j) {
+            const int32_t c = (threadIdx.x + j * blockDim.x) * kN;
+            load8<BF16, ALIGNED>(ph, c, dim, h[j]);
+            load8<BF16, ALIGNED>(pd, c, dim, g[j]);
+            if (a.dsum) load8<BF16, ALIGNED>(at_row<BF16>(a.dsum, row, a.dsum_stride), c, dim, ds[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < VECTORS; ++j)
+#pragma unroll
+            for (int e = 0; e < kN; ++e) {
+                dw[j][e] += g[j][e] * (h[j][e] * rstd);
+                g[j][e] *= w[j][e];
+                s += g[j][e] * h[j][e];
+            }
+        const float c1 = row_sum(s, s_part[i & 1]) / (float)a.dim * rstd * rstd;
+        if (!on) continue;
+#pragma unroll
+        for (int j = 0; j < VECTORS; ++j) {
+#pragma unroll
+            for (int e = 0; e < kN; ++e) {
+                g[j][e] = rstd * (g[j][e] - h[j][e] * c1);
+                if (a.dsum) g[j][e] += ds[j][e];
+            }
+            store8<BF16, ALIGNED>(at_row<BF16>(a.dx, row, a.dx_stride), (threadIdx.x + j * blockDim.x) * kN, a.dim, g[j], far, lane);
+        }
+    }
+    if (strip >= strips) return;
+#pragma unroll
+    for (int j = 0; j < VECTORS; ++j) {
+        const int32_t c = (threadIdx.x + j * blockDim.x) * kN;
+        if (c >= pitch) continue;
+        float4* to = reinterpret_cast<float4*>(parts + (int64_t)strip * pitch + c);
+        to[0] = make_float4(dw[j][0], dw[j][1], dw[j][2], dw[j][3]);
+        to[1] = make_float4(dw[j][4], dw[j][5], dw[j][6], dw[j][7]);
+    }
+}
+
+// Rows of more than kGradLongRow values: the rows' sums first, then columns by strips of rows, a thread eight columns.
+template <bool BF16, bool ALIGNED>
+__global__ void __launch_bounds__(kRowThreads8) norm_grad_sums_kernel(const __grid_constant__ NormGradArgs a, float* sums) {
+    __shared__ float s_part[1][kRowThreads8 / 32];
+    pdl_wait();
+    pdl_trigger();
+    const int32_t row = blockIdx.x;
+    float s = 0.0f;
+    for (int32_t c = threadIdx.x * kN; c < a.dim; c += kRowThreads8 * kN) {
+        float h[kN], g[kN], w[kN];
+        load8<BF16, ALIGNED>(at_row<BF16>(a.h, row, a.h_stride), c, a.dim, h);
+        load8<BF16, ALIGNED>(at_row<BF16>(a.dy, row, a.dy_stride), c, a.dim, g);
+        load8<BF16, ALIGNED>(a.weight, c, a.dim, w);
+#pragma unroll
+        for (int e = 0; e < kN; ++e) s += w[e] * g[e] * h[e];
+    }
+    s = row_sum(s, s_part);
+    const float rstd = a.rstd[row];
+    if (threadIdx.x == 0) sums[row] = s / (float)a.dim * rstd * rstd;
+}
+template <bool BF16, bool ALIGNED>
+__global__ void __launch_bounds__(kGradThreads) norm_grad_long_kernel(const __grid_constant__ NormGradArgs a, const float* sums,
+                                                                      float* parts, const int32_t strips, const int32_t pitch,
+                                                                      const bool far) {
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x & 31;
+    const int32_t c = (blockIdx.x * kGradThreads + threadIdx.x) * kN, strip = blockIdx.y;
+    const int32_t row0 = (int32_t)((int64_t)a.rows * strip / strips), row1 = (int32_t)((int64_t)a.rows * (strip + 1) / strips);
+    float w[kN], dw[kN];
+    load8<BF16, ALIGNED>(a.weight, c, a.dim, w);
+#pragma unroll
+    for (int e = 0; e < kN; ++e) dw[e] = 0.0f;
+    for (int32_t row = row0; row < row1; ++row) {
+        float h[kN], g[kN], ds[kN];
+        const float rstd = a.rstd[row], c1 = sums[row];
+        load8<BF16, ALIGNED>(at_row<BF16>(a.h, row, a.h_stride), c, a.dim, h);
+        load8<BF16, ALIGNED>(at_row<BF16>(a.dy, row, a.dy_stride), c, a.dim, g);
+        if (a.dsum) load8<BF16, ALIGNED>(at_row<BF16>(a.dsum, row, a.dsum_stride), c, a.dim, ds);
+#pragma unroll
+        for (int e = 0; e < kN; ++e) {
+            dw[e] += g[e] * (h[e] * rstd);
+            g[e] = rstd * (w[e] * g[e] - h[e] * c1);
+            if (a.dsum) g[e] += ds[e];
+        }
+        store8<BF16, ALIGNED>(at_row<BF16>(a.dx, row, a.dx_stride), c, a.dim, g, far, lane);
+    }
+    if (c >= pitch) return;
+    float4* to = reinterpret_cast<float4*>(parts + (int64_t)strip * pitch + c);
+    to[0] = make_float4(dw[0], dw[1], dw[2], dw[3]);
+    to[1] = make_float4(dw[4], dw[5], dw[6], dw[7]);
+}
+
+// dw: the strips' parts, added in an order that their number fixes.  kJoinColumns columns a CTA, so that a few thousand
+// columns give every SM some of a sum of up to kMaxStrips parts.
+constexpr int kJoinThreads = 512, kJoinColumns = 32, kJoinLanes = kJoinColumns / 4, kJoinGroups = kJoinThreads / kJoinLanes;
+template <bool BF16>
+__global__ void __launch_bounds__(kJoinThreads) norm_join_kernel(const float* parts, const int32_t strips, const int32_t pitch,
+                                                                 const int32_t dim, void* dweight) {
+    __shared__ float4 s_sum[kJoinGroups][kJoinLanes];
+    pdl_wait();
+    pdl_trigger();
+    const int at = threadIdx.x % kJoinLanes, group = threadIdx.x / kJoinLanes;
+    const int32_t c = blockIdx.x * kJoinColumns + at * 4;
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (c < pitch) {
+#pragma unroll 4
+        for (int32_t k = group; k < strips; k += kJoinGroups) {
+            const float4 x = *reinterpret_cast<const float4*>(parts + (int64_t)k * pitch + c);
+            v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+        }
+    }
+    s_sum[group][at] = v;
+#pragma unroll
+    for (int n = kJoinGroups / 2; n > 0; n >>= 1) {
+        __syncthreads();
+        if (group < n) {
+            const float4 x = s_sum[group + n][at];
+            v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+            s_sum[group][at] = v;
+        }
+    }
+    if (group) return;
+    const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (c + e >= dim) break;
+        if constexpr (BF16) static_cast<__nv_bfloat16*>(dweight)[c + e] = __float2bfloat16_rn(f[e]);
+        else static_cast<float*>(dweight)[c + e] = f[e];
+    }
+}
+
+// ---- host ----------------------------------------------------------------------
+int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+bool on16(const void* p, int64_t stride, int dtype) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * (dtype == DOMINO_DTYPE_BF16 ? 2 : 4) % 16 == 0;
+}
+
+// Threads of a row and what each holds.  One vector a thread where the row's 512 can hold it: 32 rows of 4096, a latency.
+struct Cut {
+    int threads, vectors, rows;   // rows of a CTA
+};
+Cut cut_row(int32_t dim, int most_threads) {
+    const int vectors = ceil_div(dim, kN);
+    Cut c{0, 1, 1};
+    while (vectors > most_threads * c.vectors && c.vectors < kMaxVectors) c.vectors *= 2;
+    c.threads = std::min(most_threads, ceil_div(ceil_div(vectors, c.vectors), 32) * 32);
+    c.rows = std::max(1, kCtaThreads / c.threads);
+    return c;
+}
+
+template <bool BF16, bool ALIGNED, bool CODES>
+cudaError_t launch_norm_t(const NormArgs& a, cudaStream_t st) {
+    const bool far = (int64_t)a.rows * a.dim * (CODES ? 1 : BF16 ? 2 : 4) >= kFarOut;
+    if (a.dim > kLongRow)
+        return launch_pdl(norm_long_kernel<BF16, ALIGNED, CODES>, dim3((unsigned)a.rows), dim3(kRowThreads8), 0, st, a, far);
+    const Cut c = cut_row(a.dim, kRowThreads8);
+    const dim3 grid((unsigned)ceil_div(a.rows, c.rows)), block((unsigned)c.threads, (unsigned)c.rows);
+    switch (c.vectors) {
+        case 1: return launch_pdl(norm_kernel<BF16, ALIGNED, CODES, 1>, grid, block, 0, st, a, far);
+        case 2: return launch_pdl(norm_kernel<BF16, ALIGNED, CODES, 2>, grid, block, 0, st, a, far);
+        default: return launch_pdl(norm_kernel<BF16, ALIGNED, CODES, 4>, grid, block, 0, st, a, far);
+    }
+}
+template <bool BF16, bool ALIGNED>
+cudaError_t launch_norm_c(const NormArgs& a, cudaStream_t st) {
+    return a.codes ? launch_norm_t<BF16, ALIGNED, true>(a, st) : launch_norm_t<BF16, ALIGNED, false>(a, st);
+}
+
+// Strips of rows of the gradient: as many as the SMs hold at once, and a part of dw for each.
+constexpr int kStripsPerSm = 4, kShortStripsPerSm = 16;
+struct GradCut {
+    Cut cut;
+    int32_t strips, pitch;
+    size_t sums;          // bytes of the rows' sums (long rows)
+};
+GradCut cut_grad(const NormGradArgs& a, const LaunchEnv& env) {
+    GradCut g{cut_row(a.dim, kGradThreads), 0, ceil_div(a.dim, kN) * kN, 0};
+    const bool lng = a.dim > kGradLongRow;
+    if (lng) g.sums = ((size_t)a.rows * 4 + 255) / 256 * 256;
+    const int64_t per_sm = lng ? ceil_div(kStripsPerSm * 8, ceil_div(a.dim, kGradThreads * kN)) : g.cut.rows > 1 ? kShortStripsPerSm : kStripsPerSm;
+    g.strips = (int32_t)std::max<int64_t>(1, std::min<int64_t>(a.rows, lng ? per_sm * env.num_sms / 8 : per_sm * env.num_sms));
+    return g;
+}
+
+template <bool BF16, bool ALIGNED>
+cudaError_t launch_grad_t(const NormGradArgs& a, const LaunchEnv& env, void* space, cudaStream_t st) {
+    const GradCut g = cut_grad(a, env);
+    const bool far = (int64_t)a.rows * a.dim * (BF16 ? 2 : 4) >= kFarOut;
+    float* parts = (float*)((char*)space + g.sums);
+    cudaError_t e;
+    if (a.dim > kGradLongRow) {
+        float* sums = (float*)space;
+        e = launch_pdl(norm_grad_sums_kernel<BF16, ALIGNED>, dim3((unsigned)a.rows), dim3(kRowThreads8), 0, st, a, sums);
+        if (e != cudaSuccess) return e;
+        e = launch_pdl(norm_grad_long_kernel<BF16, ALIGNED>, dim3((unsigned)ceil_div(a.dim, kGradThreads * kN), (unsigned)g.strips),
+                       dim3(kGradThreads), 0, st, a, (const float*)sums, parts, g.strips, g.pitch, far);
+    } else {
+        const dim3 grid((unsigned)ceil_div(g.strips, g.cut.rows)), block((unsigned)g.cut.threads, (unsigned)g.cut.rows);
+        switch (g.cut.vectors) {
+            case 1: e = launch_pdl(norm_grad_kernel<BF16, ALIGNED, 1>, grid, block, 0, st, a, parts, g.strips, g.pitch, far); break;
+            case 2: e = launch_pdl(norm_grad_kernel<BF16, ALIGNED, 2>, grid, block, 0, st, a, parts, g.strips, g.pitch, far); break;
+            default: e = launch_pdl(norm_grad_kernel<BF16, ALIGNED, 4>, grid, block, 0, st, a, parts, g.strips, g.pitch, far);
+        }
+    }
+    if (e != cudaSuccess) return e;
+    return launch_pdl(norm_join_kernel<BF16>, dim3((unsigned)ceil_div(a.dim, kJoinColumns)), dim3(kJoinThreads), 0, st,
+                      (const float*)parts, g.strips, g.pitch, a.dim, a.dweight);
+}
+
+}  // namespace
+
+cudaError_t launch_norm(const NormArgs& a, const LaunchEnv&, cudaStream_t st) {
+    bool aligned = on16(a.x, a.x_stride, a.dtype) && on16(a.weight, 0, a.dtype);
+    if (a.residual) aligned = aligned && on16(a.residual, a.residual_stride, a.dtype);
+    if (a.sum) aligned = aligned && on16(a.sum, a.sum_stride, a.dtype);
+    if (!a.codes) aligned = aligned && on16(a.y, a.y_stride, a.dtype);
+    if (a.dtype == DOMINO_DTYPE_BF16) return aligned ? launch_norm_c<true, true>(a, st) : launch_norm_c<true, false>(a, st);
+    return aligned ? launch_norm_c<false, true>(a, st) : launch_norm_c<false, false>(a, st);
+}
+
+size_t norm_grad_workspace(const NormGradArgs& a, const LaunchEnv& env) {
+    const GradCut g = cut_grad(a, env);
+    return g.sums + (size_t)g.strips * g.pitch * 4;
+}
+
+cudaError_t launch_norm_grad(const NormGradArgs& a, const LaunchEnv& env, void* space, cudaStream_t st) {
+    bool aligned = on16(a.h, a.h_stride, a.dtype) && on16(a.dy, a.dy_stride, a.dtype) && on16(a.dx, a.dx_stride, a.dtype) &&
+                   on16(a.weight, 0, a.dtype);
+    if (a.dsum) aligned = aligned && on16(a.dsum, a.dsum_stride, a.dtype);
+    if (a.dtype == DOMINO_DTYPE_BF16) return aligned ? launch_grad_t<true, true>(a, env, space, st) : launch_grad_t<true, false>(a, env, space, st);
+    return aligned ? launch_grad_t<false, true>(a, env, space, st) : launch_grad_t<false, false>(a, env, space, st);
+}
+
+}  // namespace domino

@@ -1,6 +1,6 @@
-// tcgen05.cuh -- device helpers of the tensor-core products (loss.cu): memory
+// tcgen05.cuh -- device helpers of the tensor-core products (loss.cu, logits8.cu): memory
 // barriers with bounded waits, TMA loads of operand tiles, the shared-memory
-// and instruction descriptors of tcgen05.mma on bf16 operands, and loads of
+// and instruction descriptors of tcgen05.mma on bf16 and e4m3 operands, and loads of
 // the accumulators from tensor memory.
 #pragma once
 #include <cuda.h>
@@ -138,6 +138,16 @@ __device__ __forceinline__ void tma_wait_all() { asm volatile("cp.async.bulk.wai
 // What this thread wrote to shared memory is seen by the copies issued after a barrier with it.
 __device__ __forceinline__ void tma_fence() { asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory"); }
 
+// 16 words (64 bytes) of each lane's row to a buffer of 32 rows in the 64-byte swizzle.
+__device__ __forceinline__ void put_words(uint32_t buffer, int lane, const uint32_t* w) {
+    const uint32_t row = buffer + lane * 64;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(row + ((i ^ ((lane >> 1) & 3)) << 4)), "r"(w[4 * i]),
+                     "r"(w[4 * i + 1]), "r"(w[4 * i + 2]), "r"(w[4 * i + 3])
+                     : "memory");
+}
+
 // Shared-memory descriptor of an operand tile in the 128-byte swizzle: start
 // address, leading and stride byte offsets (16-byte units), descriptor version
 // 1 (bits 46, 47), swizzle mode 2 (bits 61 to 63).
@@ -172,6 +182,27 @@ __device__ __forceinline__ void mma_bf16(uint32_t acc, uint64_t a, uint64_t b, u
             "{\n.reg .pred p;\n"
             "setp.ne.b32 p, %4, 0;\n"
             "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(acc),
+            "l"(a), "l"(b), "r"(desc), "r"(add ? 1u : 0u)
+            : "memory");
+}
+// The same of e4m3 operands, 32 k (32 bytes of a row) a product: both type fields are 0.
+__host__ __device__ constexpr uint32_t mma_desc8(int m, int n) {
+    return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+template <bool PAIR>
+__device__ __forceinline__ void mma_e4m3(uint32_t acc, uint64_t a, uint64_t b, uint32_t desc, bool add) {
+    if constexpr (PAIR)
+        asm volatile(
+            "{\n.reg .pred p;\n"
+            "setp.ne.b32 p, %4, 0;\n"
+            "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(acc),
+            "l"(a), "l"(b), "r"(desc), "r"(add ? 1u : 0u)
+            : "memory");
+    else
+        asm volatile(
+            "{\n.reg .pred p;\n"
+            "setp.ne.b32 p, %4, 0;\n"
+            "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(acc),
             "l"(a), "l"(b), "r"(desc), "r"(add ? 1u : 0u)
             : "memory");
 }
@@ -226,8 +257,8 @@ __device__ __forceinline__ void tmem_load32(float (&v)[32], uint32_t addr) {
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
-// The same of 16 columns, added to v.
-__device__ __forceinline__ void tmem_add16(float* v, uint32_t addr) {
+// The same of 16 columns.
+__device__ __forceinline__ void tmem_load16(float (&v)[16], uint32_t addr) {
     uint32_t r[16];
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
@@ -238,7 +269,14 @@ __device__ __forceinline__ void tmem_add16(float* v, uint32_t addr) {
         : "r"(addr)
         : "memory");
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] += __uint_as_float(r[i]);
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+// They, added to v.
+__device__ __forceinline__ void tmem_add16(float* v, uint32_t addr) {
+    float r[16];
+    tmem_load16(r, addr);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] += r[i];
 }
 
 }  // namespace

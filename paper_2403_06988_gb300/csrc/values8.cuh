@@ -1,0 +1,127 @@
+// values8.cuh -- eight values of a row a lane, bf16 or fp32 at any alignment, and
+// e4m3 codes with a scale for each 128 values.
+//
+//   a = max |v| over the block, at least 2^-100;  scale = a / 448;  code = e4m3(v (448 / a))
+//
+// 448 is the largest e4m3 value: the block's largest value takes it, and nothing
+// overflows.  Sixteen lanes of eight values make a block of a row.
+#pragma once
+#include "bf16_rows.cuh"
+#include "walk_common.cuh"
+
+namespace domino {
+namespace {
+
+constexpr int kBlock8 = 128;              // values that share a scale, along a row
+constexpr int kBlockLanes = kBlock8 / kN;
+constexpr float kMost8 = 448.0f, kLeast8 = 0x1p-100f;
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// Values c, .. c + 7 of a row of dim; zeros beyond its end.  ALIGNED: the row begins on a 16-byte boundary.  With
+// neither __ldg nor another assumption that the row is not written by this kernel: outputs may take inputs' places.
+template <bool BF16, bool ALIGNED>
+__device__ __forceinline__ void load8(const void* row, int32_t c, int32_t dim, float (&f)[kN]) {
+    const int32_t left = dim - c;
+    if constexpr (BF16) {
+        const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(row) + c;
+        if (ALIGNED && left >= kN) {
+            const uint4 u = *reinterpret_cast<const uint4*>(p);
+            f[0] = bf16_lo(u.x), f[1] = bf16_hi(u.x), f[2] = bf16_lo(u.y), f[3] = bf16_hi(u.y);
+            f[4] = bf16_lo(u.z), f[5] = bf16_hi(u.z), f[6] = bf16_lo(u.w), f[7] = bf16_hi(u.w);
+            return;
+        }
+        Eight e;
+        e.zero();
+        if (left > 0) e.load(p, left);
+        e.get(f);
+    } else {
+        const float* p = static_cast<const float*>(row) + c;
+        if (ALIGNED && left >= kN) {
+            const float4 u = reinterpret_cast<const float4*>(p)[0], v = reinterpret_cast<const float4*>(p)[1];
+            f[0] = u.x, f[1] = u.y, f[2] = u.z, f[3] = u.w, f[4] = v.x, f[5] = v.y, f[6] = v.z, f[7] = v.w;
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < kN; ++e) f[e] = e < left ? p[e] : 0.0f;
+    }
+}
+
+// The same values to a row.  The whole warp calls it, its lanes with consecutive c's.  far: past the L2.
+template <bool BF16, bool ALIGNED>
+__device__ __forceinline__ void store8(void* row, int32_t c, int32_t dim, const float (&f)[kN], bool far, int lane) {
+    const int32_t left = dim - c;
+    if constexpr (BF16) {
+        const uint32_t w[4] = {pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7])};
+        __nv_bfloat16* p = static_cast<__nv_bfloat16*>(row) + c;
+        if constexpr (ALIGNED) {
+            if (left >= kN) {
+                if (far) __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
+                else *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < kN; ++e)
+                    if (e < left) reinterpret_cast<unsigned short*>(p)[e] = (unsigned short)(w[e / 2] >> (16 * (e & 1)));
+            }
+        } else {
+            store_any(p, w, left, lane);
+        }
+    } else {
+        float* p = static_cast<float*>(row) + c;
+        if (ALIGNED && left >= kN) {
+            const float4 u = make_float4(f[0], f[1], f[2], f[3]), v = make_float4(f[4], f[5], f[6], f[7]);
+            if (far) {
+                __stcs(reinterpret_cast<float4*>(p), u);
+                __stcs(reinterpret_cast<float4*>(p) + 1, v);
+            } else {
+                reinterpret_cast<float4*>(p)[0] = u;
+                reinterpret_cast<float4*>(p)[1] = v;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < kN; ++e)
+                if (e < left) p[e] = f[e];
+        }
+    }
+}
+
+__device__ __forceinline__ float largest(const float (&f)[kN]) {
+    float a = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kN; ++e) a = fmaxf(a, fabsf(f[e]));
+    return a;
+}
+// The largest of a block's lanes.
+__device__ __forceinline__ float block_largest(float a) {
+#pragma unroll
+    for (int off = kBlockLanes / 2; off > 0; off >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, off));
+    return a;
+}
+
+__device__ __forceinline__ uint32_t two_codes(float lo, float hi) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// Eight codes at column c of a row of codes that begins on a 16-byte boundary, by = 448 / the block's largest; nothing at
+// or beyond dim is written.
+__device__ __forceinline__ void store_codes(uint8_t* row, int32_t c, int32_t dim, const float (&f)[kN], float by, bool far) {
+    const uint32_t lo = two_codes(f[0] * by, f[1] * by) | (two_codes(f[2] * by, f[3] * by) << 16);
+    const uint32_t hi = two_codes(f[4] * by, f[5] * by) | (two_codes(f[6] * by, f[7] * by) << 16);
+    uint8_t* p = row + c;
+    if (c + kN <= dim) {
+        if (far) __stcs(reinterpret_cast<uint2*>(p), make_uint2(lo, hi));
+        else *reinterpret_cast<uint2*>(p) = make_uint2(lo, hi);
+    } else {
+#pragma unroll
+        for (int e = 0; e < kN; ++e)
+            if (c + e < dim) p[e] = (uint8_t)((e < 4 ? lo : hi) >> (8 * (e & 3)));
+    }
+}
+
+}  // namespace
+}  // namespace domino
