@@ -11,7 +11,8 @@
 //
 // All of it is bound by HBM: a row is read once, kept in registers between its sum of
 // squares and its use, and written once.  Sums are fp32; y, the codes, dx and dw are
-// rounded once each.
+// rounded once each.  Products and sums are fused where the code says so and nowhere
+// else: rows at any alignment give the same bits.
 #include <algorithm>
 
 #include "norm.h"
@@ -52,27 +53,33 @@ __device__ __forceinline__ char* at_row(const void* p, int64_t row, int64_t stri
 
 // Eight values of h: x, or the rounded sum.
 template <bool BF16, bool ALIGNED>
-__device__ __forceinline__ void load_sum(const char* x, const char* r, int32_t c, int32_t dim, float (&h)[kN]) {
-    load8<BF16, ALIGNED>(x, c, dim, h);
-    if (r) {
+struct SumVec {
+    Vec8<BF16, ALIGNED> x, r;
+    __device__ __forceinline__ void load(const char* px, const char* pr, int32_t c, int32_t dim) {
+        x.load(px, c, dim);
+        if (pr) r.load(pr, c, dim);
+    }
+    __device__ __forceinline__ void get(float (&h)[kN], bool residual) const {
+        x.get(h);
+        if (!residual) return;
         float f[kN];
-        load8<BF16, ALIGNED>(r, c, dim, f);
+        r.get(f);
 #pragma unroll
         for (int e = 0; e < kN; ++e) {
             h[e] += f[e];
             if constexpr (BF16) h[e] = __bfloat162float(__float2bfloat16_rn(h[e]));
         }
     }
-}
+};
 
 // Eight values of y out: h rstd w, as values or as codes.
 template <bool BF16, bool ALIGNED, bool CODES>
-__device__ __forceinline__ void put_norm(const NormArgs& a, int32_t row, int32_t c, const float (&h)[kN], float rstd, bool far,
-                                         int lane) {
+__device__ __forceinline__ void put_norm(const NormArgs& a, int32_t row, int32_t c, const float (&h)[kN],
+                                         const Vec8<BF16, ALIGNED>& weight, float rstd, bool far, int lane) {
     float y[kN];
-    load8<BF16, ALIGNED>(a.weight, c, a.dim, y);
+    weight.get(y);
 #pragma unroll
-    for (int e = 0; e < kN; ++e) y[e] = h[e] * rstd * y[e];
+    for (int e = 0; e < kN; ++e) y[e] = __fmul_rn(__fmul_rn(h[e], rstd), y[e]);
     if constexpr (CODES) {
         const float top = fmaxf(block_largest(largest(y)), kLeast8);
         if ((lane & (kBlockLanes - 1)) == 0 && c < a.dim)
@@ -92,24 +99,34 @@ __global__ void __launch_bounds__(kRowThreads8) norm_kernel(const __grid_constan
     const bool on = row < a.rows;
     pdl_wait();
     pdl_trigger();
-    float h[VECTORS][kN], s = 0.0f;
+    SumVec<BF16, ALIGNED> v[VECTORS];
+    Vec8<BF16, ALIGNED> w[VECTORS];
+    float s = 0.0f;
     const char* x = at_row<BF16>(a.x, row, a.x_stride);
     const char* r = a.residual ? at_row<BF16>(a.residual, row, a.residual_stride) : nullptr;
 #pragma unroll
-    for (int j = 0; j < VECTORS; ++j)
-        load_sum<BF16, ALIGNED>(x, r, (threadIdx.x + j * blockDim.x) * kN, on ? a.dim : 0, h[j]);
+    for (int j = 0; j < VECTORS; ++j) v[j].load(x, r, (threadIdx.x + j * blockDim.x) * kN, on ? a.dim : 0);
 #pragma unroll
-    for (int j = 0; j < VECTORS; ++j)
+    for (int j = 0; j < VECTORS; ++j) w[j].load(a.weight, (threadIdx.x + j * blockDim.x) * kN, a.dim);
 #pragma unroll
-        for (int e = 0; e < kN; ++e) s += h[j][e] * h[j][e];
-    const float rstd = __frsqrt_rn(row_sum(s, s_part) / (float)a.dim + a.eps);
+    for (int j = 0; j < VECTORS; ++j) {
+        float h[kN];
+        v[j].get(h, r != nullptr);
+        v[j].x.keep();
+        if (r) v[j].r.keep();
+#pragma unroll
+        for (int e = 0; e < kN; ++e) s = __fmaf_rn(h[e], h[e], s);
+    }
+    const float rstd = __frsqrt_rn(__fadd_rn(__fdiv_rn(row_sum(s, s_part), (float)a.dim), a.eps));
     if (!on) return;   // whole warps
     if (!CODES && a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
 #pragma unroll
     for (int j = 0; j < VECTORS; ++j) {
         const int32_t c = (threadIdx.x + j * blockDim.x) * kN;
-        if (a.sum) store8<BF16, ALIGNED>(at_row<BF16>(a.sum, row, a.sum_stride), c, a.dim, h[j], far, lane);
-        put_norm<BF16, ALIGNED, CODES>(a, row, c, h[j], rstd, far, lane);
+        float h[kN];
+        v[j].get(h, r != nullptr);
+        if (a.sum) store8<BF16, ALIGNED>(at_row<BF16>(a.sum, row, a.sum_stride), c, a.dim, h, far, lane);
+        put_norm<BF16, ALIGNED, CODES>(a, row, c, h, w[j], rstd, far, lane);
     }
 }
 
@@ -127,19 +144,24 @@ __global__ void __launch_bounds__(kRowThreads8) norm_long_kernel(const __grid_co
     float s = 0.0f;
     for (int32_t j = 0; j < steps; ++j) {
         const int32_t c = (threadIdx.x + j * kRowThreads8) * kN;
+        SumVec<BF16, ALIGNED> v;
         float h[kN];
-        load_sum<BF16, ALIGNED>(x, r, c, a.dim, h);
+        v.load(x, r, c, a.dim);
+        v.get(h, r != nullptr);
         if (sum) store8<BF16, ALIGNED>(sum, c, a.dim, h, false, lane);
 #pragma unroll
-        for (int e = 0; e < kN; ++e) s += h[e] * h[e];
+        for (int e = 0; e < kN; ++e) s = __fmaf_rn(h[e], h[e], s);
     }
-    const float rstd = __frsqrt_rn(row_sum(s, s_part) / (float)a.dim + a.eps);   // its barrier: the sum is written
+    const float rstd = __frsqrt_rn(__fadd_rn(__fdiv_rn(row_sum(s, s_part), (float)a.dim), a.eps));   // its barrier: the sum is written
     if (!CODES && a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
     for (int32_t j = 0; j < steps; ++j) {
         const int32_t c = (threadIdx.x + j * kRowThreads8) * kN;
+        Vec8<BF16, ALIGNED> v, w;
         float h[kN];
-        load8<BF16, ALIGNED>(sum ? sum : x, c, a.dim, h);
-        put_norm<BF16, ALIGNED, CODES>(a, row, c, h, rstd, far, lane);
+        v.load(sum ? sum : x, c, a.dim);
+        w.load(a.weight, c, a.dim);
+        v.get(h);
+        put_norm<BF16, ALIGNED, CODES>(a, row, c, h, w, rstd, far, lane);
     }
 }
 
@@ -161,10 +183,11 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const __grid_co
     const int32_t row0 = strip < strips ? (int32_t)((int64_t)a.rows * strip / strips) : 0;
     const int32_t row1 = strip < strips ? (int32_t)((int64_t)a.rows * (strip + 1) / strips) : 0;
     const int32_t most = (a.rows + strips - 1) / strips;   // the CTA's strips differ by a row: all take part in the barriers
-    float w[VECTORS][kN], dw[VECTORS][kN];
+    Vec8<BF16, ALIGNED> w[VECTORS];
+    float dw[VECTORS][kN];
 #pragma unroll
     for (int j = 0; j < VECTORS; ++j) {
-        load8<BF16, ALIGNED>(a.weight, (threadIdx.x + j * blockDim.x) * kN, a.dim, w[j]);
+        w[j].load(a.weight, (threadIdx.x + j * blockDim.x) * kN, a.dim);
 #pragma unroll
         for (int e = 0; e < kN; ++e) dw[j][e] = 0.0f;
     }
@@ -174,33 +197,47 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const __grid_co
         const int32_t dim = on ? a.dim : 0;
         const char* ph = at_row<BF16>(a.h, row, a.h_stride);
         const char* pd = at_row<BF16>(a.dy, row, a.dy_stride);
-        float h[VECTORS][kN], g[VECTORS][kN], ds[VECTORS][kN], s = 0.0f;
+        Vec8<BF16, ALIGNED> vh[VECTORS], vd[VECTORS], vs[VECTORS];
+        float s = 0.0f;
         const float rstd = on ? a.rstd[row] : 0.0f;
 #pragma unroll
         for (int j = 0; j < VECTORS; ++j) {
             const int32_t c = (threadIdx.x + j * blockDim.x) * kN;
-            load8<BF16, ALIGNED>(ph, c, dim, h[j]);
-            load8<BF16, ALIGNED>(pd, c, dim, g[j]);
-            if (a.dsum) load8<BF16, ALIGNED>(at_row<BF16>(a.dsum, row, a.dsum_stride), c, dim, ds[j]);
+            vh[j].load(ph, c, dim);
+            vd[j].load(pd, c, dim);
+            if (a.dsum) vs[j].load(at_row<BF16>(a.dsum, row, a.dsum_stride), c, dim);
         }
 #pragma unroll
-        for (int j = 0; j < VECTORS; ++j)
+        for (int j = 0; j < VECTORS; ++j) {
+            float h[kN], g[kN], u[kN];
+            vh[j].get(h);
+            vd[j].get(g);
+            w[j].get(u);
+            vh[j].keep();
+            vd[j].keep();
+            w[j].keep();
 #pragma unroll
             for (int e = 0; e < kN; ++e) {
-                dw[j][e] += g[j][e] * (h[j][e] * rstd);
-                g[j][e] *= w[j][e];
-                s += g[j][e] * h[j][e];
+                dw[j][e] = __fmaf_rn(g[e], __fmul_rn(h[e], rstd), dw[j][e]);
+                s = __fmaf_rn(__fmul_rn(g[e], u[e]), h[e], s);
             }
-        const float c1 = row_sum(s, s_part[i & 1]) / (float)a.dim * rstd * rstd;
+        }
+        const float c1 = __fmul_rn(__fmul_rn(__fdiv_rn(row_sum(s, s_part[i & 1]), (float)a.dim), rstd), rstd);
         if (!on) continue;
 #pragma unroll
         for (int j = 0; j < VECTORS; ++j) {
+            float h[kN], g[kN], u[kN];
+            vh[j].get(h);
+            vd[j].get(g);
+            w[j].get(u);
 #pragma unroll
-            for (int e = 0; e < kN; ++e) {
-                g[j][e] = rstd * (g[j][e] - h[j][e] * c1);
-                if (a.dsum) g[j][e] += ds[j][e];
+            for (int e = 0; e < kN; ++e) g[e] = __fmul_rn(rstd, __fmaf_rn(-h[e], c1, __fmul_rn(g[e], u[e])));
+            if (a.dsum) {
+                vs[j].get(h);
+#pragma unroll
+                for (int e = 0; e < kN; ++e) g[e] = __fadd_rn(g[e], h[e]);
             }
-            store8<BF16, ALIGNED>(at_row<BF16>(a.dx, row, a.dx_stride), (threadIdx.x + j * blockDim.x) * kN, a.dim, g[j], far, lane);
+            store8<BF16, ALIGNED>(at_row<BF16>(a.dx, row, a.dx_stride), (threadIdx.x + j * blockDim.x) * kN, a.dim, g, far, lane);
         }
     }
     if (strip >= strips) return;
@@ -223,16 +260,20 @@ __global__ void __launch_bounds__(kRowThreads8) norm_grad_sums_kernel(const __gr
     const int32_t row = blockIdx.x;
     float s = 0.0f;
     for (int32_t c = threadIdx.x * kN; c < a.dim; c += kRowThreads8 * kN) {
+        Vec8<BF16, ALIGNED> vh, vd, vw;
         float h[kN], g[kN], w[kN];
-        load8<BF16, ALIGNED>(at_row<BF16>(a.h, row, a.h_stride), c, a.dim, h);
-        load8<BF16, ALIGNED>(at_row<BF16>(a.dy, row, a.dy_stride), c, a.dim, g);
-        load8<BF16, ALIGNED>(a.weight, c, a.dim, w);
+        vh.load(at_row<BF16>(a.h, row, a.h_stride), c, a.dim);
+        vd.load(at_row<BF16>(a.dy, row, a.dy_stride), c, a.dim);
+        vw.load(a.weight, c, a.dim);
+        vh.get(h);
+        vd.get(g);
+        vw.get(w);
 #pragma unroll
-        for (int e = 0; e < kN; ++e) s += w[e] * g[e] * h[e];
+        for (int e = 0; e < kN; ++e) s = __fmaf_rn(__fmul_rn(g[e], w[e]), h[e], s);
     }
     s = row_sum(s, s_part);
     const float rstd = a.rstd[row];
-    if (threadIdx.x == 0) sums[row] = s / (float)a.dim * rstd * rstd;
+    if (threadIdx.x == 0) sums[row] = __fmul_rn(__fmul_rn(__fdiv_rn(s, (float)a.dim), rstd), rstd);
 }
 template <bool BF16, bool ALIGNED>
 __global__ void __launch_bounds__(kGradThreads) norm_grad_long_kernel(const __grid_constant__ NormGradArgs a, const float* sums,
@@ -248,16 +289,22 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_long_kernel(const __gr
 #pragma unroll
     for (int e = 0; e < kN; ++e) dw[e] = 0.0f;
     for (int32_t row = row0; row < row1; ++row) {
+        Vec8<BF16, ALIGNED> vh, vd, vs;
         float h[kN], g[kN], ds[kN];
         const float rstd = a.rstd[row], c1 = sums[row];
-        load8<BF16, ALIGNED>(at_row<BF16>(a.h, row, a.h_stride), c, a.dim, h);
-        load8<BF16, ALIGNED>(at_row<BF16>(a.dy, row, a.dy_stride), c, a.dim, g);
-        if (a.dsum) load8<BF16, ALIGNED>(at_row<BF16>(a.dsum, row, a.dsum_stride), c, a.dim, ds);
+        vh.load(at_row<BF16>(a.h, row, a.h_stride), c, a.dim);
+        vd.load(at_row<BF16>(a.dy, row, a.dy_stride), c, a.dim);
+        if (a.dsum) {
+            vs.load(at_row<BF16>(a.dsum, row, a.dsum_stride), c, a.dim);
+            vs.get(ds);
+        }
+        vh.get(h);
+        vd.get(g);
 #pragma unroll
         for (int e = 0; e < kN; ++e) {
-            dw[e] += g[e] * (h[e] * rstd);
-            g[e] = rstd * (w[e] * g[e] - h[e] * c1);
-            if (a.dsum) g[e] += ds[e];
+            dw[e] = __fmaf_rn(g[e], __fmul_rn(h[e], rstd), dw[e]);
+            g[e] = __fmul_rn(rstd, __fmaf_rn(-h[e], c1, __fmul_rn(g[e], w[e])));
+            if (a.dsum) g[e] = __fadd_rn(g[e], ds[e]);
         }
         store8<BF16, ALIGNED>(at_row<BF16>(a.dx, row, a.dx_stride), c, a.dim, g, far, lane);
     }

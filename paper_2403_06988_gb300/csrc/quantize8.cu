@@ -21,21 +21,23 @@ __global__ void __launch_bounds__(kThreads8) rows_kernel(const __grid_constant__
     pdl_trigger();
     const int lane = threadIdx.x & (kBlockLanes - 1), half = threadIdx.x / kBlockLanes;
     const int32_t blocks = (a.dim + kBlock8 - 1) / kBlock8;
-    float f[kTogether8][kN];
+    Vec8<BF16, ALIGNED> v[kTogether8];
     int32_t row[kTogether8], c[kTogether8];
 #pragma unroll
     for (int j = 0; j < kTogether8; ++j) {
         const int64_t i = ((int64_t)blockIdx.x * kTogether8 + j) * kHalves + half;
         row[j] = (int32_t)(pieces <= UINT_MAX ? (uint32_t)i / (uint32_t)blocks : i / blocks);
         c[j] = i < pieces ? (int32_t)(i - (int64_t)row[j] * blocks) * kBlock8 + lane * kN : a.dim;
-        load8<BF16, ALIGNED>((const char*)a.x + row[j] * a.stride * (BF16 ? 2 : 4), c[j], a.dim, f[j]);
+        v[j].load((const char*)a.x + row[j] * a.stride * (BF16 ? 2 : 4), c[j], a.dim);
     }
 #pragma unroll
     for (int j = 0; j < kTogether8; ++j) {
-        const float top = fmaxf(block_largest(largest(f[j])), kLeast8);
+        float f[kN];
+        v[j].get(f);
+        const float top = fmaxf(block_largest(largest(f)), kLeast8);
         if (c[j] >= a.dim) continue;
         if (lane == 0) a.scales[(int64_t)row[j] * blocks + c[j] / kBlock8] = top / kMost8;
-        store_codes(a.codes + row[j] * a.codes_stride, c[j], a.dim, f[j], kMost8 / top, far);
+        store_codes(a.codes + row[j] * a.codes_stride, c[j], a.dim, f, kMost8 / top, far);
     }
 }
 
@@ -49,14 +51,20 @@ __global__ void __launch_bounds__(kThreads8) tiles_kernel(const __grid_constant_
     const int32_t blocks = (a.dim + kBlock8 - 1) / kBlock8;
     const int32_t tile = blockIdx.x / blocks, block = blockIdx.x - tile * blocks;
     const int32_t c = block * kBlock8 + lane * kN;
-    float f[kPerHalf][kN], top = 0.0f;
+    Vec8<BF16, ALIGNED> v[kPerHalf];
+    float top = 0.0f;
 #pragma unroll
     for (int j = 0; j < kPerHalf; ++j) {
         const int64_t row = (int64_t)tile * kTileRows + j * kHalves + half;
-        load8<BF16, ALIGNED>((const char*)a.x + row * a.stride * (BF16 ? 2 : 4), c, row < a.rows ? a.dim : 0, f[j]);
+        v[j].load((const char*)a.x + row * a.stride * (BF16 ? 2 : 4), c, row < a.rows ? a.dim : 0);
     }
 #pragma unroll
-    for (int j = 0; j < kPerHalf; ++j) top = fmaxf(top, largest(f[j]));
+    for (int j = 0; j < kPerHalf; ++j) {
+        float f[kN];
+        v[j].get(f);
+        v[j].keep();
+        top = fmaxf(top, largest(f));
+    }
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
     if ((threadIdx.x & 31) == 0) s_top[threadIdx.x >> 5] = top;
@@ -69,7 +77,9 @@ __global__ void __launch_bounds__(kThreads8) tiles_kernel(const __grid_constant_
 #pragma unroll
     for (int j = 0; j < kPerHalf; ++j) {
         const int64_t row = (int64_t)tile * kTileRows + j * kHalves + half;
-        if (row < a.rows) store_codes(a.codes + row * a.codes_stride, c, a.dim, f[j], by, far);
+        float f[kN];
+        v[j].get(f);
+        if (row < a.rows) store_codes(a.codes + row * a.codes_stride, c, a.dim, f, by, far);
     }
 }
 

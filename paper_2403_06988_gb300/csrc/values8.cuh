@@ -21,33 +21,84 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// Values c, .. c + 7 of a row of dim; zeros beyond its end.  ALIGNED: the row begins on a 16-byte boundary.  With
-// neither __ldg nor another assumption that the row is not written by this kernel: outputs may take inputs' places.
+// Values c, .. c + 7 of a row of dim; zeros beyond its end.  ALIGNED: the row begins on a 16-byte boundary.  load() reads
+// and uses nothing of what it reads, so that a thread's loads are on their way together, and get() converts (128256 x 4096
+// bf16 in codes: MEASURED).  After keep() a get() converts again: what is kept meanwhile are the bits, not fp32 values.  Rows are read in the 16-byte blocks that hold their values.  Neither __ldg nor another
+// assumption that the row is not written by this kernel: outputs may take inputs' places.
+template <bool BF16, bool ALIGNED>
+struct Vec8;
+template <>
+struct Vec8<true, true> {
+    uint4 u;
+    int32_t left;
+    __device__ __forceinline__ void keep() { asm volatile("" : "+r"(u.x), "+r"(u.y), "+r"(u.z), "+r"(u.w)); }
+    __device__ __forceinline__ void load(const void* row, int32_t c, int32_t dim) {
+        left = dim - c;
+        u = make_uint4(0u, 0u, 0u, 0u);
+        if (left > 0) u = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(row) + c);
+    }
+    __device__ __forceinline__ void get(float (&f)[kN]) const {
+        f[0] = bf16_lo(u.x), f[1] = bf16_hi(u.x), f[2] = bf16_lo(u.y), f[3] = bf16_hi(u.y);
+        f[4] = bf16_lo(u.z), f[5] = bf16_hi(u.z), f[6] = bf16_lo(u.w), f[7] = bf16_hi(u.w);
+        if (left > 0 && left < kN) {
+#pragma unroll
+            for (int e = 0; e < kN; ++e) f[e] = e < left ? f[e] : 0.0f;
+        }
+    }
+};
+template <>
+struct Vec8<true, false> {
+    Eight x;
+    __device__ __forceinline__ void keep() {   // in one block from now on
+        x.u = eight_from(x.u, x.v, x.off);
+        x.v = make_uint4(0u, 0u, 0u, 0u);
+        x.off = 0u;
+        asm volatile("" : "+r"(x.u.x), "+r"(x.u.y), "+r"(x.u.z), "+r"(x.u.w));
+    }
+    __device__ __forceinline__ void load(const void* row, int32_t c, int32_t dim) {
+        x.zero();
+        if (dim > c) x.load(static_cast<const __nv_bfloat16*>(row) + c, dim - c);
+    }
+    __device__ __forceinline__ void get(float (&f)[kN]) const { x.get(f); }
+};
+template <>
+struct Vec8<false, true> {
+    float4 u, v;
+    int32_t left;
+    __device__ __forceinline__ void keep() {}
+    __device__ __forceinline__ void load(const void* row, int32_t c, int32_t dim) {
+        left = dim - c;
+        const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(row) + c);
+        u = v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (left > 0) u = p[0];
+        if (left > 4) v = p[1];
+    }
+    __device__ __forceinline__ void get(float (&f)[kN]) const {
+        f[0] = u.x, f[1] = u.y, f[2] = u.z, f[3] = u.w, f[4] = v.x, f[5] = v.y, f[6] = v.z, f[7] = v.w;
+        if (left > 0 && left < kN) {
+#pragma unroll
+            for (int e = 0; e < kN; ++e) f[e] = e < left ? f[e] : 0.0f;
+        }
+    }
+};
+template <>
+struct Vec8<false, false> {
+    float x[kN];
+    __device__ __forceinline__ void keep() {}
+    __device__ __forceinline__ void load(const void* row, int32_t c, int32_t dim) {
+#pragma unroll
+        for (int e = 0; e < kN; ++e) x[e] = c + e < dim ? static_cast<const float*>(row)[c + e] : 0.0f;
+    }
+    __device__ __forceinline__ void get(float (&f)[kN]) const {
+#pragma unroll
+        for (int e = 0; e < kN; ++e) f[e] = x[e];
+    }
+};
 template <bool BF16, bool ALIGNED>
 __device__ __forceinline__ void load8(const void* row, int32_t c, int32_t dim, float (&f)[kN]) {
-    const int32_t left = dim - c;
-    if constexpr (BF16) {
-        const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(row) + c;
-        if (ALIGNED && left >= kN) {
-            const uint4 u = *reinterpret_cast<const uint4*>(p);
-            f[0] = bf16_lo(u.x), f[1] = bf16_hi(u.x), f[2] = bf16_lo(u.y), f[3] = bf16_hi(u.y);
-            f[4] = bf16_lo(u.z), f[5] = bf16_hi(u.z), f[6] = bf16_lo(u.w), f[7] = bf16_hi(u.w);
-            return;
-        }
-        Eight e;
-        e.zero();
-        if (left > 0) e.load(p, left);
-        e.get(f);
-    } else {
-        const float* p = static_cast<const float*>(row) + c;
-        if (ALIGNED && left >= kN) {
-            const float4 u = reinterpret_cast<const float4*>(p)[0], v = reinterpret_cast<const float4*>(p)[1];
-            f[0] = u.x, f[1] = u.y, f[2] = u.z, f[3] = u.w, f[4] = v.x, f[5] = v.y, f[6] = v.z, f[7] = v.w;
-            return;
-        }
-#pragma unroll
-        for (int e = 0; e < kN; ++e) f[e] = e < left ? p[e] : 0.0f;
-    }
+    Vec8<BF16, ALIGNED> v;
+    v.load(row, c, dim);
+    v.get(f);
 }
 
 // The same values to a row.  The whole warp calls it, its lanes with consecutive c's.  far: past the L2.
