@@ -9,6 +9,12 @@
 //                 scaled, to sums in their registers while the next is filled.  A warp's
 //                 columns lie in one block of 128 weight rows, so that a block of k costs
 //                 each of its rows one scale.
+//
+// Few rows: bound by HBM (64 x 128256 x 4096 97 us, 5.8 TB/s).  Many: by the folds.  A block
+// of 128 x 256 products takes the tensor cores 512 cycles, its 32 KB from L2 about 640, and
+// the fold's 32768 fused products on 128 lanes 256, between waits that two warps a scheduler
+// do not hide: 970 cycles in all (2048 x 128256 x 4096 820 us, 2.6 PFLOP/s; with a
+// quarter of the fused products, timed alone, 3.1).
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -28,16 +34,27 @@ constexpr int kRowsM = 128, kTileK = 128, kWideN = 256, kNarrowN = 64;
 constexpr int kRingBytes = 196608;             // of operand tiles on their way
 constexpr int kMaxStages = 16;                 // blocks of k of them
 constexpr int kFoldWarps = 8;
+// Warps that issue products, each every other accumulator's: one takes 980 cycles for a block's waits, products and commits
+// (2048 x 38912 x 4096 281 us, with two of them 262).
+constexpr int kIssuers = 2;
 template <bool PAIR, int N>
 struct Tile {
     static constexpr int kCtas = PAIR ? 2 : 1;
     static constexpr int kM = kRowsM * kCtas;
+    // A block's products of 256 columns are made, and folded, in two parts, each in an accumulator of its own, so that a fold
+    // has the time of three parts' products and not of one tile's (2048 x 38912 x 4096: 250 us, whole tiles in two
+    // accumulators 273).
+    static constexpr int kParts = N == kWideN ? 2 : 1, kPartN = N / kParts, kAccs = 4;
     static constexpr int kRowsB = N / kCtas;                // a CTA's
     static constexpr int kBytesB = kRowsB * kTileK;
     static constexpr int kColumns = N / (kFoldWarps / 4);   // a fold warp's: 32 rows, half of the columns
-    static constexpr int kAccs = N == kWideN ? 2 : 4;       // accumulators of N columns
-    static_assert(kColumns % 32 == 0 && 128 % kColumns == 0 && kAccs * N <= 512);
+    static constexpr int kFolds = kFoldWarps / kParts;      // fold warps of a part
+    static_assert(kColumns % 32 == 0 && 128 % kColumns == 0 && kAccs * kPartN <= 512);
 };
+// Registers of a thread: the fold warps' sums of 128 columns and what is on its way take more than an equal share (with 168
+// for all, loads of 16 columns and none ahead: 273 us where this takes 250; sixteen warps of 64 columns 263).  The shares'
+// sum is within what the CTA is launched with (smem_ready looks).
+constexpr int kFoldRegs = 216, kOtherRegs = 72;
 
 // Results leave through shared memory: 32 rows of 64 bytes a warp's buffer, in the 64-byte swizzle.
 constexpr int kOutBytes = 32 * 64, kOutBuffers = 2;
@@ -130,7 +147,7 @@ __device__ __forceinline__ void put_out(const Product8& p, int32_t x, int32_t y,
 template <bool BF16, bool PAIR, int N>
 __global__ void __launch_bounds__(kThreads, 1) logits8_kernel(const __grid_constant__ Product8 p) {
     using T = Tile<PAIR, N>;
-    constexpr int kColumns = T::kColumns, kAccs = T::kAccs, kTmemColumns = kAccs * N;
+    constexpr int kColumns = T::kColumns, kAccs = T::kAccs, kTmemColumns = kAccs * T::kPartN;
     extern __shared__ unsigned char smem[];
     __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_acc_full[kAccs], s_acc_empty[kAccs], s_done;
     __shared__ uint32_t s_tmem, s_failed;
@@ -145,13 +162,13 @@ __global__ void __launch_bounds__(kThreads, 1) logits8_kernel(const __grid_const
         s_failed = 0u;
         for (int s = 0; s < kMaxStages; ++s) {
             bar_init(smem_addr(&s_full[s]), 1);
-            bar_init(smem_addr(&s_empty[s]), 1);
+            bar_init(smem_addr(&s_empty[s]), T::kParts);
         }
         for (int s = 0; s < kAccs; ++s) {
             bar_init(smem_addr(&s_acc_full[s]), 1);
-            bar_init(smem_addr(&s_acc_empty[s]), kFoldWarps * T::kCtas);
+            bar_init(smem_addr(&s_acc_empty[s]), T::kFolds * T::kCtas);
         }
-        bar_init(smem_addr(&s_done), 1);
+        bar_init(smem_addr(&s_done), kIssuers);
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         tma_prefetch_map(&p.a);
         tma_prefetch_map(&p.b);
@@ -165,69 +182,82 @@ __global__ void __launch_bounds__(kThreads, 1) logits8_kernel(const __grid_const
     pdl_wait();
     pdl_trigger();
 
-    if (warp == 0) {   // ---- loads: each CTA its part of the tiles; the first CTA's barriers count the bytes of both
-        uint32_t s = 0, turn = 0, loads = 0;   // the stage, how often the ring has come round
-        bool ok = true;
-        for (int32_t i = first; i < p.items && ok; i += step) {
-            const Item t = item_at(p, i);
-            const int32_t row_a = t.m * T::kM + rank * kRowsM, row_b = t.n * N + rank * T::kRowsB;
-            for (int32_t k = 0; k < p.k_blocks; ++k) {
-                if (!(ok = warp_wait(smem_addr(&s_empty[s]), (turn & 1u) ^ 1u, failed))) break;
-                const uint32_t mine = smem_addr(&s_full[s]), a = tiles + s * stage_bytes;
-                const uint32_t full = PAIR ? in_cta(mine, 0) : mine;
-                if (elect_lane()) {
-                    if (rank == 0) bar_expect(mine, stage_bytes * T::kCtas);
-                    tma_load<PAIR>(a, &p.a, k * kTileK, row_a, full);
-                    tma_load<PAIR>(a + bytes_a, &p.b, k * kTileK, row_b, full);
-                }
-                ++loads;
-                if (++s == stages) {
-                    s = 0;
-                    ++turn;
-                }
-            }
-        }
-        // given up: the loads on their way write into this CTA's memory
-        if (!ok && rank == 0 && lane == 0)
-            for (uint32_t j = 1; j <= stages && j <= loads; ++j) {
-                const uint32_t last = loads - j;   // the stages' last loads
-                const uint64_t end = timer_ns() + kWaitNs;
-                while (!bar_try(smem_addr(&s_full[last % stages]), (last / stages) & 1u) && timer_ns() < end) {}
-            }
-    } else if (warp == 1) {   // ---- products: a block of k each an accumulator
-        if (rank == 0) {
-            constexpr uint32_t desc = mma_desc8(T::kM, N);
-            uint32_t s = 0, turn = 0, accs = 0;
+    if (warp < 4) {
+        if constexpr (T::kParts == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kOtherRegs));
+        if (warp == 0) {   // ---- loads: each CTA its part of the tiles; the first CTA's barriers count the bytes of both
+            uint32_t s = 0, turn = 0, loads = 0;   // the stage, how often the ring has come round
             bool ok = true;
             for (int32_t i = first; i < p.items && ok; i += step) {
-                for (int32_t k = 0; k < p.k_blocks; ++k, ++accs) {
-                    const uint32_t s_acc = accs % kAccs, acc = tmem + s_acc * N;
-                    if (!(ok = warp_wait(smem_addr(&s_acc_empty[s_acc]), ((accs / kAccs) & 1u) ^ 1u, failed))) break;
-                    if (!(ok = warp_wait(smem_addr(&s_full[s]), turn & 1u, failed))) break;
-                    tcgen_after();
-                    const uint64_t a = operand_desc(tiles + s * stage_bytes, 0);
-                    const uint64_t b = operand_desc(tiles + s * stage_bytes + bytes_a, 0);
+                const Item t = item_at(p, i);
+                const int32_t row_a = t.m * T::kM + rank * kRowsM, row_b = t.n * N;
+                for (int32_t k = 0; k < p.k_blocks; ++k) {
+                    if (!(ok = warp_wait(smem_addr(&s_empty[s]), (turn & 1u) ^ 1u, failed))) break;
+                    const uint32_t mine = smem_addr(&s_full[s]), a = tiles + s * stage_bytes;
+                    const uint32_t full = PAIR ? in_cta(mine, 0) : mine;
                     if (elect_lane()) {
-#pragma unroll
-                        for (int j = 0; j < kTileK / 32; ++j)   // 32 k: 32 bytes further, in 16-byte units
-                            mma_e4m3<PAIR>(acc, a + (uint64_t)(j * 2), b + (uint64_t)(j * 2), desc, j > 0);
-                        mma_commit<PAIR>(smem_addr(&s_empty[s]));
-                        mma_commit<PAIR>(smem_addr(&s_acc_full[s_acc]));
+                        if (rank == 0) bar_expect(mine, stage_bytes * T::kCtas);
+                        tma_load<PAIR>(a, &p.a, k * kTileK, row_a, full);
+                        if constexpr (PAIR) {   // half of each part's rows
+    #pragma unroll
+                            for (int h = 0; h < T::kParts; ++h)
+                                tma_load<PAIR>(a + bytes_a + h * (T::kBytesB / T::kParts), &p.b, k * kTileK,
+                                               row_b + h * T::kPartN + rank * (T::kPartN / 2), full);
+                        } else {
+                            tma_load<PAIR>(a + bytes_a, &p.b, k * kTileK, row_b, full);
+                        }
                     }
+                    ++loads;
                     if (++s == stages) {
                         s = 0;
                         ++turn;
                     }
                 }
             }
-            if (elect_lane()) mma_commit<PAIR>(smem_addr(&s_done));
+            // given up: the loads on their way write into this CTA's memory
+            if (!ok && rank == 0 && lane == 0)
+                for (uint32_t j = 1; j <= stages && j <= loads; ++j) {
+                    const uint32_t last = loads - j;   // the stages' last loads
+                    const uint64_t end = timer_ns() + kWaitNs;
+                    while (!bar_try(smem_addr(&s_full[last % stages]), (last / stages) & 1u) && timer_ns() < end) {}
+                }
+        } else if (warp <= kIssuers) {   // ---- products: a part of a block of k each an accumulator
+            if (rank == 0) {
+                constexpr uint32_t desc = mma_desc8(T::kM, T::kPartN);
+                // the warp's: every kIssuers-th accumulator, of the same part of every block where there are two
+                const int64_t blocks = (int64_t)((p.items - first + step - 1) / step) * p.k_blocks;
+                const uint32_t h = T::kParts == 2 ? warp - 1 : 0;
+                constexpr uint32_t kStep = kIssuers / T::kParts;
+                uint32_t s = T::kParts == 2 ? 0 : warp - 1, turn = 0, u = warp - 1;
+                for (int64_t block = s; block < blocks; block += kStep, u += kIssuers) {
+                    if (s >= stages) {
+                        s -= stages;
+                        ++turn;
+                    }
+                    const uint32_t s_acc = u % kAccs, acc = tmem + s_acc * T::kPartN;
+                    if (!warp_wait(smem_addr(&s_acc_empty[s_acc]), ((u / kAccs) & 1u) ^ 1u, failed)) break;
+                    if (!warp_wait(smem_addr(&s_full[s]), turn & 1u, failed)) break;
+                    tcgen_after();
+                    const uint64_t a = operand_desc(tiles + s * stage_bytes, 0);
+                    const uint64_t b = operand_desc(tiles + s * stage_bytes + bytes_a + h * (T::kBytesB / T::kParts), 0);
+                    if (elect_lane()) {
+    #pragma unroll
+                        for (int j = 0; j < kTileK / 32; ++j)   // 32 k: 32 bytes further, in 16-byte units
+                            mma_e4m3<PAIR>(acc, a + (uint64_t)(j * 2), b + (uint64_t)(j * 2), desc, j > 0);
+                        mma_commit<PAIR>(smem_addr(&s_acc_full[s_acc]));
+                        mma_commit<PAIR>(smem_addr(&s_empty[s]));
+                    }
+                    s += kStep;
+                }
+                if (elect_lane()) mma_commit<PAIR>(smem_addr(&s_done));
+            }
+            // no product, and no arrival at a barrier of this CTA, may be on its way when the CTA ends
+            if (lane == 0) {
+                const uint64_t end = timer_ns() + 3 * kWaitNs;
+                while (!bar_try(smem_addr(&s_done), 0u) && timer_ns() < end) {}
+            }
         }
-        // no product, and no arrival at a barrier of this CTA, may be on its way when the CTA ends
-        if (lane == 0) {
-            const uint64_t end = timer_ns() + 3 * kWaitNs;
-            while (!bar_try(smem_addr(&s_done), 0u) && timer_ns() < end) {}
-        }
-    } else if (warp >= 4) {   // ---- folds
+    } else {   // ---- folds
+        if constexpr (T::kParts == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kFoldRegs));
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         const uint32_t buffers = tiles + kRingBytes + (warp - 4) * kOutBuffers * kOutBytes;
         const int row_in_tile = rank * kRowsM + quarter * 32 + lane;
@@ -242,31 +272,44 @@ __global__ void __launch_bounds__(kThreads, 1) logits8_kernel(const __grid_const
             float2 x[kColumns / 2];
 #pragma unroll
             for (int e = 0; e < kColumns / 2; ++e) x[e] = make_float2(0.0f, 0.0f);
-            float next = __ldg(rs) * __ldg(cs);
+            float next_r = __ldg(rs), next_c = __ldg(cs);
             for (int32_t k = 0; k < p.k_blocks; ++k) {
-                const float c = next;
-                if (k + 1 < p.k_blocks) next = __ldg(rs + k + 1) * __ldg(cs + k + 1);
-                const uint32_t s_acc = accs % kAccs;
-                if (!(ok = warp_wait(smem_addr(&s_acc_full[s_acc]), (accs / kAccs) & 1u, failed))) break;
-                tcgen_after();
-                if (some) {
-                    const uint32_t acc = tmem + s_acc * N + half * kColumns + ((uint32_t)(quarter * 32) << 16);
-#pragma unroll
-                    for (int j = 0; j < kColumns; j += 16) {
-                        float v[16];
-                        tmem_load16(v, acc + j);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) x[j / 2 + e] = add_scaled(x[j / 2 + e], make_float2(v[2 * e], v[2 * e + 1]), c);
-                    }
+                const float c = next_r * next_c;
+                if (k + 1 < p.k_blocks) {
+                    next_r = __ldg(rs + k + 1);
+                    next_c = __ldg(cs + k + 1);
                 }
-                tcgen_before();
-                __syncwarp();
-                if (lane == 0) {
-                    const uint32_t bar = smem_addr(&s_acc_empty[s_acc]);
-                    if constexpr (PAIR) bar_arrive_cluster(in_cta(bar, 0));
-                    else bar_arrive(bar);
-                }
+                // the block's accumulator: of the warp's half where there are two
+                const uint32_t turns = accs * T::kParts + (T::kParts == 2 ? half : 0), s_acc = turns % kAccs;
                 ++accs;
+                if (!(ok = warp_wait(smem_addr(&s_acc_full[s_acc]), (turns / kAccs) & 1u, failed))) break;
+                tcgen_after();
+                const uint32_t acc = tmem + s_acc * T::kPartN + (T::kParts == 2 ? 0 : half * kColumns) + ((uint32_t)(quarter * 32) << 16);
+                const auto emptied = [&] {
+                    tcgen_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        const uint32_t bar = smem_addr(&s_acc_empty[s_acc]);
+                        if constexpr (PAIR) bar_arrive_cluster(in_cta(bar, 0));
+                        else bar_arrive(bar);
+                    }
+                };
+                if (!some) {
+                    emptied();
+                    continue;
+                }
+                // 32 columns are added while the next are on their way
+                uint32_t v[2][32];
+                tmem_fetch32(v[0], acc);
+#pragma unroll
+                for (int j = 0; j < kColumns / 32; ++j) {
+                    tmem_wait32(v[j & 1]);
+                    if (j + 1 < kColumns / 32) tmem_fetch32(v[(j + 1) & 1], acc + 32 * (j + 1));
+                    else emptied();
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        x[16 * j + e] = add_scaled(x[16 * j + e], make_float2(__uint_as_float(v[j & 1][2 * e]), __uint_as_float(v[j & 1][2 * e + 1])), c);
+                }
             }
             if (!ok) break;
             if (!some) continue;
@@ -303,11 +346,15 @@ int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 enum Shape : int { kPair = 0, kWide = 1, kNarrow = 2 };   // 256 x 256 of two CTAs, 128 x 256, 128 x 64
 int shape_m(Shape s) { return s == kPair ? 2 * kRowsM : kRowsM; }
 int shape_n(Shape s) { return s == kNarrow ? kNarrowN : kWideN; }
-int shape_box(Shape s) { return s == kWide ? kWideN : s == kPair ? kWideN / 2 : kNarrowN; }   // rows of the weight a CTA loads
+int shape_box(Shape s) { return s == kWide ? kWideN : s == kPair ? kWideN / 4 : kNarrowN; }   // rows of the weight of a load
 
+// Narrow tiles where every SM has at most one (us narrow / wide: 1 x 1000 x 64 3.0, 4.9; 128 x 8000 x 4096 11.6, 19.7; more
+// than one round of them, 64 x 32000 x 1024 13.5, 10.7; 64 x 128256 x 4096 111, 97).  Pairs read two thirds of the bytes
+// from L2; not where they leave a quarter or more of few tiles' rows empty (us pair / wide: 2048 x 38912 x 4096 250, 258;
+// 390 x 100000 x 2048 94, 97; 256 rows alike; 300 x 32000 x 1024 24, 19; 777 x 50000 x 1024 57, 54).
 Shape shape_of(const Logits8Args& a, const LaunchEnv& env) {
     const int tiles = ceil_div(a.rows, kRowsM);
-    if ((int64_t)tiles * ceil_div(a.n_tokens, kNarrowN) <= env.num_sms * 4) return kNarrow;
+    if ((int64_t)tiles * ceil_div(a.n_tokens, kNarrowN) <= env.num_sms) return kNarrow;
     return tiles % 2 == 0 || tiles > 15 ? kPair : kWide;
 }
 
@@ -323,6 +370,11 @@ cudaError_t smem_ready() {
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess || (dev < kDevices && ready[dev].load())) return e;
     e = cudaFuncSetAttribute(logits8_kernel<BF16, PAIR, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem8);
+    cudaFuncAttributes attr;
+    if (e == cudaSuccess) e = cudaFuncGetAttributes(&attr, logits8_kernel<BF16, PAIR, N>);
+    // a CTA launched with fewer registers than its warps' shares would wait for ever
+    if (e == cudaSuccess && Tile<PAIR, N>::kParts == 2 && attr.numRegs * kThreads < kFoldRegs * 32 * kFoldWarps + kOtherRegs * 128)
+        e = cudaErrorLaunchOutOfResources;
     if (e == cudaSuccess && dev < kDevices) ready[dev].store(true);
     return e;
 }

@@ -14,6 +14,7 @@
 // rounded once each.  Products and sums are fused where the code says so and nowhere
 // else: rows at any alignment give the same bits.
 #include <algorithm>
+#include <atomic>
 
 #include "norm.h"
 #include "values8.cuh"
@@ -51,43 +52,69 @@ __device__ __forceinline__ char* at_row(const void* p, int64_t row, int64_t stri
     return (char*)p + row * stride * (BF16 ? 2 : 4);
 }
 
-// Eight values of h: x, or the rounded sum.
-template <bool BF16, bool ALIGNED>
-struct SumVec {
-    Vec8<BF16, ALIGNED> x, r;
-    __device__ __forceinline__ void load(const char* px, const char* pr, int32_t c, int32_t dim) {
-        x.load(px, c, dim);
-        if (pr) r.load(pr, c, dim);
-    }
-    __device__ __forceinline__ void get(float (&h)[kN], bool residual) const {
-        x.get(h);
-        if (!residual) return;
-        float f[kN];
-        r.get(f);
+// Eight values of h, x or the rounded sum, as their bits: bf16 in four words.
+template <bool BF16>
+struct Held {
+    uint32_t w[BF16 ? 4 : 8];
+    __device__ __forceinline__ void set(const float (&h)[kN]) {
+        if constexpr (BF16) {
 #pragma unroll
-        for (int e = 0; e < kN; ++e) {
-            h[e] += f[e];
-            if constexpr (BF16) h[e] = __bfloat162float(__float2bfloat16_rn(h[e]));
+            for (int e = 0; e < 4; ++e) w[e] = pack2(h[2 * e], h[2 * e + 1]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < kN; ++e) w[e] = __float_as_uint(h[e]);
         }
     }
+    __device__ __forceinline__ void get(float (&h)[kN]) const {
+        if constexpr (BF16) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[2 * e] = bf16_lo(w[e]), h[2 * e + 1] = bf16_hi(w[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < kN; ++e) h[e] = __uint_as_float(w[e]);
+        }
+    }
+    // From now on get() unpacks again.
+    __device__ __forceinline__ void keep() {
+        if constexpr (BF16) asm volatile("" : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3]));
+    }
 };
+template <bool BF16, bool ALIGNED>
+__device__ __forceinline__ Held<BF16> held(const Vec8<BF16, ALIGNED>& x, const Vec8<BF16, ALIGNED>& r, bool residual) {
+    Held<BF16> out;
+    float h[kN];
+    x.get(h);
+    if (residual) {
+        float f[kN];
+        r.get(f);
+        add8(h, f);
+    }
+    out.set(h);   // without a residual the bits that were read
+    return out;
+}
 
 // Eight values of y out: h rstd w, as values or as codes.
 template <bool BF16, bool ALIGNED, bool CODES>
 __device__ __forceinline__ void put_norm(const NormArgs& a, int32_t row, int32_t c, const float (&h)[kN],
                                          const Vec8<BF16, ALIGNED>& weight, float rstd, bool far, int lane) {
-    float y[kN];
-    weight.get(y);
+    float y[kN], w[kN];
+    weight.get(w);
 #pragma unroll
-    for (int e = 0; e < kN; ++e) y[e] = __fmul_rn(__fmul_rn(h[e], rstd), y[e]);
+    for (int e = 0; e < kN; ++e) y[e] = h[e];
+    mul8(y, rstd);
+    mul8(y, w);
     if constexpr (CODES) {
         const float top = fmaxf(block_largest(largest(y)), kLeast8);
         if ((lane & (kBlockLanes - 1)) == 0 && c < a.dim)
-            a.scales[(int64_t)row * ((a.dim + kBlock8 - 1) / kBlock8) + c / kBlock8] = top / kMost8;
+            a.scales[(int64_t)row * ((a.dim + kBlock8 - 1) / kBlock8) + c / kBlock8] = scale_of(top);
         store_codes(a.codes + (int64_t)row * a.codes_stride, c, a.dim, y, kMost8 / top, far);
     } else {
         store8<BF16, ALIGNED>(at_row<BF16>(a.y, row, a.y_stride), c, a.dim, y, far, lane);
     }
+}
+
+__device__ __forceinline__ float root_of(float sum, const NormArgs& a) {
+    return __frsqrt_rn(__fadd_rn(__fdiv_rn(sum, (float)a.dim), a.eps));
 }
 
 // blockDim.y rows a CTA, of blockDim.x threads with VECTORS times eight values each.
@@ -99,32 +126,36 @@ __global__ void __launch_bounds__(kRowThreads8) norm_kernel(const __grid_constan
     const bool on = row < a.rows;
     pdl_wait();
     pdl_trigger();
-    SumVec<BF16, ALIGNED> v[VECTORS];
-    Vec8<BF16, ALIGNED> w[VECTORS];
-    float s = 0.0f;
+    Vec8<BF16, ALIGNED> vx[VECTORS], vr[VECTORS], w[VECTORS];
+    Held<BF16> v[VECTORS];
+    const int32_t dim = on ? a.dim : 0;
     const char* x = at_row<BF16>(a.x, row, a.x_stride);
     const char* r = a.residual ? at_row<BF16>(a.residual, row, a.residual_stride) : nullptr;
 #pragma unroll
-    for (int j = 0; j < VECTORS; ++j) v[j].load(x, r, (threadIdx.x + j * blockDim.x) * kN, on ? a.dim : 0);
+    for (int j = 0; j < VECTORS; ++j) {
+        const int32_t c = (threadIdx.x + j * blockDim.x) * kN;
+        vx[j].load(x, c, dim);
+        if (r) vr[j].load(r, c, dim);
+    }
 #pragma unroll
     for (int j = 0; j < VECTORS; ++j) w[j].load(a.weight, (threadIdx.x + j * blockDim.x) * kN, a.dim);
+    float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll
     for (int j = 0; j < VECTORS; ++j) {
         float h[kN];
-        v[j].get(h, r != nullptr);
-        v[j].x.keep();
-        if (r) v[j].r.keep();
-#pragma unroll
-        for (int e = 0; e < kN; ++e) s = __fmaf_rn(h[e], h[e], s);
+        v[j] = held(vx[j], vr[j], r != nullptr);
+        v[j].get(h);
+        v[j].keep();
+        square8(s, h);
     }
-    const float rstd = __frsqrt_rn(__fadd_rn(__fdiv_rn(row_sum(s, s_part), (float)a.dim), a.eps));
+    const float rstd = root_of(row_sum(s.x + s.y, s_part), a);
     if (!on) return;   // whole warps
     if (!CODES && a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
 #pragma unroll
     for (int j = 0; j < VECTORS; ++j) {
         const int32_t c = (threadIdx.x + j * blockDim.x) * kN;
         float h[kN];
-        v[j].get(h, r != nullptr);
+        v[j].get(h);
         if (a.sum) store8<BF16, ALIGNED>(at_row<BF16>(a.sum, row, a.sum_stride), c, a.dim, h, far, lane);
         put_norm<BF16, ALIGNED, CODES>(a, row, c, h, w[j], rstd, far, lane);
     }
@@ -141,18 +172,18 @@ __global__ void __launch_bounds__(kRowThreads8) norm_long_kernel(const __grid_co
     const char* x = at_row<BF16>(a.x, row, a.x_stride);
     const char* r = a.residual ? at_row<BF16>(a.residual, row, a.residual_stride) : nullptr;
     char* sum = a.sum ? at_row<BF16>(a.sum, row, a.sum_stride) : nullptr;
-    float s = 0.0f;
+    float2 s = make_float2(0.0f, 0.0f);
     for (int32_t j = 0; j < steps; ++j) {
         const int32_t c = (threadIdx.x + j * kRowThreads8) * kN;
-        SumVec<BF16, ALIGNED> v;
+        Vec8<BF16, ALIGNED> vx, vr;
         float h[kN];
-        v.load(x, r, c, a.dim);
-        v.get(h, r != nullptr);
+        vx.load(x, c, a.dim);
+        if (r) vr.load(r, c, a.dim);
+        held(vx, vr, r != nullptr).get(h);
         if (sum) store8<BF16, ALIGNED>(sum, c, a.dim, h, false, lane);
-#pragma unroll
-        for (int e = 0; e < kN; ++e) s = __fmaf_rn(h[e], h[e], s);
+        square8(s, h);
     }
-    const float rstd = __frsqrt_rn(__fadd_rn(__fdiv_rn(row_sum(s, s_part), (float)a.dim), a.eps));   // its barrier: the sum is written
+    const float rstd = root_of(row_sum(s.x + s.y, s_part), a);   // its barrier: the sum is written
     if (!CODES && a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
     for (int32_t j = 0; j < steps; ++j) {
         const int32_t c = (threadIdx.x + j * kRowThreads8) * kN;
@@ -241,6 +272,153 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const __grid_co
         }
     }
     if (strip >= strips) return;
+#pragma unroll
+    for (int j = 0; j < VECTORS; ++j) {
+        const int32_t c = (threadIdx.x + j * blockDim.x) * kN;
+        if (c >= pitch) continue;
+        float4* to = reinterpret_cast<float4*>(parts + (int64_t)strip * pitch + c);
+        to[0] = make_float4(dw[j][0], dw[j][1], dw[j][2], dw[j][3]);
+        to[1] = make_float4(dw[j][4], dw[j][5], dw[j][6], dw[j][7]);
+    }
+}
+
+// ---- bf16: the next rows on their way ---------------------------------------------
+// A thread's own vectors of the strip's next rows come to shared memory by asynchronous copies, and it alone reads them:
+// no barrier guards them, and what is on its way takes no registers (16384 x 4096: 99 us, 5.4 TB/s; without 123; 1024 wide
+// 40 and 46; 300 x 4096 7.2 and 8.0).  fp32 rows take twice the memory, which then holds one CTA an SM: 300 us, without
+// 191.
+constexpr int kAhead = 3;                 // rows in shared memory: one in use, the others on their way
+template <int VECTORS>
+constexpr int kStreamCtas = VECTORS == 1 ? 4 : VECTORS == 2 ? 3 : 2;   // of kGradThreads, of an SM, by their registers
+constexpr int kStreamBytes = 220 * 1024;  // of an SM
+
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
+// All but the last PENDING groups of this thread have come.
+template <int PENDING>
+__device__ __forceinline__ void copies_wait() {
+    asm volatile("cp.async.wait_group %0;\n" ::"n"(PENDING) : "memory");
+}
+
+// A thread's vectors of three rows (h, dy, dsum), kAhead times; neighbouring threads' lie side by side.
+template <int VECTORS>
+struct Ahead {
+    uint32_t base, threads;
+    __device__ __forceinline__ Ahead(const void* smem) {
+        threads = blockDim.x * blockDim.y;
+        base = (uint32_t)__cvta_generic_to_shared(smem) + (threadIdx.y * blockDim.x + threadIdx.x) * 16;
+    }
+    __device__ __forceinline__ uint32_t at(int slot, int array, int j) const {
+        return base + (uint32_t)((slot * 3 + array) * VECTORS + j) * threads * 16;
+    }
+    __device__ __forceinline__ void copy(int slot, int array, const char* row, int32_t dim) const {
+#pragma unroll
+        for (int j = 0; j < VECTORS; ++j) {
+            const int32_t c = (threadIdx.x + j * blockDim.x) * kN;
+            if (c < dim) copy16(at(slot, array, j), row + (int64_t)c * 2);
+        }
+    }
+    __device__ __forceinline__ Vec8<true, true> read(int slot, int array, int j, int32_t dim) const {
+        Vec8<true, true> v;
+        v.left = dim - (int32_t)(threadIdx.x + j * blockDim.x) * kN;
+        v.u = make_uint4(0u, 0u, 0u, 0u);
+        if (v.left > 0)
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n"
+                         : "=r"(v.u.x), "=r"(v.u.y), "=r"(v.u.z), "=r"(v.u.w)
+                         : "r"(at(slot, array, j))
+                         : "memory");
+        return v;
+    }
+};
+
+// A CTA's blockDim.y strips of rows.
+struct Strip {
+    int32_t row0, row1, most;   // most: rows of the longest strip, all take part in the barriers
+    __device__ __forceinline__ Strip(int32_t rows, int32_t strips) {
+        const int32_t i = blockIdx.x * blockDim.y + threadIdx.y;
+        row0 = i < strips ? (int32_t)((int64_t)rows * i / strips) : 0;
+        row1 = i < strips ? (int32_t)((int64_t)rows * (i + 1) / strips) : 0;
+        most = (rows + strips - 1) / strips;
+    }
+};
+
+template <int VECTORS>
+__global__ void __launch_bounds__(kGradThreads, kStreamCtas<VECTORS>) norm_grad_stream_kernel(const __grid_constant__ NormGradArgs a, float* parts,
+                                                                        const int32_t strips, const int32_t pitch, const bool far) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ float s_part[2][kCtaThreads / 32][kRowThreads8 / 32];
+    const int lane = threadIdx.x & 31;
+    const Strip t(a.rows, strips);
+    const Ahead<VECTORS> ahead(smem);
+    pdl_wait();
+    pdl_trigger();
+    const auto fetch = [&](int32_t i) {
+        const int32_t row = t.row0 + i;
+        if (row < t.row1) {
+            ahead.copy(i % kAhead, 0, at_row<true>(a.h, row, a.h_stride), a.dim);
+            ahead.copy(i % kAhead, 1, at_row<true>(a.dy, row, a.dy_stride), a.dim);
+            if (a.dsum) ahead.copy(i % kAhead, 2, at_row<true>(a.dsum, row, a.dsum_stride), a.dim);
+        }
+        copies_done();
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead - 1; ++i) fetch(i);
+    Vec8<true, true> w[VECTORS];
+    float dw[VECTORS][kN];
+#pragma unroll
+    for (int j = 0; j < VECTORS; ++j) {
+        w[j].load(a.weight, (threadIdx.x + j * blockDim.x) * kN, a.dim);
+#pragma unroll
+        for (int e = 0; e < kN; ++e) dw[j][e] = 0.0f;
+    }
+    float next = t.row0 < t.row1 ? a.rstd[t.row0] : 0.0f;
+    for (int32_t i = 0; i < t.most; ++i) {
+        const int32_t row = t.row0 + i;
+        const bool on = row < t.row1;
+        const float rstd = next;
+        if (row + 1 < t.row1) next = a.rstd[row + 1];
+        fetch(i + kAhead - 1);   // where row i - 1 was
+        copies_wait<kAhead - 1>();
+        const int slot = i % kAhead;
+        float s = 0.0f;
+        if (on) {
+#pragma unroll
+            for (int j = 0; j < VECTORS; ++j) {
+                float h[kN], g[kN], u[kN];
+                ahead.read(slot, 0, j, a.dim).get(h);
+                ahead.read(slot, 1, j, a.dim).get(g);
+                w[j].keep();
+                w[j].get(u);
+#pragma unroll
+                for (int e = 0; e < kN; ++e) {
+                    dw[j][e] = __fmaf_rn(g[e], __fmul_rn(h[e], rstd), dw[j][e]);
+                    s = __fmaf_rn(__fmul_rn(g[e], u[e]), h[e], s);
+                }
+            }
+        }
+        const float c1 = __fmul_rn(__fmul_rn(__fdiv_rn(row_sum(s, s_part[i & 1]), (float)a.dim), rstd), rstd);
+        if (!on) continue;
+#pragma unroll
+        for (int j = 0; j < VECTORS; ++j) {
+            float h[kN], g[kN], u[kN];
+            ahead.read(slot, 0, j, a.dim).get(h);
+            ahead.read(slot, 1, j, a.dim).get(g);
+            w[j].keep();
+            w[j].get(u);
+#pragma unroll
+            for (int e = 0; e < kN; ++e) g[e] = __fmul_rn(rstd, __fmaf_rn(-h[e], c1, __fmul_rn(g[e], u[e])));
+            if (a.dsum) {
+                ahead.read(slot, 2, j, a.dim).get(h);
+#pragma unroll
+                for (int e = 0; e < kN; ++e) g[e] = __fadd_rn(g[e], h[e]);
+            }
+            store8<true, true>(at_row<true>(a.dx, row, a.dx_stride), (threadIdx.x + j * blockDim.x) * kN, a.dim, g, far, lane);
+        }
+    }
+    if (t.row0 >= t.row1) return;
+    const int32_t strip = blockIdx.x * blockDim.y + threadIdx.y;
 #pragma unroll
     for (int j = 0; j < VECTORS; ++j) {
         const int32_t c = (threadIdx.x + j * blockDim.x) * kN;
@@ -360,7 +538,7 @@ bool on16(const void* p, int64_t stride, int dtype) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * (dtype == DOMINO_DTYPE_BF16 ? 2 : 4) % 16 == 0;
 }
 
-// Threads of a row and what each holds.  One vector a thread where the row's 512 can hold it: 32 rows of 4096, a latency.
+// Threads of a row and the vectors that each holds.
 struct Cut {
     int threads, vectors, rows;   // rows of a CTA
 };
@@ -378,7 +556,9 @@ cudaError_t launch_norm_t(const NormArgs& a, cudaStream_t st) {
     const bool far = (int64_t)a.rows * a.dim * (CODES ? 1 : BF16 ? 2 : 4) >= kFarOut;
     if (a.dim > kLongRow)
         return launch_pdl(norm_long_kernel<BF16, ALIGNED, CODES>, dim3((unsigned)a.rows), dim3(kRowThreads8), 0, st, a, far);
-    const Cut c = cut_row(a.dim, kRowThreads8);
+    // 256 threads a row where they can hold it: a CTA's row waits at one barrier, and smaller CTAs wait less (16384 x 4096
+    // bf16: norm 78 us, in codes 77; with 512 threads 102 and 102)
+    const Cut c = cut_row(a.dim, a.dim <= 256 * kMaxVectors * kN ? 256 : kRowThreads8);
     const dim3 grid((unsigned)ceil_div(a.rows, c.rows)), block((unsigned)c.threads, (unsigned)c.rows);
     switch (c.vectors) {
         case 1: return launch_pdl(norm_kernel<BF16, ALIGNED, CODES, 1>, grid, block, 0, st, a, far);
@@ -397,14 +577,42 @@ struct GradCut {
     Cut cut;
     int32_t strips, pitch;
     size_t sums;          // bytes of the rows' sums (long rows)
+    int stream;           // bytes of a CTA of the kernel that fetches ahead; 0: the other
 };
+bool grad_aligned(const NormGradArgs& a) {
+    return on16(a.h, a.h_stride, a.dtype) && on16(a.dy, a.dy_stride, a.dtype) && on16(a.dx, a.dx_stride, a.dtype) &&
+           on16(a.weight, 0, a.dtype) && (!a.dsum || on16(a.dsum, a.dsum_stride, a.dtype));
+}
 GradCut cut_grad(const NormGradArgs& a, const LaunchEnv& env) {
-    GradCut g{cut_row(a.dim, kGradThreads), 0, ceil_div(a.dim, kN) * kN, 0};
+    GradCut g{cut_row(a.dim, kGradThreads), 0, ceil_div(a.dim, kN) * kN, 0, 0};
     const bool lng = a.dim > kGradLongRow;
     if (lng) g.sums = ((size_t)a.rows * 4 + 255) / 256 * 256;
+    if (!lng && a.dtype == DOMINO_DTYPE_BF16 && grad_aligned(a)) {
+        const int ctas = g.cut.vectors == 1 ? kStreamCtas<1> : g.cut.vectors == 2 ? kStreamCtas<2> : kStreamCtas<4>;
+        const int threads = g.cut.threads * g.cut.rows;
+        g.stream = kAhead * 3 * g.cut.vectors * threads * 16;
+        const int per_sm = std::max(1, std::min(kStreamBytes / g.stream, ctas * kGradThreads / threads));
+        g.strips = (int32_t)std::min<int64_t>(a.rows, (int64_t)per_sm * env.num_sms * g.cut.rows);
+        return g;
+    }
     const int64_t per_sm = lng ? ceil_div(kStripsPerSm * 8, ceil_div(a.dim, kGradThreads * kN)) : g.cut.rows > 1 ? kShortStripsPerSm : kStripsPerSm;
     g.strips = (int32_t)std::max<int64_t>(1, std::min<int64_t>(a.rows, lng ? per_sm * env.num_sms / 8 : per_sm * env.num_sms));
     return g;
+}
+
+template <int VECTORS>
+cudaError_t launch_grad_stream(const NormGradArgs& a, const GradCut& g, float* parts, bool far, cudaStream_t st) {
+    static std::atomic<bool> ready[64];   // more than 48 KB of shared memory: raised once per device
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !ready[dev].load()) {
+        e = cudaFuncSetAttribute(norm_grad_stream_kernel<VECTORS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamBytes);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) ready[dev].store(true);
+    }
+    return launch_pdl(norm_grad_stream_kernel<VECTORS>, dim3((unsigned)ceil_div(g.strips, g.cut.rows)),
+                      dim3((unsigned)g.cut.threads, (unsigned)g.cut.rows), (size_t)g.stream, st, a, parts, g.strips, g.pitch, far);
 }
 
 template <bool BF16, bool ALIGNED>
@@ -419,6 +627,12 @@ cudaError_t launch_grad_t(const NormGradArgs& a, const LaunchEnv& env, void* spa
         if (e != cudaSuccess) return e;
         e = launch_pdl(norm_grad_long_kernel<BF16, ALIGNED>, dim3((unsigned)ceil_div(a.dim, kGradThreads * kN), (unsigned)g.strips),
                        dim3(kGradThreads), 0, st, a, (const float*)sums, parts, g.strips, g.pitch, far);
+    } else if (g.stream) {
+        switch (g.cut.vectors) {
+            case 1: e = launch_grad_stream<1>(a, g, parts, far, st); break;
+            case 2: e = launch_grad_stream<2>(a, g, parts, far, st); break;
+            default: e = launch_grad_stream<4>(a, g, parts, far, st);
+        }
     } else {
         const dim3 grid((unsigned)ceil_div(g.strips, g.cut.rows)), block((unsigned)g.cut.threads, (unsigned)g.cut.rows);
         switch (g.cut.vectors) {
@@ -449,9 +663,7 @@ size_t norm_grad_workspace(const NormGradArgs& a, const LaunchEnv& env) {
 }
 
 cudaError_t launch_norm_grad(const NormGradArgs& a, const LaunchEnv& env, void* space, cudaStream_t st) {
-    bool aligned = on16(a.h, a.h_stride, a.dtype) && on16(a.dy, a.dy_stride, a.dtype) && on16(a.dx, a.dx_stride, a.dtype) &&
-                   on16(a.weight, 0, a.dtype);
-    if (a.dsum) aligned = aligned && on16(a.dsum, a.dsum_stride, a.dtype);
+    const bool aligned = grad_aligned(a);
     if (a.dtype == DOMINO_DTYPE_BF16) return aligned ? launch_grad_t<true, true>(a, env, space, st) : launch_grad_t<true, false>(a, env, space, st);
     return aligned ? launch_grad_t<false, true>(a, env, space, st) : launch_grad_t<false, false>(a, env, space, st);
 }

@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(kThreads8) rows_kernel(const __grid_constant__
         v[j].get(f);
         const float top = fmaxf(block_largest(largest(f)), kLeast8);
         if (c[j] >= a.dim) continue;
-        if (lane == 0) a.scales[(int64_t)row[j] * blocks + c[j] / kBlock8] = top / kMost8;
+        if (lane == 0) a.scales[(int64_t)row[j] * blocks + c[j] / kBlock8] = scale_of(top);
         store_codes(a.codes + row[j] * a.codes_stride, c[j], a.dim, f, kMost8 / top, far);
     }
 }
@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(kThreads8) tiles_kernel(const __grid_constant_
 #pragma unroll
     for (int w = 0; w < kThreads8 / 32; ++w) top = fmaxf(top, s_top[w]);
     top = fmaxf(top, kLeast8);
-    if (threadIdx.x == 0) a.scales[(int64_t)tile * blocks + block] = top / kMost8;
+    if (threadIdx.x == 0) a.scales[(int64_t)tile * blocks + block] = scale_of(top);
     const float by = kMost8 / top;
 #pragma unroll
     for (int j = 0; j < kPerHalf; ++j) {

@@ -3,6 +3,7 @@
 //
 //   a = max |v| over the block, at least 2^-100;  scale = a / 448;  code = e4m3(v (448 / a))
 //
+// The scale is a times the rounded 1 / 448 (two roundings: a second division would be a tenth of a norm's instructions).
 // 448 is the largest e4m3 value: the block's largest value takes it, and nothing
 // overflows.  Sixteen lanes of eight values make a block of a row.
 #pragma once
@@ -16,6 +17,46 @@ constexpr int kBlock8 = 128;              // values that share a scale, along a 
 constexpr int kBlockLanes = kBlock8 / kN;
 constexpr float kMost8 = 448.0f, kLeast8 = 0x1p-100f;
 
+// Two values an instruction, each rounded once as one by one.
+__device__ __forceinline__ unsigned long long pair_of(float a, float b) {
+    unsigned long long x;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a), "f"(b));
+    return x;
+}
+__device__ __forceinline__ void from_pair(float& a, float& b, unsigned long long x) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x));
+}
+__device__ __forceinline__ void add8(float (&f)[kN], const float (&g)[kN]) {
+#pragma unroll
+    for (int e = 0; e < kN; e += 2) {
+        unsigned long long r;
+        asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair_of(f[e], f[e + 1])), "l"(pair_of(g[e], g[e + 1])));
+        from_pair(f[e], f[e + 1], r);
+    }
+}
+__device__ __forceinline__ void mul8(float (&f)[kN], const float (&g)[kN]) {
+#pragma unroll
+    for (int e = 0; e < kN; e += 2) {
+        unsigned long long r;
+        asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair_of(f[e], f[e + 1])), "l"(pair_of(g[e], g[e + 1])));
+        from_pair(f[e], f[e + 1], r);
+    }
+}
+__device__ __forceinline__ void mul8(float (&f)[kN], float by) {
+    const float g[kN] = {by, by, by, by, by, by, by, by};
+    mul8(f, g);
+}
+// The squares, added to the sums of the even and the odd ones.
+__device__ __forceinline__ void square8(float2& s, const float (&f)[kN]) {
+#pragma unroll
+    for (int e = 0; e < kN; e += 2) {
+        unsigned long long r;
+        const unsigned long long x = pair_of(f[e], f[e + 1]);
+        asm("fma.rn.f32x2 %0, %1, %1, %2;" : "=l"(r) : "l"(x), "l"(pair_of(s.x, s.y)));
+        from_pair(s.x, s.y, r);
+    }
+}
+
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
@@ -23,8 +64,9 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 
 // Values c, .. c + 7 of a row of dim; zeros beyond its end.  ALIGNED: the row begins on a 16-byte boundary.  load() reads
 // and uses nothing of what it reads, so that a thread's loads are on their way together, and get() converts (128256 x 4096
-// bf16 in codes: MEASURED).  After keep() a get() converts again: what is kept meanwhile are the bits, not fp32 values.  Rows are read in the 16-byte blocks that hold their values.  Neither __ldg nor another
-// assumption that the row is not written by this kernel: outputs may take inputs' places.
+// bf16 in codes: 259 us, converted as they come 689).  After keep() a get() converts again: what is kept meanwhile are the
+// bits, not fp32 values.  Rows are read in the 16-byte blocks that hold their values.  Neither __ldg nor another assumption
+// that the row is not written by this kernel: outputs may take inputs' places.
 template <bool BF16, bool ALIGNED>
 struct Vec8;
 template <>
@@ -139,6 +181,8 @@ __device__ __forceinline__ void store8(void* row, int32_t c, int32_t dim, const 
     }
 }
 
+__device__ __forceinline__ float scale_of(float top) { return top * (1.0f / kMost8); }
+
 __device__ __forceinline__ float largest(const float (&f)[kN]) {
     float a = 0.0f;
 #pragma unroll
@@ -161,8 +205,10 @@ __device__ __forceinline__ uint32_t two_codes(float lo, float hi) {
 // Eight codes at column c of a row of codes that begins on a 16-byte boundary, by = 448 / the block's largest; nothing at
 // or beyond dim is written.
 __device__ __forceinline__ void store_codes(uint8_t* row, int32_t c, int32_t dim, const float (&f)[kN], float by, bool far) {
-    const uint32_t lo = two_codes(f[0] * by, f[1] * by) | (two_codes(f[2] * by, f[3] * by) << 16);
-    const uint32_t hi = two_codes(f[4] * by, f[5] * by) | (two_codes(f[6] * by, f[7] * by) << 16);
+    float v[kN] = {f[0], f[1], f[2], f[3], f[4], f[5], f[6], f[7]};
+    mul8(v, by);
+    const uint32_t lo = two_codes(v[0], v[1]) | (two_codes(v[2], v[3]) << 16);
+    const uint32_t hi = two_codes(v[4], v[5]) | (two_codes(v[6], v[7]) << 16);
     uint8_t* p = row + c;
     if (c + kN <= dim) {
         if (far) __stcs(reinterpret_cast<uint2*>(p), make_uint2(lo, hi));
