@@ -11,6 +11,12 @@
 // decodes the rest as decode.cuh does, bound by HBM; the marked ones, numbered by the
 // set bits before them, get a counter each, then their logit, and are folded on their
 // own.  Whole-number atomics only: the results are the same on every run.
+//
+// 256 x 128256 bf16, a third of the rows dense, histories of up to 4096 tokens: 28 us (the
+// decode alone 24; the bytes' floor is 10.6): two of the 256 rows on
+// most SMs, and a row's fold waits for its loads and for its own results (the SMs issue in a
+// quarter of cycles).  More CTAs a row cost more than they share out: 32 us with two, 52 with
+// four.  One row: a chain of five latencies of memory and ten barriers, 7.9 us.
 #include <algorithm>
 #include <atomic>
 
@@ -20,11 +26,14 @@
 namespace domino {
 namespace {
 
-constexpr int kSegmentWords = 2048;        // of a row at a time, at most: a place in it fits 16 bits
-constexpr int kWordsEach = kSegmentWords / kDecodeThreads;
+// Mask words of a row at a time, at most: 131072 tokens, the usual vocabularies whole (128 x 152064 with log-probabilities in
+// two parts a CTA 54 us, in one 35).
+constexpr int kSegmentWords = 4096;
 constexpr int kBiasEach = kMaxBias / kDecodeThreads;
 constexpr int kPenalizedSmem = 100 * 1024; // of a CTA, at most: two an SM
-static_assert(kWordsEach == 4 && kBiasEach * kDecodeThreads == kMaxBias);
+constexpr int kQuads = kSegmentWords / 4 / kDecodeThreads;   // four mask words each, of a thread
+constexpr int kHeld = 8;                   // history tokens a thread keeps, of each 512
+static_assert(kQuads == 2 && kBiasEach * kDecodeThreads == kMaxBias);
 
 struct Rows {
     const void* logits;
@@ -51,13 +60,15 @@ __host__ __device__ inline Layout layout(int segment, int places) {
     l.mask = 16;
     l.changed = l.mask + segment * 4 + 16;
     l.before = l.changed + segment * 4;
-    l.value = l.before + segment * 2;      // segment: a multiple of 4, places of 8
-    l.value = (l.value + 15) & ~15;
+    l.value = (l.before + segment * 2 + 15) & ~15;   // segment: a multiple of 4, places of 8
     l.place = l.value + places * 4;
-    l.list = l.place + places * 2;
+    l.list = l.place + places * 4;
     l.end = l.list + kDecodeListBytes;
     return l;
 }
+
+constexpr int kManyTokens = 32;            // of 128
+__device__ __forceinline__ void fetch_l2(const char* p) { asm volatile("prefetch.global.L2 [%0];\n" ::"l"(p)); }
 
 // A segment of a row: mask words w0, .. w0 + n - 1.
 struct Segment {
@@ -65,14 +76,14 @@ struct Segment {
     uint32_t* changed;
     uint16_t* before;
     uint32_t* value;
-    uint16_t* place;
+    uint32_t* place;               // from the segment's first token on
     int w0, n;
     int total;                     // changed tokens that are allowed
 
     // The number of token t, or -1: not in this segment, not changed or not allowed.
     __device__ __forceinline__ int number(int32_t t) const {
-        const uint32_t j = (uint32_t)(t >> 5) - (uint32_t)w0;   // below 0: a large one
-        if (j >= (uint32_t)n) return -1;
+        const uint32_t j = (uint32_t)(t >> 5) - (uint32_t)w0;
+        if (t < 0 || j >= (uint32_t)n) return -1;
         const uint32_t word = changed[j], bit = 1u << (t & 31);
         return word & bit ? before[j] + __popc(word & (bit - 1u)) : -1;
     }
@@ -91,64 +102,106 @@ struct Segment {
 // nothing reads any more; it ends with a barrier.  report: the first time for a row.
 template <bool BF16>
 __device__ __forceinline__ void make_segment(Segment& g, const Rows& a, int r, int len, const char* lrow, uint32_t* report, int tid) {
-    __shared__ int s_sum[kDecodeWarps];
+    __shared__ int s_sum[kQuads][kDecodeWarps];
     const int lane = tid & 31, warp = tid >> 5;
     const uint32_t* mrow = a.mask ? a.mask + (int64_t)r * a.W + g.w0 : nullptr;
     const int32_t* hist = a.p.history_dev + (int64_t)r * a.p.history_len;
     const int32_t* ids = a.p.bias_ids_dev + (int64_t)r * a.p.n_bias;
     const int n_bias = a.p.n_bias;
-    for (int j = tid; j < g.n; j += kDecodeThreads) {
-        g.mask[j] = mrow ? __ldg(mrow + j) : 0xFFFFFFFFu;
-        g.changed[j] = 0u;
-    }
-    if (tid == 0) g.mask[-1] = g.mask[g.n] = 0u;
-    __syncthreads();
-    for (int i = tid; i < len; i += kDecodeThreads) g.mark(__ldg(hist + i), a.V, report);
-    for (int i = tid; i < n_bias; i += kDecodeThreads) g.mark(__ldg(ids + i), a.V, report);
-    __syncthreads();
-    // allowed and changed, allowed and not; numbers
-    uint32_t m[kWordsEach], c[kWordsEach];
-    int count = 0;
+    // the first tokens of the history and the ids are on their way beside the masks, and stay for the second pass
+    int32_t held[kHeld], id[kBiasEach];
 #pragma unroll
-    for (int k = 0; k < kWordsEach; ++k) {
-        const int j = tid * kWordsEach + k;
-        m[k] = c[k] = 0u;
-        if (j < g.n) {
-            const int left = a.V - 32 * (g.w0 + j);
-            m[k] = g.mask[j];
-            if (left < 32) m[k] &= (1u << left) - 1u;
-            c[k] = m[k] & g.changed[j];
-            m[k] &= ~c[k];
+    for (int k = 0; k < kHeld; ++k) {
+        const int i = tid + k * kDecodeThreads;
+        held[k] = i < len ? __ldg(hist + i) : -1;
+    }
+#pragma unroll
+    for (int k = 0; k < kBiasEach; ++k) {
+        const int i = tid + k * kDecodeThreads;
+        id[k] = i < n_bias ? __ldg(ids + i) : -1;
+    }
+    uint4 m4[kQuads];
+    const bool quads = mrow && (reinterpret_cast<uintptr_t>(mrow) & 15) == 0 && (g.n & 3) == 0;
+    const int rounds = (g.n + 4 * kDecodeThreads - 1) / (4 * kDecodeThreads);
+#pragma unroll
+    for (int k = 0; k < kQuads; ++k) {
+        const int j = (tid + k * kDecodeThreads) * 4;
+        m4[k] = make_uint4(0u, 0u, 0u, 0u);
+        if (j >= g.n) continue;
+        if (quads) {
+            m4[k] = __ldg(reinterpret_cast<const uint4*>(mrow + j));
+        } else {
+            m4[k].x = mrow ? __ldg(mrow + j) : 0xFFFFFFFFu;
+            if (j + 1 < g.n) m4[k].y = mrow ? __ldg(mrow + j + 1) : 0xFFFFFFFFu;
+            if (j + 2 < g.n) m4[k].z = mrow ? __ldg(mrow + j + 2) : 0xFFFFFFFFu;
+            if (j + 3 < g.n) m4[k].w = mrow ? __ldg(mrow + j + 3) : 0xFFFFFFFFu;
         }
-        count += __popc(c[k]);
     }
-    int upto = count;
 #pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, upto, off);
-        if (lane >= off) upto += y;
+    for (int k = 0; k < kQuads; ++k) {
+        const int j = (tid + k * kDecodeThreads) * 4, left = a.V - 32 * (g.w0 + j);   // of the row
+        if (j >= g.n) continue;
+        // many allowed tokens: their logits are fetched to L2 meanwhile
+        if (__popc(m4[k].x) + __popc(m4[k].y) + __popc(m4[k].z) + __popc(m4[k].w) >= kManyTokens && left >= 128) {
+            const char* at = lrow + (int64_t)(g.w0 + j) * (BF16 ? 64 : 128);
+#pragma unroll
+            for (int e = 0; e < (BF16 ? 2 : 4); ++e) fetch_l2(at + 128 * e);
+        }
+        if (left < 128) {   // the row's last words: no bits beyond it
+            m4[k].x &= left < 32 ? (1u << left) - 1u : 0xFFFFFFFFu;
+            m4[k].y &= left < 64 ? left < 32 ? 0u : (1u << (left - 32)) - 1u : 0xFFFFFFFFu;
+            m4[k].z &= left < 96 ? left < 64 ? 0u : (1u << (left - 64)) - 1u : 0xFFFFFFFFu;
+            m4[k].w &= left < 96 ? 0u : (1u << (left - 96)) - 1u;
+        }
+        reinterpret_cast<uint4*>(g.changed)[j / 4] = make_uint4(0u, 0u, 0u, 0u);
     }
-    if (lane == 31) s_sum[warp] = upto;
+    if (tid == 0) g.mask[-1] = 0u;
     __syncthreads();
-    int at = upto - count;
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) g.mark(held[k], a.V, report);
+    for (int i = tid + kHeld * kDecodeThreads; i < len; i += kDecodeThreads) g.mark(__ldg(hist + i), a.V, report);
+#pragma unroll
+    for (int k = 0; k < kBiasEach; ++k) g.mark(id[k], a.V, report);
+    __syncthreads();
+    // allowed and changed, allowed and not; numbers: of each round's words, by threads, by warps
     g.total = 0;
-#pragma unroll
-    for (int w = 0; w < kDecodeWarps; ++w) {
-        if (w < warp) at += s_sum[w];
-        g.total += s_sum[w];
-    }
-#pragma unroll
-    for (int k = 0; k < kWordsEach; ++k) {
-        const int j = tid * kWordsEach + k;
-        if (j >= g.n) break;
-        g.mask[j] = m[k];
-        g.changed[j] = c[k];
-        g.before[j] = (uint16_t)at;
-        for (uint32_t w = c[k]; w; w &= w - 1) {
-            g.place[at] = (uint16_t)(32 * j + __ffs((int)w) - 1);
-            g.value[at++] = n_bias ? 0xFFFFFFFFu : 0u;
+    for (int k = 0; k < rounds; ++k) {
+        const int j = (tid + k * kDecodeThreads) * 4;
+        uint4 c = make_uint4(0u, 0u, 0u, 0u), m = k == 0 ? m4[0] : m4[kQuads - 1];
+        if (j < g.n) {
+            c = reinterpret_cast<const uint4*>(g.changed)[j / 4];
+            c = make_uint4(c.x & m.x, c.y & m.y, c.z & m.z, c.w & m.w);
+            reinterpret_cast<uint4*>(g.changed)[j / 4] = c;
+            reinterpret_cast<uint4*>(g.mask)[j / 4] = make_uint4(m.x & ~c.x, m.y & ~c.y, m.z & ~c.z, m.w & ~c.w);
         }
+        const int n0 = __popc(c.x), n1 = n0 + __popc(c.y), n2 = n1 + __popc(c.z), count = n2 + __popc(c.w);
+        int upto = count;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, upto, off);
+            if (lane >= off) upto += y;
+        }
+        if (lane == 31) s_sum[k][warp] = upto;
+        __syncthreads();
+        int at = upto - count + g.total;
+#pragma unroll
+        for (int w = 0; w < kDecodeWarps; ++w) {
+            if (w < warp) at += s_sum[k][w];
+            g.total += s_sum[k][w];
+        }
+        if (j < g.n)
+            reinterpret_cast<uint2*>(g.before)[j / 4] =
+                make_uint2((uint32_t)at | ((uint32_t)(at + n0) << 16), (uint32_t)(at + n1) | ((uint32_t)(at + n2) << 16));
     }
+    if (tid == 0) g.mask[g.n] = 0u;
+    __syncthreads();
+    // the places, a word a thread: neighbouring words, full where their tokens are frequent ones, are different threads'
+    for (int j = tid; j < g.n; j += kDecodeThreads) {
+        uint32_t w = g.changed[j];
+        if (w)
+            for (int i = g.before[j]; w; w &= w - 1) g.place[i++] = 32u * j + __ffs((int)w) - 1;
+    }
+    for (int k = tid; k < g.total; k += kDecodeThreads) g.value[k] = n_bias ? 0xFFFFFFFFu : 0u;
     __syncthreads();
     if (g.total == 0) return;
     // of equal ids the first: the lowest index at each place
@@ -158,9 +211,8 @@ __device__ __forceinline__ void make_segment(Segment& g, const Rows& a, int r, i
     if (n_bias) {
 #pragma unroll
         for (int k = 0; k < kBiasEach; ++k) {
-            const int i = tid + k * kDecodeThreads;
-            if (i < n_bias) mine[k] = g.number(__ldg(ids + i));
-            if (mine[k] >= 0) atomicMin(g.value + mine[k], (uint32_t)i);
+            mine[k] = g.number(id[k]);
+            if (mine[k] >= 0) atomicMin(g.value + mine[k], (uint32_t)(tid + k * kDecodeThreads));
         }
         __syncthreads();
 #pragma unroll
@@ -172,12 +224,15 @@ __device__ __forceinline__ void make_segment(Segment& g, const Rows& a, int r, i
     }
     // times beyond the prompt; the highest bit: in the prompt
     const int prompt = a.p.prompt_lengths_dev ? __ldg(a.p.prompt_lengths_dev + r) : 0;
-    for (int i = tid; i < len; i += kDecodeThreads) {
-        const int k = g.number(__ldg(hist + i));
-        if (k < 0) continue;
+    const auto count_one = [&](int i, int32_t t) {
+        const int k = g.number(t);
+        if (k < 0) return;
         if (i < prompt) atomicOr(g.value + k, 0x80000000u);
         else atomicAdd(g.value + k, 1u);
-    }
+    };
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) count_one(tid + k * kDecodeThreads, held[k]);
+    for (int i = tid + kHeld * kDecodeThreads; i < len; i += kDecodeThreads) count_one(i, __ldg(hist + i));
     __syncthreads();
     const float rep = a.p.repetition_dev ? __ldg(a.p.repetition_dev + r) : 1.0f;
     const float pres = a.p.presence_dev ? __ldg(a.p.presence_dev + r) : 0.0f;
@@ -212,7 +267,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) penalized_kernel(const __gr
     g.changed = reinterpret_cast<uint32_t*>(smem + l.changed);
     g.before = reinterpret_cast<uint16_t*>(smem + l.before);
     g.value = reinterpret_cast<uint32_t*>(smem + l.value);
-    g.place = reinterpret_cast<uint16_t*>(smem + l.place);
+    g.place = reinterpret_cast<uint32_t*>(smem + l.place);
     uint16_t* list = reinterpret_cast<uint16_t*>(smem + l.list) + warp * kDecodeList;
     const int r = blockIdx.x / a.slices, slice = blockIdx.x - r * a.slices;
     if (BF16 && FOLD != kFoldSample) fill_keep(s_keep, tid);
