@@ -12,11 +12,11 @@
 // set bits before them, get a counter each, then their logit, and are folded on their
 // own.  Whole-number atomics only: the results are the same on every run.
 //
-// 256 x 128256 bf16, a third of the rows dense, histories of up to 4096 tokens: 28 us (the
-// decode alone 24; the bytes' floor is 10.6): two of the 256 rows on
-// most SMs, and a row's fold waits for its loads and for its own results (the SMs issue in a
-// quarter of cycles).  More CTAs a row cost more than they share out: 32 us with two, 52 with
-// four.  One row: a chain of five latencies of memory and ten barriers, 7.9 us.
+// 256 x 128256 bf16, a third of the rows dense, histories of up to 4096 tokens: 28 us, of which
+// the decode alone takes 24 (the bytes' floor is 10.6): most SMs have two of the 256 rows, and a
+// row's fold waits for its loads and for its own results (the SMs issue in a quarter of the
+// cycles).  More CTAs a row cost more than they share out: 32 us with two, 52 with four.  One
+// row is a chain of five latencies of memory and ten barriers: 7.9 us.
 #include <algorithm>
 #include <atomic>
 
