@@ -520,7 +520,7 @@ int domino_norm8(domino_t h, const void* x_dev, int64_t x_stride, const void* re
  *   g = weight dy,  dx = rstd (g - h rstd^2 mean(g h)) + dsum   (of x and of the residual),
  *   dweight = the sum over the rows of dy h rstd,
  * all of dtype, rounded once.  dx_dev may be dsum_dev or dy_dev, with the same
- * stride.  Takes scratch: up to 16 times as many fp32 rows of dim as the GPU has SMs. */
+ * stride.  Takes scratch: up to 32 fp32 rows of dim for each SM. */
 int domino_norm_grad(domino_t h, const void* sum_dev, int64_t sum_stride, const void* weight_dev, const float* rstd_dev,
                      const void* dy_dev, int64_t dy_stride, const void* dsum_dev, int64_t dsum_stride, int32_t dtype,
                      int32_t rows, int32_t dim, void* dx_dev, int64_t dx_stride, void* dweight_dev, void* stream);

@@ -46,6 +46,32 @@ __device__ __forceinline__ void mul8(float (&f)[kN], float by) {
     const float g[kN] = {by, by, by, by, by, by, by, by};
     mul8(f, g);
 }
+// a b + c
+__device__ __forceinline__ void fma8(float (&r)[kN], const float (&a)[kN], const float (&b)[kN], const float (&c)[kN]) {
+#pragma unroll
+    for (int e = 0; e < kN; e += 2) {
+        unsigned long long x;
+        asm("fma.rn.f32x2 %0, %1, %2, %3;"
+            : "=l"(x)
+            : "l"(pair_of(a[e], a[e + 1])), "l"(pair_of(b[e], b[e + 1])), "l"(pair_of(c[e], c[e + 1])));
+        from_pair(r[e], r[e + 1], x);
+    }
+}
+__device__ __forceinline__ void fma8(float (&r)[kN], const float (&a)[kN], float b, const float (&c)[kN]) {
+    const float g[kN] = {b, b, b, b, b, b, b, b};
+    fma8(r, a, g, c);
+}
+// The products, added to the sums of the even and the odd ones.
+__device__ __forceinline__ void dot8(float2& s, const float (&f)[kN], const float (&g)[kN]) {
+#pragma unroll
+    for (int e = 0; e < kN; e += 2) {
+        unsigned long long r;
+        asm("fma.rn.f32x2 %0, %1, %2, %3;"
+            : "=l"(r)
+            : "l"(pair_of(f[e], f[e + 1])), "l"(pair_of(g[e], g[e + 1])), "l"(pair_of(s.x, s.y)));
+        from_pair(s.x, s.y, r);
+    }
+}
 // The squares, added to the sums of the even and the odd ones.
 __device__ __forceinline__ void square8(float2& s, const float (&f)[kN]) {
 #pragma unroll
