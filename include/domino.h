@@ -503,7 +503,8 @@ int domino_embed_grad(domino_t h, const int32_t* tokens_dev, int32_t n, const vo
  * x_dev, residual_dev (NULL: none), sum_dev (required with a residual, NULL else), y_dev
  * [rows][stride], weight_dev [dim], all of dtype (fp32 or bf16); rstd_dev float [rows] or
  * NULL.  sum_dev may be residual_dev or x_dev, with the same stride.  eps >= 0 and
- * finite; a row of zeros with eps = 0 has no norm (NaN).  Needs no scratch. */
+ * finite; a row of zeros with eps = 0 has no norm (NaN), nor has one whose sum of squares
+ * is beyond fp32.  Needs no scratch. */
 int domino_norm(domino_t h, const void* x_dev, int64_t x_stride, const void* residual_dev, int64_t residual_stride,
                 const void* weight_dev, int32_t dtype, int32_t rows, int32_t dim, float eps, void* y_dev,
                 int64_t y_stride, void* sum_dev, int64_t sum_stride, float* rstd_dev, void* stream);
@@ -553,7 +554,7 @@ typedef struct {
     const float* frequency_dev;        /* [batch]; NULL: 0 */
     const int32_t* bias_ids_dev;       /* [batch][n_bias]; below 0: none; of equal ids the first counts */
     const float* bias_values_dev;      /* [batch][n_bias], finite or -inf */
-    int32_t history_len;               /* >= 0 */
+    int32_t history_len;               /* 0 .. 2^30 (above: DOMINO_E_UNSUPPORTED) */
     int32_t n_bias;                    /* 0 .. 1024 */
 } domino_penalties;
 

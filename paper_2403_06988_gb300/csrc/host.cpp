@@ -2242,7 +2242,8 @@ int penalized_args(PenalizedArgs& a, domino_ctx* h, const void* logits, int32_t 
         !on_words(mask, p->history_dev, p->lengths_dev, p->prompt_lengths_dev) ||
         !on_words(p->repetition_dev, p->presence_dev, p->frequency_dev) || !on_words(p->bias_ids_dev, p->bias_values_dev))
         return DOMINO_E_INVALID_ARG;
-    if (batch > INT32_MAX / 8) return DOMINO_E_UNSUPPORTED;   // up to eight CTAs a row
+    // up to eight CTAs a row; places in a history are counted in 32 bits, a CTA's threads beyond the last
+    if (batch > INT32_MAX / 8 || p->history_len > (1 << 30)) return DOMINO_E_UNSUPPORTED;
     a = PenalizedArgs{};
     a.logits = logits;
     a.stride = stride;

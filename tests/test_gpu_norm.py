@@ -169,6 +169,21 @@ def test_small_and_large_values(d):
     assert (decode(q)[1] == 448).all() and decode(q)[3, 7] == -448
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_widest_rows(d, dtype):
+    T, D = 3, 1 << 20
+    x, r, w, dy, ds = inputs(T, D, dtype)
+    ref = Norm(x, w, r, dy=dy, dsum=ds)
+    y, h, rstd = d.norm(x, w, r)
+    assert torch.equal(h, ref.sum)
+    assert_within(y, ref.y, ref.tol["y"], "y")
+    q, scales, _ = d.norm8(x, w, r)
+    check_codes(q, scales, ref.y, ref.rel_y, 1, "norm8")
+    dx, dw = d.norm_grad(h, w, rstd, dy, ds)
+    assert_within(dx, ref.dx, ref.tol["dx"], "dx")
+    assert_within(dw, ref.dweight, ref.tol["dweight"], "dweight")
+
+
 def test_no_rows(d):
     x, r, w, dy, _ = inputs(3, 24, "bf16")
     y, h, rstd = d.norm(x[:0], w, r[:0])

@@ -165,6 +165,22 @@ def test_rows_apart(d, pad, dtype):  # noqa: F811
     c.check(d.mask_logits_penalized(c.logits, mask=c.mask, want_logprobs=True, **c.args))
 
 
+@pytest.mark.parametrize("batch,V", [(6, 700), (3, 50001), (200, 5000)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_ties_go_to_the_lowest_token(d, batch, V, dtype):  # noqa: F811
+    """Few different logits, and penalties that are whole: changed and other tokens tie at the top."""
+    c = Case(batch, V, 80, 9, dtype, seed=14, density=0.6)
+    c.logits = c.logits.float().round().clamp(-2, 1).to(c.logits.dtype)
+    c.host["repetition"][:], c.host["presence"][:], c.host["frequency"][:] = 1.0, 1.0, 0.0
+    c.host["presence"][::2] = 0.0
+    c.host["bias_values"] = np.sign(c.host["bias_values"]).astype(np.float32)
+    c.args = {n: None if v is None else torch.from_numpy(v).cuda() for n, v in c.host.items()}
+    c.x = c.penalise(c.logits.float().cpu().numpy())
+    c.check(d.mask_logits_penalized(c.logits, mask=c.mask, want_logprobs=True, **c.args))
+    arg, _, _ = d.mask_logits_penalized(c.logits, mask=c.mask, want_lse=False, **c.args)
+    assert (arg.cpu().numpy() == c.want()[2][0]).all()
+
+
 def test_of_equal_biases_the_first_counts(d):  # noqa: F811
     c = Case(4, 2000, 50, 700, "f32", seed=4, equal_bias=True, density=0.9)
     c.check(d.mask_logits_penalized(c.logits, mask=c.mask, want_logprobs=True, **c.args))
@@ -323,5 +339,8 @@ def test_refusals(d):  # noqa: F811
     with pytest.raises(DominoError) as e:
         B.domino_mask_logits_penalized(d.h, c.logits.data_ptr(), 0, 4, 500, 500, None, c.mask, arg)
     assert e.value.status == -1
+    with pytest.raises(DominoError) as e:
+        B.domino_mask_logits_penalized(d.h, c.logits.data_ptr(), 0, 4, 500, 500, B.penalties(c.args["history"], (1 << 30) + 1), c.mask, arg)
+    assert e.value.status == -3
     empty = d.mask_logits_penalized(c.logits[:0], c.args["history"][:0])
     assert empty[0].shape == (0,)

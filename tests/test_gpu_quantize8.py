@@ -46,6 +46,14 @@ def test_exact_codes(d):  # noqa: F811
     assert not q[1].float().any()
 
 
+@pytest.mark.parametrize("block", [1, 128])
+@pytest.mark.parametrize("size", [3e38, 1e30, 1e-25, 1e-36])
+def test_sizes_of_values(d, size, block):  # noqa: F811
+    """Up to the largest; blocks below 2^-100 keep its scale, and their codes get small."""
+    x = matrix(130, 260, "f32").clamp(-1, 1) * size
+    check_codes(*d.quantize8(x, block), x.double(), 0.0, block, "quantize8")
+
+
 def test_offsets_beyond_32_bits(d):  # noqa: F811
     R, D = 140000, 16384
     x = torch.zeros(R, D, dtype=torch.bfloat16, device="cuda")
