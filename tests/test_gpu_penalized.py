@@ -119,7 +119,7 @@ class Case:
 
 
 SIZES = [(1, 1, 0, 0), (1, 1, 3, 1), (1, 32000, 500, 16), (3, 50, 1, 3), (5, 1000, 63, 1), (4, 50001, 1023, 7), (24, 8000, 200, 300), (7, 128256, 4096, 64),
-         (160, 3001, 100, 5), (2, 70000, 9000, 1024), (3, 40, 300, 60), (310, 66000, 20, 2)]
+         (160, 3001, 100, 5), (2, 70000, 9000, 1024), (3, 40, 300, 60), (310, 66000, 20, 2), (153, 20011, 700, 30), (161, 31, 5, 2), (177, 129, 0, 0)]
 
 
 @pytest.mark.parametrize("batch,V,L,n_bias", SIZES)
