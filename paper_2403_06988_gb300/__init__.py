@@ -316,9 +316,9 @@ class Domino:
         """Root-mean-square norm of x + residual: (y, sum, rstd).  x, residual [rows, dim], weight [dim], y and sum of one
         type, bf16 or fp32; rstd fp32 [rows].  Without a residual sum is x itself.  out: (y, sum, rstd) to write to; its
         sum may be x or residual."""
-        import torch
         y, h, rstd = out if out is not None else (None, None, None)
         if self.fill_byte is not None:
+            import torch
             y = self._fill(y, *x.shape, x.dtype, x, stream)
             h = self._fill(h, *x.shape, x.dtype, x, stream) if residual is not None else h
             rstd = self._fill(rstd, x.shape[0], None, torch.float32, x, stream)
@@ -328,9 +328,9 @@ class Domino:
     def norm8(self, x, weight, residual=None, eps: float = 1e-6, out=None, stream=None) -> Tuple:
         """norm with y as logits8 takes it: (codes, scales, sum).  codes float8_e4m3fn [rows, dim], its rows on 16-byte
         boundaries; scales fp32 [rows, ceil(dim / 128)]."""
-        import torch
         q, sc, h = out if out is not None else (None, None, None)
         if self.fill_byte is not None:
+            import torch
             q = self._fill_codes(q, *x.shape, x, stream)
             sc = self._fill(sc, x.shape[0], -(-x.shape[1] // 128), torch.float32, x, stream)
             h = self._fill(h, *x.shape, x.dtype, x, stream) if residual is not None else h
@@ -350,9 +350,9 @@ class Domino:
     def quantize8(self, x, block: int = 1, out=None, stream=None) -> Tuple:
         """(codes, scales) of a matrix: a scale for each 1 x 128 values (block 1, hidden states) or 128 x 128 (block 128, a
         weight); see norm8."""
-        import torch
         q, sc = out if out is not None else (None, None)
         if self.fill_byte is not None:
+            import torch
             q = self._fill_codes(q, *x.shape, x, stream)
             sc = self._fill(sc, x.shape[0] if block == 1 else -(-x.shape[0] // 128), -(-x.shape[1] // 128), torch.float32, x, stream)
         return self._result("domino_quantize8", _calls().quantize8(
@@ -361,16 +361,13 @@ class Domino:
     def logits8(self, codes, scales, weight_codes, weight_scales, dtype=None, out=None, stream=None):
         """hidden @ weight.T of codes: [rows, n_tokens] in dtype (fp32 unless bf16 is asked for), rows on 16-byte boundaries.
         codes, scales: the hidden states', by norm8 or quantize8; weight_codes, weight_scales: by quantize8(weight, 128)."""
-        import torch
-        if dtype is None:
-            dtype = torch.float32 if out is None else out.dtype
-        if dtype not in (torch.float32, torch.bfloat16):
-            raise TypeError("dtype must be float32 or bfloat16")
         if out is None and self.fill_byte is not None:
-            n, per = weight_codes.shape[0], 16 // dtype.itemsize
-            out = self._empty((codes.shape[0], -(-n // per) * per), dtype, codes.device, stream)[:, :n]
+            import torch
+            made = torch.float32 if dtype is None else dtype
+            n, per = weight_codes.shape[0], 16 // made.itemsize
+            out = self._empty((codes.shape[0], -(-n // per) * per), made, codes.device, stream)[:, :n]
         return self._result("domino_logits8", _calls().logits8(
-            self.h, self.device, codes, scales, weight_codes, weight_scales, dtype == torch.bfloat16, out,
+            self.h, self.device, codes, scales, weight_codes, weight_scales, dtype, out,
             None if stream is None else B._stream(stream)))
 
     def mask_logits_penalized(self, logits, history=None, lengths=None, prompt_lengths=None, repetition=None, presence=None,
@@ -382,9 +379,9 @@ class Domino:
         those beyond the prompt one that occurs c times loses frequency * c + presence.  bias_values are added to the
         logits of bias_ids [rows, k] (below 0: none).  lengths, prompt_lengths int32 and the penalties fp32 [rows]; what is
         None penalises nothing.  mask as step_mask's or None.  The logits are not changed."""
-        import torch
         argmax, lse, lp = out if out is not None else (None, None, None)
         if self.fill_byte is not None:
+            import torch
             n = logits.shape[0]
             argmax = self._fill(argmax, n, None, torch.int32, logits, stream)
             lse = self._fill(lse, n, None, torch.float32, logits, stream) if want_lse else None
@@ -398,8 +395,8 @@ class Domino:
                               prompt_lengths=None, repetition=None, presence=None, frequency=None, bias_ids=None,
                               bias_values=None, mask=None, out=None, stream=None):
         """mask_sample of logits under mask_logits_penalized's penalties and biases."""
-        import torch
         if self.fill_byte is not None:
+            import torch
             out = self._fill(out, logits.shape[0], None, torch.int32, logits, stream)
         return self._result("domino_mask_sample_penalized", _calls().mask_sample_penalized(
             self.h, self.device, logits, history, lengths, prompt_lengths, repetition, presence, frequency, bias_ids, bias_values,

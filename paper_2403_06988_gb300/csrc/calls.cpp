@@ -13,6 +13,7 @@
 #include <ATen/ATen.h>
 #include <ATen/core/grad_mode.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
@@ -471,15 +472,28 @@ PyObject* quantize8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// (handle, device, codes, scales, weight codes, weight scales, whether bf16, out, stream)
+// The type of logits: that of `out` where none is given, fp32 where there is none either.
+int32_t logits_type(PyObject* dtype, PyObject* out) {
+    at::ScalarType t = at::kFloat;
+    if (dtype != Py_None) {
+        if (!THPDtype_Check(dtype)) throw Refused{PyExc_TypeError, "dtype", "a torch.dtype expected"};
+        t = reinterpret_cast<THPDtype*>(dtype)->scalar_type;
+    } else if (THPVariable_Check(out)) {
+        t = THPVariable_Unpack(out).scalar_type();
+    }
+    if (t != at::kFloat && t != at::kBFloat16) throw Refused{PyExc_TypeError, "dtype", "must be float32 or bfloat16"};
+    return t == at::kBFloat16 ? DOMINO_DTYPE_BF16 : DOMINO_DTYPE_F32;
+}
+
+// (handle, device, codes, scales, weight codes, weight scales, dtype, out, stream)
 PyObject* logits8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded<9>(n, [&]() -> PyObject* {
+        const int32_t dtype = logits_type(a[6], a[7]);
         const Call c(a, a[8]);
         const Codes h = codes(a[2], c.device, "codes"), w = codes(a[4], c.device, "weight codes");
         if (w.cols != h.cols) throw Refused{PyExc_ValueError, "weight codes", "the hidden codes' number of columns expected"};
         const at::Tensor hs = scales(a[3], c, "scales", h.rows, blocks(h.cols), nullptr);
         const at::Tensor ws = scales(a[5], c, "weight scales", blocks(w.rows), blocks(w.cols), nullptr);
-        const int32_t dtype = a[6] == Py_True ? DOMINO_DTYPE_BF16 : DOMINO_DTYPE_F32;
         Matrix out;
         if (a[7] == Py_None) {   // rows on 16-byte boundaries
             const int64_t per = dtype == DOMINO_DTYPE_BF16 ? 8 : 4, step = (w.rows + per - 1) / per * per;

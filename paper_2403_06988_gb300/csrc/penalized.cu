@@ -67,9 +67,6 @@ __host__ __device__ inline Layout layout(int segment, int places) {
     return l;
 }
 
-constexpr int kManyTokens = 32;            // of 128
-__device__ __forceinline__ void fetch_l2(const char* p) { asm volatile("prefetch.global.L2 [%0];\n" ::"l"(p)); }
-
 // A segment of a row: mask words w0, .. w0 + n - 1.
 struct Segment {
     uint32_t* mask;
@@ -141,12 +138,6 @@ __device__ __forceinline__ void make_segment(Segment& g, const Rows& a, int r, i
     for (int k = 0; k < kQuads; ++k) {
         const int j = (tid + k * kDecodeThreads) * 4, left = a.V - 32 * (g.w0 + j);   // of the row
         if (j >= g.n) continue;
-        // many allowed tokens: their logits are fetched to L2 meanwhile
-        if (__popc(m4[k].x) + __popc(m4[k].y) + __popc(m4[k].z) + __popc(m4[k].w) >= kManyTokens && left >= 128) {
-            const char* at = lrow + (int64_t)(g.w0 + j) * (BF16 ? 64 : 128);
-#pragma unroll
-            for (int e = 0; e < (BF16 ? 2 : 4); ++e) fetch_l2(at + 128 * e);
-        }
         if (left < 128) {   // the row's last words: no bits beyond it
             m4[k].x &= left < 32 ? (1u << left) - 1u : 0xFFFFFFFFu;
             m4[k].y &= left < 64 ? left < 32 ? 0u : (1u << (left - 32)) - 1u : 0xFFFFFFFFu;
