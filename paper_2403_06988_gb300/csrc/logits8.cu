@@ -54,7 +54,7 @@ struct Tile {
 // Registers of a thread: the fold warps' sums of 128 columns and what is on its way take more than an equal share (with 168
 // for all, loads of 16 columns and none ahead: 273 us where this takes 250; sixteen warps of 64 columns 263).  The shares'
 // sum is within what the CTA is launched with (smem_ready looks).
-constexpr int kFoldRegs = 216, kOtherRegs = 72;
+constexpr int kFoldRegs = 224, kOtherRegs = 56;
 
 // Results leave through shared memory: 32 rows of 64 bytes a warp's buffer, in the 64-byte swizzle.
 constexpr int kOutBytes = 32 * 64, kOutBuffers = 2;

@@ -30,7 +30,9 @@ namespace {
 // two parts a CTA 54 us, in one 35).
 constexpr int kSegmentWords = 4096;
 constexpr int kBiasEach = kMaxBias / kDecodeThreads;
-constexpr int kPenalizedSmem = 100 * 1024; // of a CTA, at most: two an SM
+// Of a CTA, at most.  Long histories take an SM for a row rather than more parts of it: 100 x 128256 with 16000 tokens each 36
+// us, in parts that leave room for two CTAs an SM 132.
+constexpr int kPenalizedSmem = 212 * 1024;
 constexpr int kQuads = kSegmentWords / 4 / kDecodeThreads;   // four mask words each, of a thread
 constexpr int kHeld = 8;                   // history tokens a thread keeps, of each 512
 static_assert(kQuads == 2 && kBiasEach * kDecodeThreads == kMaxBias);
