@@ -23,6 +23,7 @@ namespace domino {
 namespace {
 
 constexpr int kRowThreads8 = 512;         // of a row, at most
+constexpr int kFewThreads = 256;          // of a row that they can hold
 constexpr int kCtaThreads = 128;          // of a CTA, at least: short rows share one
 constexpr int kMaxVectors = 4;            // of a thread, in registers
 constexpr int32_t kLongRow = kRowThreads8 * kMaxVectors * kN;   // longer rows are read twice
@@ -118,8 +119,15 @@ __device__ __forceinline__ float root_of(float sum, const NormArgs& a) {
 }
 
 // blockDim.y rows a CTA, of blockDim.x threads with VECTORS times eight values each.
+// Registers of bf16 rows on 16-byte boundaries are held down so that an SM has 1024 to 2048 threads (16384 rows, us in codes,
+// held down / not: 8192 wide 137, 150; 4096 73, 77; 2048 44, 51; fp32 and rows off the boundaries lose by it).
+template <bool BF16, bool ALIGNED, int VECTORS>
+constexpr int kNormThreads = BF16 && ALIGNED && VECTORS <= 2 ? kFewThreads : kRowThreads8;
+template <bool BF16, bool ALIGNED, int VECTORS>
+constexpr int kNormCtas = !(BF16 && ALIGNED) ? 0 : VECTORS == 1 ? 8 : VECTORS == 2 ? 6 : 2;   // 0: as many as there are
 template <bool BF16, bool ALIGNED, bool CODES, int VECTORS>
-__global__ void __launch_bounds__(kRowThreads8) norm_kernel(const __grid_constant__ NormArgs a, const bool far) {
+__global__ void __launch_bounds__(kNormThreads<BF16, ALIGNED, VECTORS>, kNormCtas<BF16, ALIGNED, VECTORS>)
+    norm_kernel(const __grid_constant__ NormArgs a, const bool far) {
     __shared__ float s_part[kCtaThreads / 32][kRowThreads8 / 32];
     const int lane = threadIdx.x & 31;
     const int32_t row = blockIdx.x * blockDim.y + threadIdx.y;
@@ -582,8 +590,8 @@ cudaError_t launch_norm_t(const NormArgs& a, cudaStream_t st) {
     if (a.dim > kLongRow)
         return launch_pdl(norm_long_kernel<BF16, ALIGNED, CODES>, dim3((unsigned)a.rows), dim3(kRowThreads8), 0, st, a, far);
     // 256 threads a row where they can hold it: a CTA's row waits at one barrier, and smaller CTAs wait less (16384 x 4096
-    // bf16: norm 78 us, in codes 77; with 512 threads 102 and 102)
-    const Cut c = cut_row(a.dim, a.dim <= 256 * kMaxVectors * kN ? 256 : kRowThreads8);
+    // bf16: norm 78 us, in codes 77; with 512 threads 102 and 102, before registers were held down)
+    const Cut c = cut_row(a.dim, a.dim <= kFewThreads * kMaxVectors * kN ? kFewThreads : kRowThreads8);
     const dim3 grid((unsigned)ceil_div(a.rows, c.rows)), block((unsigned)c.threads, (unsigned)c.rows);
     switch (c.vectors) {
         case 1: return launch_pdl(norm_kernel<BF16, ALIGNED, CODES, 1>, grid, block, 0, st, a, far);
