@@ -127,7 +127,15 @@ struct Vec8<true, false> {
         x.zero();
         if (dim > c) x.load(static_cast<const __nv_bfloat16*>(row) + c, dim - c);
     }
-    __device__ __forceinline__ void get(float (&f)[kN]) const { x.get(f); }
+    __device__ __forceinline__ void get(float (&f)[kN]) const {
+        const uint4 u = eight_from(x.u, x.v, x.off);
+        f[0] = bf16_lo(u.x), f[1] = bf16_hi(u.x), f[2] = bf16_lo(u.y), f[3] = bf16_hi(u.y);
+        f[4] = bf16_lo(u.z), f[5] = bf16_hi(u.z), f[6] = bf16_lo(u.w), f[7] = bf16_hi(u.w);
+        if (x.n < kN) {   // the row's end
+#pragma unroll
+            for (int e = 0; e < kN; ++e) f[e] = (uint32_t)e < x.n ? f[e] : 0.0f;
+        }
+    }
 };
 template <>
 struct Vec8<false, true> {
@@ -150,23 +158,93 @@ struct Vec8<false, true> {
     }
 };
 template <>
-struct Vec8<false, false> {
-    float x[kN];
-    __device__ __forceinline__ void keep() {}
+struct Vec8<false, false> {   // three blocks hold them (norm of 8000 x 333 10.8 us, read and written one by one 15.1)
+    float4 a, b, c4;
+    uint32_t off, n;
+    __device__ __forceinline__ void keep() {   // in two blocks from now on
+        float f[kN];
+        get(f);
+        a = make_float4(f[0], f[1], f[2], f[3]);
+        b = make_float4(f[4], f[5], f[6], f[7]);
+        c4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        off = 0u;
+        n = kN;
+    }
     __device__ __forceinline__ void load(const void* row, int32_t c, int32_t dim) {
-#pragma unroll
-        for (int e = 0; e < kN; ++e) x[e] = c + e < dim ? static_cast<const float*>(row)[c + e] : 0.0f;
+        a = b = c4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        off = 0u;
+        n = kN;
+        if (c >= dim) return;
+        const uintptr_t at = reinterpret_cast<uintptr_t>(static_cast<const float*>(row) + c);
+        const float4* block = reinterpret_cast<const float4*>(at & ~(uintptr_t)15);
+        off = (uint32_t)(at & 15) / 4;
+        n = (uint32_t)min(dim - c, kN);
+        a = block[0];
+        if (off + n > 4) b = block[1];
+        if (off + n > 8) c4 = block[2];
     }
     __device__ __forceinline__ void get(float (&f)[kN]) const {
+        float w[12] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, c4.x, c4.y, c4.z, c4.w};
 #pragma unroll
-        for (int e = 0; e < kN; ++e) f[e] = x[e];
+        for (int e = 0; e < kN + 1; ++e) w[e] = off & 2u ? w[e + 2] : w[e];
+#pragma unroll
+        for (int e = 0; e < kN; ++e) f[e] = off & 1u ? w[e + 1] : w[e];
+        if (n < kN) {
+#pragma unroll
+            for (int e = 0; e < kN; ++e) f[e] = (uint32_t)e < n ? f[e] : 0.0f;
+        }
     }
 };
+
+// Eight values of a weight.  What rows off the boundaries are multiplied with is on one all the same; where it is not, value
+// by value.
 template <bool BF16, bool ALIGNED>
-__device__ __forceinline__ void load8(const void* row, int32_t c, int32_t dim, float (&f)[kN]) {
-    Vec8<BF16, ALIGNED> v;
-    v.load(row, c, dim);
-    v.get(f);
+struct VecOf : Vec8<BF16, true> {
+    __device__ __forceinline__ void load(const void* p, int32_t c, int32_t dim) {
+        const bool on = ALIGNED || (reinterpret_cast<uintptr_t>(p) & 15) == 0;
+        Vec8<BF16, true>::load(p, c, on ? dim : 0);
+        if (on) return;
+        this->left = dim - c;
+        if constexpr (BF16) {
+            uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int e = 0; e < kN; ++e)
+                if (e < this->left) w[e / 2] |= (uint32_t) static_cast<const unsigned short*>(p)[c + e] << (16 * (e & 1));
+            this->u = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+            float f[kN];
+#pragma unroll
+            for (int e = 0; e < kN; ++e) f[e] = e < this->left ? static_cast<const float*>(p)[c + e] : 0.0f;
+            this->u = make_float4(f[0], f[1], f[2], f[3]);
+            this->v = make_float4(f[4], f[5], f[6], f[7]);
+        }
+    }
+};
+// A warp's 256 consecutive fp32 values (eight a lane, `left` of this lane's to the row's end) to a row at any alignment: in
+// 16-byte blocks, each lane's first with the last values of the lane before it, and one by one at the two ends.
+__device__ __forceinline__ void store_any4(float* p, const float (&f)[kN], int32_t left, int lane) {
+    const int off = (int)(reinterpret_cast<uintptr_t>(p) & 15) / 4;   // the same in every lane
+    float w[kN + 3];   // from off values before the lane's first
+    const float p5 = __shfl_up_sync(0xffffffffu, f[5], 1), p6 = __shfl_up_sync(0xffffffffu, f[6], 1), p7 = __shfl_up_sync(0xffffffffu, f[7], 1);
+    const float all[kN + 3] = {p5, p6, p7, f[0], f[1], f[2], f[3], f[4], f[5], f[6], f[7]};
+    // w[k] = all[k + 3 - off]
+#pragma unroll
+    for (int k = 0; k < kN; ++k) {
+        const float x0 = all[k + 3], x1 = all[k + 2], x2 = all[k + 1], x3 = all[k];
+        w[k] = off & 2 ? (off & 1 ? x3 : x2) : (off & 1 ? x1 : x0);
+    }
+    float4* block = reinterpret_cast<float4*>(p - off);
+    const bool first = (off == 0 || lane > 0) && left >= 4 - off, second = left >= 8 - off;
+    const bool next = off > 0 && lane < 31 && left - kN >= 4 - off;   // the next lane writes this one's last values
+    if (first) block[0] = make_float4(w[0], w[1], w[2], w[3]);
+    if (second) block[1] = make_float4(w[4], w[5], w[6], w[7]);
+    if (!first || !second || (off > 0 && !next)) {
+#pragma unroll
+        for (int e = 0; e < kN; ++e) {
+            const bool done = e < 4 - off ? first : e < 8 - off ? second : next;
+            if (e < left && !done) p[e] = f[e];
+        }
+    }
 }
 
 // The same values to a row.  The whole warp calls it, its lanes with consecutive c's.  far: past the L2.
@@ -199,10 +277,12 @@ __device__ __forceinline__ void store8(void* row, int32_t c, int32_t dim, const 
                 reinterpret_cast<float4*>(p)[0] = u;
                 reinterpret_cast<float4*>(p)[1] = v;
             }
-        } else {
+        } else if constexpr (ALIGNED) {
 #pragma unroll
             for (int e = 0; e < kN; ++e)
                 if (e < left) p[e] = f[e];
+        } else {
+            store_any4(p, f, left, lane);
         }
     }
 }
