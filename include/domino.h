@@ -491,7 +491,8 @@ int domino_embed_grad(domino_t h, const int32_t* tokens_dev, int32_t n, const vo
  * Codes are e4m3 (8 bits: 4 of exponent, 3 of mantissa, largest 448) with a float
  * scale for each block of 128 values along a row (the last block of a row may be
  * shorter), for one row or for 128 rows together:
- *   a = the largest |v| of the block, at least 2^-100;  scale = a / 448;
+ *   a = the largest |v| of the block, at least 2^-100;
+ *   scale = a / 448 (a times the rounded 1 / 448, in fp32);
  *   code = e4m3(v (448 / a)), ties to even;  v is about code * scale.
  * Rows of codes begin on 16-byte boundaries (pointer and stride are multiples of 16,
  * DOMINO_E_INVALID_ARG else); bytes of a row at or beyond dim are neither read nor
