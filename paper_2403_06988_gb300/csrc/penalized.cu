@@ -355,8 +355,6 @@ cudaError_t launch_penalized(const PenalizedArgs& p, const LaunchEnv& env, cudaS
     a.stride = p.stride;
     a.mask = p.mask;
     a.p = p.p;
-    if (!a.p.history_dev) a.p.history_len = 0;
-    if (a.p.history_len == 0) a.p.lengths_dev = nullptr;
     a.V = p.n_tokens;
     a.W = (p.n_tokens + 31) / 32;
     a.argmax = p.argmax;
