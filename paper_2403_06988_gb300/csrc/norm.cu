@@ -247,6 +247,17 @@ constexpr int kGradThreads = 256;         // of a row, at most
 constexpr int kGradVectors = 4;
 constexpr int32_t kGradLongRow = kGradThreads * kGradVectors * kN;
 
+// A CTA's blockDim.y strips of rows.
+struct Strip {
+    int32_t row0, row1, most;   // most: rows of the longest strip, all take part in the barriers
+    __device__ __forceinline__ Strip(int32_t rows, int32_t strips) {
+        const int32_t i = blockIdx.x * blockDim.y + threadIdx.y;
+        row0 = i < strips ? (int32_t)((int64_t)rows * i / strips) : 0;
+        row1 = i < strips ? (int32_t)((int64_t)rows * (i + 1) / strips) : 0;
+        most = (rows + strips - 1) / strips;
+    }
+};
+
 // A CTA's rows (blockDim.y strips of them, threads as in norm_kernel) one after the other; the strip's part of dw stays
 // in registers and goes to parts[strip][pitch].
 // (Registers of fp32 rows off 16-byte boundaries are held down: 8000 x 333 19.4 us, else 21.3.)
@@ -255,12 +266,9 @@ __global__ void __launch_bounds__(kGradThreads, !BF16 && !ALIGNED && VECTORS == 
                                                                  const int32_t strips, const int32_t pitch, const bool far) {
     __shared__ float s_part[2][kCtaThreads / 32][kRowThreads8 / 32];
     const int lane = threadIdx.x & 31;
-    const int32_t strip = blockIdx.x * blockDim.y + threadIdx.y;
+    const Strip t(a.rows, strips);
     pdl_wait();
     pdl_trigger();
-    const int32_t row0 = strip < strips ? (int32_t)((int64_t)a.rows * strip / strips) : 0;
-    const int32_t row1 = strip < strips ? (int32_t)((int64_t)a.rows * (strip + 1) / strips) : 0;
-    const int32_t most = (a.rows + strips - 1) / strips;   // the CTA's strips differ by a row: all take part in the barriers
     VecOf<BF16, ALIGNED> w[VECTORS];
     float dw[VECTORS][kN];
 #pragma unroll
@@ -269,9 +277,9 @@ __global__ void __launch_bounds__(kGradThreads, !BF16 && !ALIGNED && VECTORS == 
 #pragma unroll
         for (int e = 0; e < kN; ++e) dw[j][e] = 0.0f;
     }
-    for (int32_t i = 0; i < most; ++i) {
-        const int32_t row = row0 + i;
-        const bool on = row < row1;
+    for (int32_t i = 0; i < t.most; ++i) {
+        const int32_t row = t.row0 + i;
+        const bool on = row < t.row1;
         const int32_t dim = on ? a.dim : 0;
         const char* ph = at_row<BF16>(a.h, row, a.h_stride);
         const char* pd = at_row<BF16>(a.dy, row, a.dy_stride);
@@ -313,7 +321,8 @@ __global__ void __launch_bounds__(kGradThreads, !BF16 && !ALIGNED && VECTORS == 
             store8<BF16, ALIGNED>(at_row<BF16>(a.dx, row, a.dx_stride), (threadIdx.x + j * blockDim.x) * kN, a.dim, g, far, lane);
         }
     }
-    if (strip >= strips) return;
+    if (t.row0 >= t.row1) return;
+    const int32_t strip = blockIdx.x * blockDim.y + threadIdx.y;
 #pragma unroll
     for (int j = 0; j < VECTORS; ++j) {
         const int32_t c = (threadIdx.x + j * blockDim.x) * kN;
@@ -375,17 +384,6 @@ struct Ahead {
                          : "r"(at(slot, array, j))
                          : "memory");
         return v;
-    }
-};
-
-// A CTA's blockDim.y strips of rows.
-struct Strip {
-    int32_t row0, row1, most;   // most: rows of the longest strip, all take part in the barriers
-    __device__ __forceinline__ Strip(int32_t rows, int32_t strips) {
-        const int32_t i = blockIdx.x * blockDim.y + threadIdx.y;
-        row0 = i < strips ? (int32_t)((int64_t)rows * i / strips) : 0;
-        row1 = i < strips ? (int32_t)((int64_t)rows * (i + 1) / strips) : 0;
-        most = (rows + strips - 1) / strips;
     }
 };
 
@@ -675,7 +673,7 @@ cudaError_t launch_grad_t(const NormGradArgs& a, const LaunchEnv& env, void* spa
         if (e != cudaSuccess) return e;
         e = launch_pdl(norm_grad_long_kernel<BF16, ALIGNED>, dim3((unsigned)ceil_div(a.dim, kGradThreads * kN), (unsigned)g.strips),
                        dim3(kGradThreads), 0, st, a, (const float*)sums, parts, g.strips, g.pitch, far);
-    } else if (g.stream) {
+    } else if constexpr (BF16 && ALIGNED) {   // as cut_grad divides them
         switch (g.cut.vectors) {
             case 1: e = launch_grad_stream<1>(a, g, parts, far, st); break;
             case 2: e = launch_grad_stream<2>(a, g, parts, far, st); break;

@@ -33,18 +33,6 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
         : "memory");
     return ok != 0;
 }
-// bar_try that does not wait.
-__device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n.reg .pred p;\n"
-        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
-        "selp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
 // The address in the cluster of what lies at `addr` in CTA `rank`.
 __device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
     uint32_t r;
@@ -294,8 +282,8 @@ __device__ __forceinline__ void tmem_wait32(uint32_t (&r)[32]) {
     asm volatile("" : "+r"(r[30]), "+r"(r[31]));
 }
 
-// tmem_load32 of 16 columns.
-__device__ __forceinline__ void tmem_load16(float (&v)[16], uint32_t addr) {
+// tmem_load32 of 16 columns, added to v.
+__device__ __forceinline__ void tmem_add16(float* v, uint32_t addr) {
     uint32_t r[16];
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
@@ -306,14 +294,7 @@ __device__ __forceinline__ void tmem_load16(float (&v)[16], uint32_t addr) {
         : "r"(addr)
         : "memory");
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
-}
-// They, added to v.
-__device__ __forceinline__ void tmem_add16(float* v, uint32_t addr) {
-    float r[16];
-    tmem_load16(r, addr);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] += r[i];
+    for (int i = 0; i < 16; ++i) v[i] += __uint_as_float(r[i]);
 }
 
 }  // namespace
