@@ -505,7 +505,8 @@ int domino_embed_grad(domino_t h, const int32_t* tokens_dev, int32_t n, const vo
  * [rows][stride], weight_dev [dim], all of dtype (fp32 or bf16); rstd_dev float [rows] or
  * NULL.  sum_dev may be residual_dev or x_dev, with the same stride.  eps >= 0 and
  * finite; a row of zeros with eps = 0 has no norm (NaN), nor has one whose sum of squares
- * is beyond fp32.  Needs no scratch. */
+ * is beyond fp32, and with eps = 0 values below 2^-63 lose accuracy, their squares being
+ * below fp32's normal numbers.  Needs no scratch. */
 int domino_norm(domino_t h, const void* x_dev, int64_t x_stride, const void* residual_dev, int64_t residual_stride,
                 const void* weight_dev, int32_t dtype, int32_t rows, int32_t dim, float eps, void* y_dev,
                 int64_t y_stride, void* sum_dev, int64_t sum_stride, float* rstd_dev, void* stream);
@@ -522,7 +523,8 @@ int domino_norm8(domino_t h, const void* x_dev, int64_t x_stride, const void* re
  *   g = weight dy,  dx = rstd (g - h rstd^2 mean(g h)) + dsum   (of x and of the residual),
  *   dweight = the sum over the rows of dy h rstd,
  * all of dtype, rounded once.  dx_dev may be dsum_dev or dy_dev, with the same
- * stride.  Takes scratch: up to 32 fp32 rows of dim for each SM. */
+ * stride.  Takes scratch: up to 32 fp32 rows of dim for each SM, and where dim is above
+ * 8192 4 bytes a row. */
 int domino_norm_grad(domino_t h, const void* sum_dev, int64_t sum_stride, const void* weight_dev, const float* rstd_dev,
                      const void* dy_dev, int64_t dy_stride, const void* dsum_dev, int64_t dsum_stride, int32_t dtype,
                      int32_t rows, int32_t dim, void* dx_dev, int64_t dx_stride, void* dweight_dev, void* stream);
@@ -538,7 +540,8 @@ int domino_quantize8(domino_t h, const void* x_dev, int64_t x_stride, int32_t dt
  *                  (sum over the block's k of hidden[t][k] weight[v][k]).
  * hidden_dev [rows][hidden_stride] with scales [rows][ceil(dim / 128)]; weight_dev
  * [n_tokens][weight_stride] with scales [ceil(n_tokens / 128)][ceil(dim / 128)]; logits_dev
- * [rows][logits_stride] of dtype (fp32 or bf16).  Sums are fp32, rounded once to dtype.
+ * [rows][logits_stride] of dtype (fp32 or bf16).  Sums are fp32, rounded once to dtype; the
+ * product of a block's two scales is one rounded fp32 number and has to be finite.
  * Logits whose rows are on 16-byte boundaries are written faster.  Needs no scratch. */
 int domino_logits8(domino_t h, const uint8_t* hidden_dev, int64_t hidden_stride, const float* hidden_scales_dev,
                    const uint8_t* weight_dev, int64_t weight_stride, const float* weight_scales_dev, int32_t rows,
