@@ -12,7 +12,9 @@
 // All of it is bound by HBM: a row is read once, kept in registers between its sum of
 // squares and its use, and written once.  Sums are fp32; y, the codes, dx and dw are
 // rounded once each.  Products and sums are fused where the code says so and nowhere
-// else: rows at any alignment give the same bits.
+// else.  The norm's rows give the same bits at any alignment, and so do the gradient's of
+// fp32 and of more than 8192 columns; other bf16 rows of the gradient are divided otherwise
+// on 16-byte boundaries than off them, which orders its sums otherwise.
 #include <algorithm>
 #include <atomic>
 
