@@ -615,7 +615,9 @@ __device__ __forceinline__ void decode_combine(DecodeShared& sh, float& m, int& 
 // Log-probabilities of a slice's tokens (tok0 a multiple of 128): logit - lse
 // where allowed, -inf elsewhere.  Rows on 32-byte boundaries of the output and
 // 16-byte boundaries of the logits: a thread takes 8 tokens (one 32-byte
-// store); rows of V % 4 == 0: 4 tokens; else one.
+// store); rows of V % 4 == 0 on 16-byte boundaries: 4 tokens; else four at a
+// time from the output's first 16-byte boundary on, and the at most six tokens
+// at the two ends one by one.
 template <bool BF16, int THREADS = kDecodeThreads>
 __device__ __forceinline__ void write_logprobs(const char* lrow, int V, const uint32_t* s_mask, int tok0, int ntok,
                                                float lse, float* orow, int tid) {

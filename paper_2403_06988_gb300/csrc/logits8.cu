@@ -13,8 +13,9 @@
 // Few rows: bound by HBM (64 x 128256 x 4096 90 us, 6.2 TB/s).  Many: by the folds.  A block
 // of 128 x 256 products takes the tensor cores 512 cycles, its 32 KB from L2 about 640, and
 // the fold's 32768 fused products on 128 lanes 256, between waits that two warps a scheduler
-// do not hide: 970 cycles in all (2048 x 128256 x 4096 820 us, 2.6 PFLOP/s; with a
-// quarter of the fused products, timed alone, 3.1).
+// do not hide: 970 cycles in all (2048 x 38912 x 4096 252 us, 2.6 PFLOP/s; with a quarter of
+// the fused products, timed alone, 214).  Larger calls are held by the power cap too: 2048 x
+// 128256 x 4096 850 to 905 us, 2.4 to 2.5 PFLOP/s; of values that are nearly alike 800.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -52,8 +53,8 @@ struct Tile {
     static_assert(kColumns % 32 == 0 && 128 % kColumns == 0 && kAccs * kPartN <= 512);
 };
 // Registers of a thread: the fold warps' sums of 128 columns and what is on its way take more than an equal share (with 168
-// for all, loads of 16 columns and none ahead: 273 us where this takes 250; sixteen warps of 64 columns 263).  The shares'
-// sum is within what the CTA is launched with (smem_ready looks).
+// for all, loads of 16 columns and none ahead: 273 us where this takes 250; sixteen warps of 64 columns 263; 216 for 224
+// alike).  The shares' sum is within what the CTA is launched with (smem_ready looks).
 constexpr int kFoldRegs = 224, kOtherRegs = 56;
 
 // Results leave through shared memory: 32 rows of 64 bytes a warp's buffer, in the 64-byte swizzle.

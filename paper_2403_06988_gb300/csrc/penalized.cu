@@ -14,9 +14,10 @@
 //
 // 256 x 128256 bf16, a third of the rows dense, histories of up to 4096 tokens: 28 us, of which
 // the decode alone takes 24 (the bytes' floor is 10.6): most SMs have two of the 256 rows, and a
-// row's fold waits for its loads and for its own results (the SMs issue in a quarter of the
+// row's fold waits for its loads and for its own results (the SMs issue in half of the
 // cycles).  More CTAs a row cost more than they share out: 32 us with two, 52 with four.  One
-// row is a chain of five latencies of memory and ten barriers: 7.9 us.
+// row is a chain of five latencies of memory and ten barriers: 7.9 us.  Draws: 96 us, 89 with
+// histories of up to 64 tokens (greedy 24); one row 8.7.
 #include <algorithm>
 #include <atomic>
 
@@ -26,8 +27,9 @@
 namespace domino {
 namespace {
 
-// Mask words of a row at a time, at most: 131072 tokens, the usual vocabularies whole (128 x 152064 with log-probabilities in
-// two parts a CTA 54 us, in one 35).
+// Mask words of a row at a time, at most: 131072 tokens, most vocabularies whole.  More go in two parts (160 x 131072 24 us,
+// with log-probabilities, for which each part is made again, 44; x 152064 33 and 65), unless two CTAs share them out (128 x
+// 152064 20 and 33).
 constexpr int kSegmentWords = 4096;
 constexpr int kBiasEach = kMaxBias / kDecodeThreads;
 // Of a CTA, at most.  Long histories take an SM for a row rather than more parts of it: 100 x 128256 with 16000 tokens each 36
